@@ -29,7 +29,7 @@
  *  - `stream` is a hipStream_t (NULL = the default stream). Every call only
  *    enqueues work on `stream` and returns without synchronising; outputs
  *    are valid once the stream reaches that point. No call but
- *    countdown_plan_create / countdown_plan_destroy / countdown_calibrate
+ *    those that create or destroy a handle and countdown_calibrate
  *    allocates device memory.
  *  - thld is one fp32 constant per layer (Sec. 4: the calibrated layerwise
  *    threshold). Selection is strict (coefficient > thld). thld = -INFINITY
@@ -322,6 +322,132 @@ cd_status countdown_plan_set_phases(cd_plan *plan, unsigned phases);
  * `stream`; CD_EINVAL for bad arguments.
  */
 cd_status countdown_stream_read(const void *src, size_t bytes, uint32_t *sink, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection. A pool holds
+ * n_adapters adapters of one rank r beside a projection d_in -> d_out:
+ *   A [n_adapters][rank][d_in] bf16, B [n_adapters][d_out][rank] bf16,
+ *   scale [n_adapters] fp32 (NULL: 1 for every adapter).
+ * Token t uses adapter a = ids[t]; with ids[t] outside [0, n_adapters) (by
+ * convention -1) it uses none, and A, B and scale are not read for it. An
+ * adapter of a smaller rank is stored with zero rows of A (columns of B).
+ *   lat_t = A_a x_t,   delta_t = scale_a B_a lat_t   (0 without an adapter).
+ * Products and sums are fp32; lat is not rounded below fp32.
+ *
+ * Conventions beyond those at the top of this file:
+ *  - ids int32[T] and scale are 4-byte aligned device arrays, all other
+ *    pointers 16-byte aligned. They are read by the kernels: calls can be
+ *    captured in a graph and replayed with other values behind the pointers.
+ *  - x, dy, base, y and dx are row-major with a row stride (ld*, in elements,
+ *    a multiple of 8, at least the row's width), so they may be column slices
+ *    of wider tensors; what lies between their rows is left as it was.
+ *  - `type` (CD_TYPE_*) is the type of y and base (of dx and base in the
+ *    backward call); each result is rounded to it once, to nearest even.
+ *  - base may be the output itself (same pointer and stride). Otherwise an
+ *    output must share no element with an input or with another output
+ *    (CD_EINVAL; tensors of different row strides whose ranges touch count as
+ *    sharing).
+ *  - T = 0 is a valid empty call (the backward call then writes zeros to dA
+ *    and dB). T > max_tokens is CD_EINVAL.
+ *  - Results do not depend on timing: the same call on the same inputs gives
+ *    the same bits.
+ *  - A pool belongs to the device current at its creation, and its workspace
+ *    serves one call at a time: calls on one pool must not overlap (two
+ *    streams, two graphs replayed at once); use one pool each.
+ */
+#define CD_TYPE_F32 0
+#define CD_TYPE_BF16 1
+
+typedef struct cd_adapters cd_adapters;
+
+/* Flags of countdown_adapters_create. */
+#define CD_ADAPTERS_TRAIN 1u  /* also allocate the workspace of the backward call */
+
+/*
+ * Create the workspace of a pool's calls on the current device. d_in and d_out:
+ * positive multiples of 8 up to 65536; rank: a multiple of 8 up to 256;
+ * 1 <= n_adapters <= 1024; 1 <= max_tokens <= 2^20. CD_EINVAL for malformed
+ * sizes and unknown flags, CD_EUNSUPPORTED beyond those limits (both before any
+ * HIP call), CD_ENOMEM / CD_EHIP when allocation fails. *out is set only on
+ * success. Holds rank floats per token, with CD_ADAPTERS_TRAIN twice that.
+ */
+cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapters, int max_tokens,
+                                    unsigned flags, cd_adapters **out);
+
+/* Release a pool's workspace (synchronises the device first). NULL is a no-op. */
+cd_status countdown_adapters_destroy(cd_adapters *ad);
+
+/*
+ * y_t = W x_t + delta_t for a decode batch of T <= 16 tokens (CD_EUNSUPPORTED
+ * beyond): W [d_out][d_in] bf16 is streamed once for all of them. For more
+ * tokens the projection is a matrix product of its own, and
+ * countdown_adapters_add adds to it.
+ */
+cd_status countdown_adapters_project(cd_adapters *ad, const uint16_t *x, size_t ldx, int T,
+                                     const uint16_t *W, const int32_t *ids, const uint16_t *A,
+                                     const uint16_t *B, const float *scale, int type, void *y,
+                                     size_t ldy, void *stream);
+
+/*
+ * y_t = base_t + delta_t for any number of tokens (base NULL: y_t = delta_t).
+ * base is what a shared projection gave: an FFN call's y, or a prompt's product.
+ */
+cd_status countdown_adapters_add(cd_adapters *ad, const uint16_t *x, size_t ldx, int T,
+                                 const int32_t *ids, const uint16_t *A, const uint16_t *B,
+                                 const float *scale, int type, const void *base, size_t ldb,
+                                 void *y, size_t ldy, void *stream);
+
+/*
+ * Gradients of sum_t <dy_t, delta_t> (a CD_ADAPTERS_TRAIN pool, else CD_EINVAL):
+ *   glat_t = scale_a B_a^T dy_t,   dx_t = base_t + A_a^T glat_t,
+ *   dA_a = sum_{t: ids[t] = a} glat_t x_t^T,
+ *   dB_a = sum_{t: ids[t] = a} dy_t (scale_a lat_t)^T.
+ * dy [T][d_out] bf16. dx [T][d_in] of `type`; base, if given, is the gradient
+ * that reached x by other paths (the shared projection's W^T dy). dA
+ * [n_adapters][rank][d_in] and dB [n_adapters][d_out][rank] fp32 are
+ * overwritten whole (zeros where no token uses the adapter). dx, dA and dB may
+ * each be NULL: that gradient is not computed.
+ */
+cd_status countdown_adapters_backward(cd_adapters *ad, const uint16_t *x, size_t ldx,
+                                      const uint16_t *dy, size_t lddy, int T, const int32_t *ids,
+                                      const uint16_t *A, const uint16_t *B, const float *scale,
+                                      int type, const void *base, size_t ldb, void *dx,
+                                      size_t lddx, float *dA, float *dB, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The global gradient norm over many tensors, and clipping:
+ *   norm = sqrt(sum over all tensors and elements of g^2)   (fp64),
+ *   out  = g * fp32(max_norm / norm) if norm > max_norm, else g.
+ * A norm that is not finite (an infinity or NaN among the gradients) leaves
+ * out = g; the caller sees it in *norm and can skip its step.
+ */
+typedef struct cd_clip cd_clip;
+
+typedef struct {
+    const void *grad;  /* device, `count` contiguous elements; any alignment of its type */
+    void *out;         /* device, same count and type: == grad (in place) or elsewhere */
+    size_t count;      /* 0: an empty tensor, its pointers are not used */
+    int type;          /* CD_TYPE_F32 or CD_TYPE_BF16 */
+} cd_grad;
+
+/* Create the workspace for calls with up to max_tensors (<= 65536) tensors on the current device. */
+cd_status countdown_clip_create(int max_tensors, cd_clip **out);
+/* Release it (synchronises the device first). NULL is a no-op. */
+cd_status countdown_clip_destroy(cd_clip *clip);
+
+/*
+ * The norm of n tensors into *norm (a device double, 8-byte aligned, may be
+ * NULL), and the scaled tensors. `grads` is a HOST array, read before the call
+ * returns. max_norm >= 0 (NaN: CD_EINVAL); with max_norm = +INFINITY nothing is
+ * scaled, and an `out` that is NULL or the gradient itself is not written. With
+ * a finite max_norm every non-empty tensor needs an out. Outputs must not share
+ * memory with each other, with *norm or, but for an out that is its own grad
+ * (same pointer), with a gradient. n = 0 gives norm 0. Squares and their sums
+ * are fp64 and added in a fixed order: the norm has the same bits every time.
+ * Calls on one cd_clip must not overlap.
+ */
+cd_status countdown_clip_grads(cd_clip *clip, const cd_grad *grads, int n, double max_norm,
+                               double *norm, void *stream);
 
 /*
  * Host-only validation of an FFN call's arguments against a shape, exactly

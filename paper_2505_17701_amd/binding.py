@@ -21,6 +21,8 @@ CD_VARIANT_MONO, CD_VARIANT_DUAL_IDEAL, CD_VARIANT_DUAL_PRED, CD_VARIANT_DENSE =
 CD_VARIANT_CATS, CD_VARIANT_DUAL_TERN = 4, 5
 CD_PLAN_KEEP_COEF, CD_PLAN_DETERMINISTIC = 1, 2
 CD_PHASE_COEF, CD_PHASE_DOWN, CD_PHASE_ALL = 1, 2, 3
+CD_TYPE_F32, CD_TYPE_BF16 = 0, 1
+CD_ADAPTERS_TRAIN = 1
 
 # every symbol include/countdown.h declares
 EXPORTS = (
@@ -32,6 +34,9 @@ EXPORTS = (
     "countdown_export_active",
     "countdown_plan_set_phases", "countdown_stream_read", "countdown_check_args",
     "countdown_check_shape", "countdown_status_string", "countdown_abi_version",
+    "countdown_adapters_create", "countdown_adapters_destroy", "countdown_adapters_project",
+    "countdown_adapters_add", "countdown_adapters_backward",
+    "countdown_clip_create", "countdown_clip_destroy", "countdown_clip_grads",
 )
 
 _lib = None
@@ -53,6 +58,7 @@ def load_library(path: str = LIB_PATH):
                            "(python -m paper_2505_17701_amd.build)")
     lib = C.CDLL(path)
     vp, i, u, f, d = C.c_void_p, C.c_int, C.c_uint, C.c_float, C.c_double
+    z = C.c_size_t
     sig = {
         "countdown_plan_create": (i, [i, i, i, i, u, C.POINTER(vp)]),
         "countdown_plan_destroy": (i, [vp]),
@@ -77,6 +83,15 @@ def load_library(path: str = LIB_PATH):
         "countdown_check_shape": (i, [i, i, i, i]),
         "countdown_status_string": (C.c_char_p, [i]),
         "countdown_abi_version": (i, []),
+        "countdown_adapters_create": (i, [i, i, i, i, i, u, C.POINTER(vp)]),
+        "countdown_adapters_destroy": (i, [vp]),
+        "countdown_adapters_project": (i, [vp, vp, z, i, vp, vp, vp, vp, vp, i, vp, z, vp]),
+        "countdown_adapters_add": (i, [vp, vp, z, i, vp, vp, vp, vp, i, vp, z, vp, z, vp]),
+        "countdown_adapters_backward": (i, [vp, vp, z, vp, z, i, vp, vp, vp, vp, i, vp, z, vp, z,
+                                            vp, vp, vp]),
+        "countdown_clip_create": (i, [i, C.POINTER(vp)]),
+        "countdown_clip_destroy": (i, [vp]),
+        "countdown_clip_grads": (i, [vp, vp, i, d, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -470,6 +485,242 @@ def countdown_stream_read(src, sink, stream=None) -> None:
     _check(load_library().countdown_stream_read(
         _ptr(src), src.numel() * src.element_size(), _ptr(sink), _stream(stream)),
         "countdown_stream_read")
+
+
+class Adapters:
+    """Owns a ``cd_adapters``: the workspace of the calls on a pool of ``n_adapters`` low-rank
+    adapters beside a ``d_in`` -> ``d_out`` projection, for up to ``max_tokens`` tokens a
+    call (``train``: the backward call too). The weights stay with the caller:
+    A [n_adapters, rank, d_in] and B [n_adapters, d_out, rank], bf16."""
+
+    def __init__(self, d_in: int, d_out: int, rank: int, n_adapters: int, max_tokens: int,
+                 train: bool = False):
+        self.d_in, self.d_out, self.rank = d_in, d_out, rank
+        self.n_adapters, self.max_tokens, self.train = n_adapters, max_tokens, train
+        self._a_shape = (n_adapters, rank, d_in)
+        self._b_shape = (n_adapters, d_out, rank)
+        h = C.c_void_p()
+        _check(load_library().countdown_adapters_create(
+            d_in, d_out, rank, n_adapters, max_tokens, CD_ADAPTERS_TRAIN if train else 0,
+            C.byref(h)), "countdown_adapters_create")
+        self.handle = h.value
+        self.device = (_torch or _use_torch()).cuda.current_device()
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(load_library().countdown_adapters_destroy(self.handle),
+                   "countdown_adapters_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+def countdown_adapters_create(d_in, d_out, rank, n_adapters, max_tokens, train=False):
+    return Adapters(d_in, d_out, rank, n_adapters, max_tokens, train)
+
+
+def countdown_adapters_destroy(pool: Adapters) -> None:
+    pool.close()
+
+
+def _rows(t, n, width, name, device):
+    """(pointer, row stride) of a [n, width] tensor whose rows are contiguous."""
+    if t.shape != (n, width):
+        raise ValueError(f"{name} must have shape {(n, width)}, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must live on GPU {device}, where the pool was created")
+    row, col = t.stride()
+    if n <= 1 or t.is_contiguous():  # (the stride of a single row says nothing)
+        row = width
+    if col != 1 and width > 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return t.data_ptr(), row
+
+
+def _whole(t, shape, dtype, name, device):
+    """Pointer of a contiguous tensor of exactly this shape and type."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must live on GPU {device}, where the pool was created")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _row_type(t, name) -> int:
+    if t.dtype is _F32:
+        return CD_TYPE_F32
+    if t.dtype is _BF16:
+        return CD_TYPE_BF16
+    raise TypeError(f"{name}: expected float32 or bfloat16, got {t.dtype}")
+
+
+def _pool_args(pool: Adapters, x, ids, A, B, scale):
+    if pool.handle is None:
+        raise ValueError("the pool is closed")
+    if x.dim() != 2 or x.dtype is not _BF16:
+        raise TypeError(f"x must be a bfloat16 [T, {pool.d_in}] tensor")
+    T, dev = x.shape[0], pool.device
+    xp, ldx = _rows(x, T, pool.d_in, "x", dev)
+    return (T, xp, ldx, _whole(ids, (T,), _torch.int32, "ids", dev),
+            _whole(A, pool._a_shape, _BF16, "A", dev), _whole(B, pool._b_shape, _BF16, "B", dev),
+            None if scale is None else _whole(scale, (pool.n_adapters,), _F32, "scale", dev))
+
+
+def countdown_adapters_project(pool: Adapters, x, W, ids, A, B, scale=None, y=None, stream=None):
+    """y = x W^T + each token's own adapter, for up to 16 tokens; returns y ``[T, d_out]``
+    (fp32, or the type of the given fp32 / bf16 ``y``). ``ids`` int32 [T]: the adapter of
+    each token (outside [0, n_adapters): none); ``scale`` fp32 [n_adapters] or None."""
+    T, xp, ldx, ip, ap, bp, sp = _pool_args(pool, x, ids, A, B, scale)
+    if y is None:
+        y = _torch.empty((T, pool.d_out), dtype=_F32, device=x.device)
+    yp, ldy = _rows(y, T, pool.d_out, "y", pool.device)
+    _check(load_library().countdown_adapters_project(
+        pool.handle, xp, ldx, T, _whole(W, (pool.d_out, pool.d_in), _BF16, "W", pool.device), ip,
+        ap, bp, sp, _row_type(y, "y"), yp, ldy, _stream(stream)), "countdown_adapters_project")
+    return y
+
+
+def _base(base, out, T, width, out_name, dtype, device):
+    """The output (made if None: of base's type, else dtype) and the pointers of base and output."""
+    if out is None:
+        out = _torch.empty((T, width), dtype=dtype if base is None else base.dtype,
+                           device=f"cuda:{device}")
+    op, ldo = _rows(out, T, width, out_name, device)
+    if base is None:
+        return out, None, 0, op, ldo
+    if base.dtype is not out.dtype:
+        raise TypeError(f"base and {out_name} must have one type, got {base.dtype} and {out.dtype}")
+    bp, ldb = (op, ldo) if base is out else _rows(base, T, width, "base", device)
+    return out, bp, ldb, op, ldo
+
+
+def countdown_adapters_add(pool: Adapters, x, ids, A, B, scale=None, base=None, y=None,
+                           stream=None):
+    """y = base + each token's own adapter of x, for any number of tokens; returns y
+    ``[T, d_out]``. ``base`` (fp32 or bf16, None: zeros) is what the shared projection gave,
+    e.g. an FFN call's y; ``y`` may be ``base`` itself (in place), has its type, and is a new
+    tensor if None."""
+    T, xp, ldx, ip, ap, bp, sp = _pool_args(pool, x, ids, A, B, scale)
+    y, basep, ldb, yp, ldy = _base(base, y, T, pool.d_out, "y", _F32, pool.device)
+    _check(load_library().countdown_adapters_add(
+        pool.handle, xp, ldx, T, ip, ap, bp, sp, _row_type(y, "y"), basep, ldb, yp, ldy,
+        _stream(stream)), "countdown_adapters_add")
+    return y
+
+
+def countdown_adapters_backward(pool: Adapters, x, dy, ids, A, B, scale=None, base=None, dx=None,
+                                dA=None, dB=None, need=(True, True, True), stream=None):
+    """The gradients ``(dx, dA, dB)`` of the adapters' part for ``dy`` (bf16 [T, d_out]).
+    dx = base + A^T (scale B^T dy) has base's type (bf16 without one); dA and dB are fp32 of
+    A's and B's shapes, overwritten whole. ``need`` says which of the three are computed
+    (None is returned for the others); given tensors are written, missing ones made."""
+    T, xp, ldx, ip, ap, bp, sp = _pool_args(pool, x, ids, A, B, scale)
+    dev = pool.device
+    if dy.dtype is not _BF16:
+        raise TypeError(f"dy: expected a bfloat16 tensor, got {dy.dtype}")
+    dyp, lddy = _rows(dy, T, pool.d_out, "dy", dev)
+    basep, ldb, dxp, lddx, dap, dbp, kind = None, 0, None, 0, None, None, CD_TYPE_BF16
+    if need[0]:
+        dx, basep, ldb, dxp, lddx = _base(base, dx, T, pool.d_in, "dx", _BF16, dev)
+        kind = _row_type(dx, "dx")
+    if need[1]:
+        if dA is None:
+            dA = _torch.empty(pool._a_shape, dtype=_F32, device=x.device)
+        dap = _whole(dA, pool._a_shape, _F32, "dA", dev)
+    if need[2]:
+        if dB is None:
+            dB = _torch.empty(pool._b_shape, dtype=_F32, device=x.device)
+        dbp = _whole(dB, pool._b_shape, _F32, "dB", dev)
+    _check(load_library().countdown_adapters_backward(
+        pool.handle, xp, ldx, dyp, lddy, T, ip, ap, bp, sp, kind, basep, ldb, dxp, lddx, dap, dbp,
+        _stream(stream)), "countdown_adapters_backward")
+    return dx if need[0] else None, dA if need[1] else None, dB if need[2] else None
+
+
+class GradClip:
+    """Owns a ``cd_clip``: the workspace of :func:`countdown_clip_grads` for up to
+    ``max_tensors`` gradients a call."""
+
+    def __init__(self, max_tensors: int):
+        self.max_tensors = max_tensors
+        h = C.c_void_p()
+        _check(load_library().countdown_clip_create(max_tensors, C.byref(h)),
+               "countdown_clip_create")
+        self.handle = h.value
+        self.device = (_torch or _use_torch()).cuda.current_device()
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(load_library().countdown_clip_destroy(self.handle), "countdown_clip_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+def countdown_clip_create(max_tensors):
+    return GradClip(max_tensors)
+
+
+def countdown_clip_destroy(clip: GradClip) -> None:
+    clip.close()
+
+
+def countdown_clip_grads(clip: GradClip, grads, max_norm: float, out=None, norm=None, stream=None):
+    """The global norm of a list of fp32 / bf16 gradients, as a new fp64 device tensor [1] (or
+    into ``norm``), and the gradients scaled by min(1, max_norm / norm): in place, or into the
+    tensors of the list ``out``. ``max_norm`` inf scales nothing (without ``out`` only the norm
+    is computed). A norm that is not finite leaves the gradients as they are."""
+    if clip.handle is None:
+        raise ValueError("the workspace is closed")
+    if out is None:
+        out = grads
+    elif len(out) != len(grads):
+        raise ValueError(f"out must have as many tensors as grads ({len(grads)}), got {len(out)}")
+    dev, words = clip.device, []
+    for g, o in zip(grads, out):
+        if g.get_device() != dev or not g.is_contiguous():
+            raise ValueError(f"gradients must be contiguous tensors on GPU {dev}")
+        p, n = g.data_ptr(), g.numel()
+        words += (p, p if o is g else _out_ptr(g, o, dev), n, _row_type(g, "gradient"))
+    if norm is None:
+        norm = _torch.empty(1, dtype=_torch.float64, device=f"cuda:{dev}")
+    table = (C.c_uint64 * len(words))(*words)  # cd_grad: three 64-bit words, the type in a fourth
+    _check(load_library().countdown_clip_grads(
+        clip.handle, table, len(grads), float(max_norm),
+        _whole(norm, (1,), _torch.float64, "norm", dev), _stream(stream)), "countdown_clip_grads")
+    return norm
+
+
+def _out_ptr(g, o, device) -> int:
+    if o.shape != g.shape or o.dtype is not g.dtype:
+        raise ValueError("an output must have its gradient's shape and type")
+    if o.get_device() != device or not o.is_contiguous():
+        raise ValueError(f"outputs must be contiguous tensors on GPU {device}")
+    return o.data_ptr()
 
 
 def countdown_check_args(variant, d_model, d_ff, max_batch, d_rank, x, B, W_gate, W_up, W_down,

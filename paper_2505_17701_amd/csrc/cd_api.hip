@@ -936,3 +936,7 @@ extern "C" cd_status countdown_ffn_mono_noalloc(const uint16_t *x, int B, const 
     return run_ffn(&p, CD_VARIANT_MONO, x, B, W_gate, W_up, W_down, nullptr, nullptr, thld, y,
                    stream);
 }
+
+// ------------------------------------------------- low-rank adapters, gradient clipping
+#include "cd_adapters.hpp"
+#include "cd_clip.hpp"

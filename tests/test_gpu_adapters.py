@@ -1,0 +1,423 @@
+"""Low-rank adapters beside a shared projection against the definition in 64 bits.
+
+Tolerances. A sum of n products accumulated in fp32 in any order is off by at most
+n * 2^-23 * sum|terms| (each addition by at most one unit in the last place). Chained
+sums add their counts: y's adapter part has d_in + rank additions over the magnitudes
+scale |B| |A| |x|, and eight more roundings (splitting the latent, the scale, base). A result
+is then rounded once to its type, by half a step of the value."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -23
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+@pytest.fixture(scope="module")
+def cd():
+    from paper_2505_17701_amd import binding
+
+    return binding
+
+
+def rand(g, *shape, sigma=1.0, dtype=torch.bfloat16):
+    return (torch.randn(shape, generator=g) * sigma).to(dtype)
+
+
+def make_ids(g, T, n, how):
+    if how == "none":
+        return torch.full((T,), -1, dtype=torch.int32)
+    if how == "one":  # every token the same adapter
+        return torch.full((T,), n - 1, dtype=torch.int32)
+    if how == "runs":  # packed requests
+        ids = torch.empty(T, dtype=torch.int32)
+        t = 0
+        while t < T:
+            m = int(torch.randint(1, max(2, T // 4 + 1), (1,), generator=g))
+            ids[t:t + m] = int(torch.randint(-1, n, (1,), generator=g))
+            t += m
+        return ids
+    ids = torch.randint(-1, n + 1, (T,), generator=g, dtype=torch.int32)  # n: out of range
+    odd = torch.tensor([-5, 2 ** 31 - 1, -2 ** 31, n], dtype=torch.int32)
+    return torch.where(ids >= n, odd[torch.randint(0, 4, (T,), generator=g)], ids)
+
+
+class Case:
+    def __init__(self, seed, T, di, do, r, n, how="mixed", scale=True):
+        g = torch.Generator().manual_seed(seed)
+        self.T, self.di, self.do, self.r, self.n = T, di, do, r, n
+        self.x, self.dy = rand(g, T, di), rand(g, T, do, sigma=0.1)
+        self.A, self.B = rand(g, n, r, di, sigma=0.05), rand(g, n, do, r, sigma=0.05)
+        self.W = rand(g, do, di, sigma=0.05)
+        self.scale = torch.rand(n, generator=g) * 3 - 1 if scale else None
+        self.ids = make_ids(g, T, n, how)
+        self.base = rand(g, T, do, dtype=torch.float32)
+        self.dbase = rand(g, T, di, dtype=torch.float32)
+
+    def s(self, a):
+        return 1.0 if self.scale is None else float(self.scale[a])
+
+    def rows(self):
+        return [(a, torch.nonzero(self.ids == a).flatten()) for a in range(self.n)]
+
+    def dev(self):
+        c = object.__new__(Case)
+        c.__dict__ = {k: v.cuda() if torch.is_tensor(v) else v for k, v in self.__dict__.items()}
+        return c
+
+    def delta(self):
+        """(delta, its magnitude) [T, d_out] in fp64."""
+        y, m = torch.zeros(self.T, self.do).double(), torch.zeros(self.T, self.do).double()
+        for a, t in self.rows():
+            A, B, x = self.A[a].double(), self.B[a].double(), self.x[t].double()
+            y[t] = self.s(a) * (x @ A.t()) @ B.t()
+            m[t] = abs(self.s(a)) * (x.abs() @ A.abs().t()) @ B.abs().t()
+        return y, m
+
+    def grads(self):
+        """{name: (value, magnitude, additions)} of dx (without base), dA, dB in fp64."""
+        dx = [torch.zeros(self.T, self.di).double() for _ in range(2)]
+        dA = [torch.zeros(self.n, self.r, self.di).double() for _ in range(2)]
+        dB = [torch.zeros(self.n, self.do, self.r).double() for _ in range(2)]
+        for a, t in self.rows():
+            for k, f in enumerate((lambda v: v.double(), lambda v: v.double().abs())):
+                s = self.s(a) if k == 0 else abs(self.s(a))
+                A, B, x, dy = f(self.A[a]), f(self.B[a]), f(self.x[t]), f(self.dy[t])
+                g = s * dy @ B
+                dx[k][t] = g @ A
+                dA[k][a] = g.t() @ x
+                dB[k][a] = s * dy.t() @ (x @ A.t())
+        return {"dx": (*dx, self.do + self.r), "dA": (*dA, self.do + self.T),
+                "dB": (*dB, self.di + self.T)}
+
+
+def check(got, ref, mag, adds, name=""):
+    """|got - ref| <= (adds + 8) u mag + half a step of got's type; NaN where ref has it."""
+    got64 = got.detach().cpu().double()
+    assert torch.equal(torch.isnan(got64), torch.isnan(ref)), name
+    fine = ~torch.isnan(ref)
+    tol = (adds + 8) * U * mag + torch.finfo(got.dtype).eps / 2 * (ref.abs() + (adds + 8) * U * mag)
+    over = ((got64 - ref).abs() - tol)[fine]
+    assert over.numel() == 0 or float(over.max()) <= 0, \
+        f"{name}: {int((over > 0).sum())} of {over.numel()} off, worst by {float(over.max()):.3e}"
+
+
+SHAPES = [  # T, d_in, d_out, rank, adapters, ids
+    (1, 256, 688, 16, 3, "one"),
+    (1, 8, 8, 8, 1, "one"),
+    (2, 1024, 520, 64, 5, "mixed"),
+    (7, 520, 1032, 24, 32, "mixed"),
+    (8, 688, 256, 256, 2, "mixed"),
+    (13, 264, 72, 40, 3, "runs"),
+    (16, 4096, 256, 8, 64, "mixed"),
+    (16, 256, 688, 16, 3, "none"),
+    (5, 2504, 1000, 32, 4, "mixed"),
+]
+LONG = [
+    (17, 256, 688, 16, 3, "mixed"),
+    (33, 72, 40, 8, 2, "mixed"),
+    (64, 520, 264, 128, 4, "runs"),
+    (65, 264, 520, 16, 1, "one"),
+    (129, 136, 1032, 72, 40, "mixed"),
+    (300, 688, 256, 48, 7, "runs"),
+    (777, 256, 264, 256, 3, "runs"),
+    (1000, 264, 136, 16, 1000, "mixed"),
+    (1500, 1032, 520, 32, 5, "runs"),
+    (200, 64, 64, 16, 4, "none"),
+]
+
+
+@pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_project(cd, shape, y_type):
+    c = Case(1, *shape)
+    ref, mag = c.delta()
+    ref = ref + c.x.double() @ c.W.double().t()
+    mag = mag + c.x.double().abs() @ c.W.double().abs().t()
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=16) as pool:
+        y = torch.empty(c.T, c.do, dtype=y_type, device="cuda")
+        out = cd.countdown_adapters_project(pool, d.x, d.W, d.ids, d.A, d.B, d.scale, y=y)
+        assert out is y
+        check(y, ref, mag, c.di + c.r, "y")
+        if y_type == torch.float32:
+            again = cd.countdown_adapters_project(pool, d.x, d.W, d.ids, d.A, d.B, d.scale)
+            assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", SHAPES + LONG)
+def test_add(cd, shape, y_type):
+    c = Case(2, *shape)
+    delta, mag = c.delta()
+    base = c.base.to(y_type)
+    ref, mag = delta + base.double(), mag + base.double().abs()
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=c.T + 3) as pool:
+        args = (pool, d.x, d.ids, d.A, d.B, d.scale)
+        y = cd.countdown_adapters_add(*args, base=base.cuda())
+        assert y.dtype == y_type
+        check(y, ref, mag, c.di + c.r, "y")
+        none = ((c.ids < 0) | (c.ids >= c.n)).cuda()
+        assert torch.equal(y[none], base.cuda()[none])  # tokens without an adapter
+        place = base.cuda()
+        assert cd.countdown_adapters_add(*args, base=place, y=place) is place
+        assert torch.equal(place, y)
+        alone = torch.full_like(place, float("nan"))
+        cd.countdown_adapters_add(*args, y=alone)
+        check(alone, delta, mag, c.di + c.r, "without base")
+        assert torch.equal(cd.countdown_adapters_add(*args, base=base.cuda()), y)
+
+
+@pytest.mark.parametrize("dx_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", SHAPES + LONG)
+def test_backward(cd, shape, dx_type):
+    c = Case(3, *shape)
+    want = c.grads()
+    base = c.dbase.to(dx_type)
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=c.T, train=True) as pool:
+        args = (pool, d.x, d.dy, d.ids, d.A, d.B, d.scale)
+        dx, dA, dB = cd.countdown_adapters_backward(*args, base=base.cuda())
+        v, m, n = want["dx"]
+        check(dx, v + base.double(), m + base.double().abs(), n, "dx")
+        check(dA, *want["dA"], "dA")
+        check(dB, *want["dB"], "dB")
+        # each gradient alone, into given memory
+        nan = lambda t: torch.full_like(t, float("nan"))  # noqa: E731
+        only = cd.countdown_adapters_backward(*args, dx=nan(dx), need=(True, False, False))
+        check(only[0], v, m, n, "dx without base")
+        assert only[1] is None and only[2] is None
+        out = nan(dA)
+        assert torch.equal(cd.countdown_adapters_backward(*args, dA=out,
+                                                          need=(False, True, False))[1], dA)
+        out = nan(dB)
+        assert torch.equal(cd.countdown_adapters_backward(*args, dB=out,
+                                                          need=(False, False, True))[2], dB)
+
+
+def test_gradients_against_differences(cd):
+    """<dy, y> is linear in each of x, A, B: its central difference over a step in one
+    element (from -4 to 4, both bf16) is the gradient, but for the rounding of y and of it."""
+    c = Case(4, 6, 40, 56, 8, 2)
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=c.T, train=True) as pool:
+        dx, dA, dB = cd.countdown_adapters_backward(pool, d.x, d.dy, d.ids, d.A, d.B, d.scale,
+                                                    dx=torch.empty(c.T, c.di, device="cuda"))
+
+        def loss():  # and how far it may be off
+            y = cd.countdown_adapters_add(pool, d.x, d.ids, d.A, d.B, d.scale)
+            h = Case.__new__(Case)
+            h.__dict__ = {k: v.cpu() if torch.is_tensor(v) else v for k, v in d.__dict__.items()}
+            mag = h.delta()[1] * h.dy.double().abs()
+            return float((y.double() * d.dy.double()).sum()), \
+                (c.di + c.r + 8) * U * float(mag.sum())
+
+        want = c.grads()
+        g = torch.Generator().manual_seed(5)
+        for name, t, grad in (("dx", d.x, dx), ("dA", d.A, dA), ("dB", d.B, dB)):
+            flat, gflat = t.view(-1), grad.view(-1)
+            _, mag, adds = want[name]
+            for i in torch.randint(0, flat.numel(), (12,), generator=g).tolist():
+                old = flat[i].clone()
+                flat[i] = 4.0
+                up, off = loss()
+                flat[i] = -4.0
+                down, off2 = loss()
+                flat[i] = old
+                tol = (off + off2) / 8 + (adds + 8) * U * float(mag.view(-1)[i])
+                assert abs((up - down) / 8 - float(gflat[i])) <= tol
+
+
+def test_strides_leave_the_rest(cd):
+    """x, base, y, dy and dx as column slices of wider tensors; y and base two slices of one."""
+    c = Case(6, 37, 264, 136, 24, 4)
+    d = c.dev()
+    wide = torch.full((c.T, 4096), 7.0, device="cuda")
+    xs = torch.full((c.T + 2, 512), 9.0, dtype=torch.bfloat16, device="cuda")
+    x = xs[1:-1, 64:64 + c.di]
+    x.copy_(d.x)
+    base, y = wide[:, 8:8 + c.do], wide[:, 256:256 + c.do]
+    base.copy_(d.base)
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=64, train=True) as pool:
+        args = (d.ids, d.A, d.B, d.scale)
+        plain = cd.countdown_adapters_add(pool, d.x, *args, base=d.base)
+        cd.countdown_adapters_add(pool, x, *args, base=base, y=y)
+        assert torch.equal(y, plain) and torch.equal(base, d.base)
+        y.fill_(7.0)
+        base.fill_(7.0)
+        assert bool((wide == 7.0).all())
+        dys = torch.full((c.T, 200), 9.0, dtype=torch.bfloat16, device="cuda")
+        dys[:, :c.do] = d.dy
+        dxs = torch.full((c.T, 272), 3.0, dtype=torch.bfloat16, device="cuda")
+        want = cd.countdown_adapters_backward(pool, d.x, d.dy, *args)
+        got = cd.countdown_adapters_backward(pool, x, dys[:, :c.do], *args, dx=dxs[:, :c.di])
+        for w, v in zip(want, got):
+            assert torch.equal(w, v)
+        assert bool((dxs[:, c.di:] == 3.0).all())
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=16) as pool:
+        ids = d.ids[:9].contiguous()
+        plain = cd.countdown_adapters_project(pool, d.x[:9], d.W, ids, d.A, d.B, d.scale)
+        got = cd.countdown_adapters_project(pool, x[:9], d.W, ids, d.A, d.B, d.scale, y=y[:9])
+        assert torch.equal(got, plain)
+        y.fill_(7.0)
+        assert bool((wide == 7.0).all())
+
+
+@pytest.mark.parametrize("T", [9, 200])
+def test_bad_numbers_stay_where_they_are(cd, T):
+    """NaN and infinity in one token, and in an adapter that no token uses, reach nothing else."""
+    c = Case(7, T, 264, 136, 16, 4)
+    c.ids = torch.arange(T, dtype=torch.int32) % 3 - 1  # -1, 0, 1; adapters 2 and 3 unused
+    c.A[3], c.B[3], c.scale[3] = float("nan"), float("inf"), float("nan")
+    c.A[2], c.B[2] = float("inf"), float("nan")
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=T, train=True) as pool:
+        args = (d.ids, d.A, d.B, d.scale)
+        good = cd.countdown_adapters_add(pool, d.x, *args, base=d.base)
+        grads = cd.countdown_adapters_backward(pool, d.x, d.dy, *args)
+        assert torch.isfinite(good).all() and all(torch.isfinite(v).all() for v in grads)
+        assert bool((grads[1][2:] == 0).all()) and bool((grads[2][2:] == 0).all())
+        x, dy = d.x.clone(), d.dy.clone()
+        x[0], dy[0] = float("nan"), float("inf")  # token 0 has no adapter
+        assert torch.equal(cd.countdown_adapters_add(pool, x, *args, base=d.base), good)
+        for v, w in zip(cd.countdown_adapters_backward(pool, x, dy, *args), grads):
+            assert torch.equal(v, w)
+        x[1] = float("nan")  # token 1: adapter 0
+        y = cd.countdown_adapters_add(pool, x, *args, base=d.base)
+        assert torch.isnan(y[1]).all() and torch.equal(y[2:], good[2:])
+        dx, dA, dB = cd.countdown_adapters_backward(pool, x, d.dy, *args)
+        assert torch.isnan(dA[0]).all() and torch.isnan(dB[0]).all()
+        assert torch.equal(dA[1:], grads[1][1:]) and torch.equal(dB[1:], grads[2][1:])
+        assert torch.equal(dx, grads[0])
+        if T <= 16:
+            p = cd.countdown_adapters_project(pool, d.x, d.W, *args)
+            q = cd.countdown_adapters_project(pool, x, d.W, *args)
+            assert torch.equal(p[2:], q[2:]) and torch.isfinite(p).all()
+            assert torch.isnan(q[:2]).all()
+
+
+def test_empty_call(cd):
+    c = Case(8, 4, 64, 72, 8, 2)
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=4, train=True) as pool:
+        x, ids, dy = d.x[:0], d.ids[:0], d.dy[:0]
+        assert cd.countdown_adapters_project(pool, x, d.W, ids, d.A, d.B).shape == (0, c.do)
+        assert cd.countdown_adapters_add(pool, x, ids, d.A, d.B).shape == (0, c.do)
+        dA, dB = torch.full_like(d.A, 5.0).float(), torch.full_like(d.B, 5.0).float()
+        dx, _, _ = cd.countdown_adapters_backward(pool, x, dy, ids, d.A, d.B, dA=dA, dB=dB)
+        assert dx.shape == (0, c.di) and not dA.any() and not dB.any()
+
+
+@pytest.mark.parametrize("T", [8, 150])
+def test_graph_replays_with_other_values(cd, T):
+    """A captured add + backward, replayed with other tokens, adapters and ids behind the same
+    pointers, eager calls of another pool between the replays."""
+    first = Case(9, T, 264, 520, 24, 5)
+    d = first.dev()
+    args = (d.ids, d.A, d.B, d.scale)
+    pool = cd.Adapters(first.di, first.do, first.r, first.n, max_tokens=T, train=True)
+    eager = cd.Adapters(first.di, first.do, first.r, first.n, max_tokens=T, train=True)
+    y = torch.empty(T, first.do, device="cuda")
+    p = torch.empty(min(T, 16), first.do, device="cuda")
+    xs, idss = d.x[:16], d.ids[:16]
+    dx, dA, dB = (torch.empty_like(t, dtype=torch.float32) for t in (d.x, d.A, d.B))
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        cd.countdown_adapters_add(pool, d.x, *args, base=d.base, y=y)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        cd.countdown_adapters_add(pool, d.x, *args, base=d.base, y=y)
+        cd.countdown_adapters_backward(pool, d.x, d.dy, *args, dx=dx, dA=dA, dB=dB)
+        cd.countdown_adapters_project(pool, xs, d.W, idss, d.A, d.B, d.scale, y=p)
+    for seed in (10, 11, 12, 13):
+        new = Case(seed, T, 264, 520, 24, 5, how=("mixed", "runs", "none", "one")[seed % 4]).dev()
+        for k in ("x", "dy", "ids", "A", "B", "scale", "base", "W"):
+            getattr(d, k).copy_(getattr(new, k))
+        want = [cd.countdown_adapters_add(eager, d.x, *args, base=d.base),
+                *cd.countdown_adapters_backward(eager, d.x, d.dy, *args, dx=torch.empty_like(dx)),
+                cd.countdown_adapters_project(eager, xs, d.W, idss, d.A, d.B, d.scale)]
+        for t in (y, dx, dA, dB, p):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for w, v in zip(want, (y, dx, dA, dB, p)):
+            assert torch.equal(w, v)
+    pool.close()
+    eager.close()
+
+
+def test_two_pools_on_two_streams(cd):
+    cases = [Case(20 + i, 150, 264, 520, 16, 3).dev() for i in range(2)]
+    pools = [cd.Adapters(264, 520, 16, 3, max_tokens=150, train=True) for _ in range(2)]
+    want = [[cd.countdown_adapters_add(p, c.x, c.ids, c.A, c.B, c.scale, base=c.base),
+             *cd.countdown_adapters_backward(p, c.x, c.dy, c.ids, c.A, c.B, c.scale)]
+            for p, c in zip(pools, cases)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                p, c = pools[k], cases[k]
+                got[k] = [cd.countdown_adapters_add(p, c.x, c.ids, c.A, c.B, c.scale, base=c.base),
+                          *cd.countdown_adapters_backward(p, c.x, c.dy, c.ids, c.A, c.B, c.scale)]
+    torch.cuda.synchronize()
+    for k in range(2):
+        for w, v in zip(want[k], got[k]):
+            assert torch.equal(w, v)
+    for p in pools:
+        p.close()
+
+
+def test_binding_refusals(cd):
+    c = Case(30, 8, 64, 72, 8, 2)
+    d = c.dev()
+    pool = cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=8)
+    ok = dict(pool=pool, x=d.x, ids=d.ids, A=d.A, B=d.B, scale=d.scale)
+
+    def add(**kw):
+        return cd.countdown_adapters_add(**{**ok, **kw})
+
+    add()
+    f32 = torch.zeros(8, c.do, device="cuda")
+    for kw, err in [
+            (dict(x=d.x.float()), TypeError), (dict(x=c.x), ValueError),
+            (dict(x=d.x[:, :56]), ValueError), (dict(x=d.x.t().contiguous().t()), ValueError),
+            (dict(ids=d.ids.long()), TypeError), (dict(ids=d.ids[:7]), ValueError),
+            (dict(A=d.A[:1]), ValueError), (dict(A=d.A.float()), TypeError),
+            (dict(B=d.B.transpose(1, 2)), ValueError), (dict(scale=d.scale[:1]), ValueError),
+            (dict(base=f32[:7]), ValueError), (dict(base=f32.half()), TypeError),
+            (dict(base=f32, y=f32.bfloat16()), TypeError), (dict(y=f32.double()), TypeError),
+            (dict(x=d.x.new_zeros(8, 68)[:, 4:]), cd.CountdownError),  # misaligned rows
+            (dict(x=torch.zeros(9, 64, dtype=torch.bfloat16, device="cuda"),
+                  ids=torch.zeros(9, dtype=torch.int32, device="cuda")), cd.CountdownError)]:
+        with pytest.raises(err):
+            add(**kw)
+    with pytest.raises(cd.CountdownError):  # not a training pool
+        cd.countdown_adapters_backward(pool, d.x, d.dy, d.ids, d.A, d.B)
+    wide = torch.zeros(8, 256, device="cuda")
+    with pytest.raises(cd.CountdownError):  # base and y overlap by some columns
+        add(base=wide[:, :72], y=wide[:, 64:136])
+    rows = torch.zeros(9, 72, device="cuda")
+    with pytest.raises(cd.CountdownError):  # and by rows
+        add(base=rows[:8], y=rows[1:])
+    pool.close()
+    with pytest.raises(ValueError):
+        add()
+    big = cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=32)
+    x17 = torch.zeros(17, c.di, dtype=torch.bfloat16, device="cuda")
+    ids17 = torch.zeros(17, dtype=torch.int32, device="cuda")
+    with pytest.raises(cd.CountdownError) as e:
+        cd.countdown_adapters_project(big, x17, d.W, ids17, d.A, d.B)
+    assert e.value.status == cd.CD_EUNSUPPORTED
+    big.close()
