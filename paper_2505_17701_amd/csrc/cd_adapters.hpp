@@ -13,7 +13,25 @@ namespace {
 constexpr int kAdMaxDim = 65536, kAdMaxRank = 256, kAdMaxAdapters = 1024;
 constexpr int kAdMaxTokens = 1 << 20;
 constexpr int kAdDecodeTokens = 16;  // tokens of countdown_adapters_project
+constexpr int kAdDirectTokens = 32;  // up to here countdown_adapters_add goes token by token
 constexpr int kAdBlock = 256, kAdWaves = kAdBlock / cdk::kWave;
+constexpr int kAdPad = 32;  // tokens of one adapter are padded to the contraction of an MFMA
+
+using cdk::f32x4_t;
+using cdk::load16;
+using cdk::mfma16;
+using cdk::or_zero;
+using cdk::u32x4;
+
+// The tokens in the order of their adapters. Adapter a's tokens sit at padded positions
+// [first, first + count), first a multiple of kAdPad; those without an adapter are group n.
+struct AdGroup {
+    int first, count;
+};
+// A tile of tokens of one group (count 0: an unused slot).
+struct AdTile {
+    int group, first, count, pad;
+};
 
 struct AdArgs {
     const uint16_t *x;  // [T][d_in], row stride ldx
@@ -31,134 +49,634 @@ struct AdArgs {
     size_t ldo;
     int type;  // of base and out
     float *dA, *dB;
-    float *lat, *glat;  // [T][rank]; both without scale_a
     int T, n, d_in, d_out, rank;
+    // workspace. lat and glat hold scale_a lat_t and glat_t, by token (decode) or position
+    float *lat, *glat;
+    int *order;       // token at each position
+    AdGroup *groups;  // [n + 1]
+    AdTile *tiles;
+    uint16_t *Bt;            // [n][rank][d_out], B transposed (training)
+    uint16_t *latT, *glatT;  // [3][rank][positions]: lat and glat split in three bf16 terms
+    int positions;
+    int tile;  // tokens of a tile: 16, 32 or 64
 };
-
-__device__ __forceinline__ float ad_load(const void *p, int type, size_t i)
-{
-    return type == CD_TYPE_F32 ? static_cast<const float *>(p)[i]
-                               : cdk::bf16_lo(static_cast<const uint16_t *>(p)[i]);
-}
-__device__ __forceinline__ void ad_store(void *p, int type, size_t i, float v)
-{
-    if (type == CD_TYPE_F32)
-        static_cast<float *>(p)[i] = v;
-    else
-        static_cast<uint16_t *>(p)[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
-}
 
 __device__ __forceinline__ bool ad_valid(const AdArgs &a, int id) { return (unsigned)id < (unsigned)a.n; }
 __device__ __forceinline__ float ad_scale(const AdArgs &a, int id) { return a.scale ? a.scale[id] : 1.0f; }
 
-// dot product of two bf16 rows of n (a multiple of 8) columns, over a wave
-__device__ __forceinline__ float ad_dot(const uint16_t *p, const uint16_t *q, int n)
+__device__ __forceinline__ uint32_t ad_pack(float lo, float hi)
 {
-    float s = 0.0f;
-    for (int i = threadIdx.x % cdk::kWave * 8; i < n; i += cdk::kColsPerLoad)
-        s = cdk::dot8(cdk::load16(p + i), cdk::load16(q + i), s);
-    return cdk::wave_sum(s);
+    return __builtin_bit_cast(uint16_t, (__bf16)lo) |
+           (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
 }
 
-// lat[t][k]: one wave per (t, k)
+// v = t[0] + t[1] + t[2], each with 8 significant bits cut from what is left: exact, so an
+// fp32 factor of a bf16 matrix product costs three products instead of any rounding
+__device__ __forceinline__ void ad_split(float v, uint32_t (&t)[3])
+{
+    t[0] = __float_as_uint(v) & 0xffff0000u;
+    float r = fabsf(v) < INFINITY ? v - __uint_as_float(t[0]) : 0.0f;  // infinity and NaN: t[0] alone
+    t[1] = __float_as_uint(r) & 0xffff0000u;
+    r -= __uint_as_float(t[1]);
+    t[2] = __float_as_uint(r) & 0xffff0000u;
+}
+
+// the terms of 8 values as MFMA operands
+__device__ __forceinline__ void ad_split8(const f32x4_t (&v)[2], u32x4 (&t)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t lo[3], hi[3];
+        ad_split(v[i / 2][i % 2 * 2], lo);
+        ad_split(v[i / 2][i % 2 * 2 + 1], hi);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            t[k][i] = lo[k] >> 16 | hi[k];
+    }
+}
+
+// Columns of an 8 x 8 block of bf16 whose rows are r[0..7]: c[j] = column j. It turns 16-byte
+// loads along one dimension into MFMA operands that contract over the other.
+__device__ __forceinline__ void ad_transpose8(const u32x4 (&r)[8], u32x4 (&c)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c[j][i] = __builtin_amdgcn_perm(r[2 * i + 1][j / 2], r[2 * i][j / 2],
+                                            j % 2 ? 0x07060302u : 0x05040100u);
+}
+
+// out = base + v for 4 consecutive columns (no: the token has no adapter, base alone)
+__device__ __forceinline__ void ad_store4(const AdArgs &a, size_t t, int col, f32x4_t v, bool no)
+{
+    if (a.type == CD_TYPE_F32) {
+        if (a.base) {
+            const f32x4_t b = *reinterpret_cast<const f32x4_t *>(
+                static_cast<const float *>(a.base) + t * a.ldb + col);
+            v = no ? b : v + b;
+        }
+        *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + t * a.ldo + col) = v;
+        return;
+    }
+    uint2 w;
+    if (a.base) {
+        const uint2 b = *reinterpret_cast<const uint2 *>(
+            static_cast<const uint16_t *>(a.base) + t * a.ldb + col);
+        w = no ? b : uint2{ad_pack(v[0] + cdk::bf16_lo(b.x), v[1] + cdk::bf16_hi(b.x)),
+                           ad_pack(v[2] + cdk::bf16_lo(b.y), v[3] + cdk::bf16_hi(b.y))};
+    } else {
+        w = uint2{ad_pack(v[0], v[1]), ad_pack(v[2], v[3])};
+    }
+    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + col) = w;
+}
+
+// ---------------------------------------------------------------- decode: token by token
+
+// lat[t][k] = scale A x: one wave per (t, k)
 __global__ __launch_bounds__(kAdBlock) void k_ad_lat(const AdArgs a)
 {
-    const size_t w = (size_t)blockIdx.x * kAdWaves + threadIdx.x / cdk::kWave;
-    const size_t t = w / a.rank;
-    if (t >= (size_t)a.T)
+    const int w = blockIdx.x * kAdWaves + threadIdx.x / cdk::kWave;
+    const int t = w / a.rank, k = w % a.rank;
+    if (t >= a.T)
         return;
-    const int k = (int)(w % a.rank), id = a.ids[t];
-    if (!ad_valid(a, id))
-        return;
-    const float v = ad_dot(a.x + t * a.ldx, a.A + ((size_t)id * a.rank + k) * a.d_in, a.d_in);
-    if (threadIdx.x % cdk::kWave == 0)
-        a.lat[w] = v;
-}
-
-// out[t][o] = base or W x_t, + scale B lat: one wave per (t, o) with W, else one lane
-template <bool PROJECT>
-__global__ __launch_bounds__(kAdBlock) void k_ad_out(const AdArgs a)
-{
-    const size_t i = (size_t)blockIdx.x * (PROJECT ? kAdWaves : kAdBlock) +
-                     threadIdx.x / (PROJECT ? cdk::kWave : 1);
-    const size_t t = i / a.d_out, o = i % a.d_out;
-    if (t >= (size_t)a.T)
-        return;
-    float v = 0.0f;
-    if constexpr (PROJECT) {
-        v = ad_dot(a.x + t * a.ldx, a.W + o * a.d_in, a.d_in);
-        if (threadIdx.x % cdk::kWave != 0)
-            return;
-    }
     const int id = a.ids[t];
-    if (ad_valid(a, id)) {
-        const uint16_t *b = a.B + ((size_t)id * a.d_out + o) * a.rank;
-        float s = 0.0f;
-        for (int k = 0; k < a.rank; ++k)
-            s += a.lat[t * a.rank + k] * cdk::bf16_lo(b[k]);
-        v += ad_scale(a, id) * s;
-    }
-    if (a.base)
-        v += ad_load(a.base, a.type, t * a.ldb + o);
-    ad_store(a.out, a.type, t * a.ldo + o, v);
-}
-
-// glat[t][k] (without the scale): one wave per (t, k)
-__global__ __launch_bounds__(kAdBlock) void k_ad_glat(const AdArgs a)
-{
-    const size_t w = (size_t)blockIdx.x * kAdWaves + threadIdx.x / cdk::kWave;
-    const size_t t = w / a.rank;
-    if (t >= (size_t)a.T)
-        return;
-    const int k = (int)(w % a.rank), id = a.ids[t];
     if (!ad_valid(a, id))
         return;
+    const uint16_t *p = a.x + t * a.ldx, *q = a.A + ((size_t)id * a.rank + k) * a.d_in;
     float s = 0.0f;
-    for (int o = threadIdx.x % cdk::kWave; o < a.d_out; o += cdk::kWave)
-        s += cdk::bf16_lo(a.dy[t * a.lddy + o]) *
-             cdk::bf16_lo(a.B[((size_t)id * a.d_out + o) * a.rank + k]);
+#pragma unroll 4
+    for (int i = threadIdx.x % cdk::kWave * 8; i < a.d_in; i += cdk::kColsPerLoad)
+        s = cdk::dot8(load16(p + i), load16(q + i), s);
     s = cdk::wave_sum(s);
     if (threadIdx.x % cdk::kWave == 0)
-        a.glat[w] = s;
+        a.lat[w] = s * ad_scale(a, id);
 }
 
-// dx[t][i]: one lane each
+// sum over the rank of lat[k] B[a][o][k]
+__device__ __forceinline__ float ad_row(const AdArgs &a, int id, int o, const float *lat)
+{
+    const uint16_t *b = a.B + ((size_t)id * a.d_out + o) * a.rank;
+    float s = 0.0f;
+    for (int k = 0; k < a.rank; k += 8) {
+        const u32x4 v = load16(b + k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            s += lat[k + 2 * i] * cdk::bf16_lo(v[i]) + lat[k + 2 * i + 1] * cdk::bf16_hi(v[i]);
+    }
+    return s;
+}
+
+// y = base + B lat: one lane per output, blockIdx.y the token
+__global__ __launch_bounds__(kAdBlock) void k_ad_up(const AdArgs a)
+{
+    const int t = blockIdx.y, o = blockIdx.x * kAdBlock + threadIdx.x, id = a.ids[t];
+    if (o >= a.d_out)
+        return;
+    const bool no = !ad_valid(a, id);
+    float v = no ? 0.0f : ad_row(a, id, o, a.lat + t * a.rank);
+    if (a.type == CD_TYPE_F32) {
+        const float *b = static_cast<const float *>(a.base);
+        if (b)
+            v = no ? b[t * a.ldb + o] : v + b[t * a.ldb + o];
+        static_cast<float *>(a.out)[t * a.ldo + o] = v;
+    } else {
+        const uint16_t *b = static_cast<const uint16_t *>(a.base);
+        uint16_t w = __builtin_bit_cast(uint16_t, (__bf16)(b ? v + cdk::bf16_lo(b[t * a.ldb + o]) : v));
+        static_cast<uint16_t *>(a.out)[t * a.ldo + o] = no && b ? b[t * a.ldb + o] : w;
+    }
+}
+
+// y = W x + B lat for up to 16 tokens: a workgroup's eight waves each take an eighth of the
+// columns of 16 rows of W (all of their loads in flight at once), the tokens are the other
+// operand; the waves' sums meet in LDS, where the adapters' part is added.
+constexpr int kAdProjBlock = 512, kAdProjWaves = kAdProjBlock / cdk::kWave;
+
+__global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
+{
+    __shared__ f32x4_t sums[kAdProjWaves][cdk::kWave];
+    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int m = lane % 16, g = lane / 16;
+    const int o0 = blockIdx.x * 16;
+    const bool row_ok = o0 + m < a.d_out, tok_ok = m < a.T;
+    const uint16_t *w = a.W + (size_t)(o0 + m) * a.d_in, *x = a.x + m * a.ldx;
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int kb = wave * 128; kb < a.d_in; kb += 128 * kAdProjWaves) {
+        u32x4 wv[4], xv[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = kb + 32 * u + 8 * g;
+            wv[u] = load16(or_zero(row_ok && k < a.d_in, w + k));
+            xv[u] = load16(or_zero(tok_ok && k < a.d_in, x + k));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            acc = mfma16(wv[u], xv[u], acc);
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (threadIdx.x >= 256)
+        return;
+    const int t = threadIdx.x / 16, r = threadIdx.x % 16, o = o0 + r;  // one output each
+    if (t >= a.T || o >= a.d_out)
+        return;
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kAdProjWaves; ++i)
+        v += sums[i][r / 4 * 16 + t][r % 4];
+    const int id = a.ids[t];
+    if (ad_valid(a, id))
+        v += ad_row(a, id, o, a.lat + t * a.rank);
+    if (a.type == CD_TYPE_F32)
+        static_cast<float *>(a.out)[t * a.ldo + o] = v;
+    else
+        static_cast<uint16_t *>(a.out)[t * a.ldo + o] = __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+// ------------------------------------------------- many tokens: grouped by their adapters
+
+constexpr int kAdSortBlock = 1024;
+
+// sums over the workgroup of two counts, the second also as the exclusive prefix before
+// this thread
+__device__ __forceinline__ void ad_scan(int &less, int &mine, int &before)
+{
+    __shared__ int wl[kAdSortBlock / cdk::kWave], wm[kAdSortBlock / cdk::kWave];
+    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    int inc = mine;
+#pragma unroll
+    for (int d = 1; d < cdk::kWave; d *= 2) {
+        less += __shfl_xor(less, d);
+        const int up = __shfl_up(inc, d);
+        inc += lane >= d ? up : 0;
+    }
+    if (lane == cdk::kWave - 1) {
+        wl[wave] = less;
+        wm[wave] = inc;
+    }
+    __syncthreads();
+    before = inc - mine;
+    less = mine = 0;
+    for (int i = 0; i < kAdSortBlock / cdk::kWave; ++i) {
+        less += wl[i];
+        before += i < wave ? wm[i] : 0;
+        mine += wm[i];
+    }
+}
+
+// Workgroup g <= n finds the tokens of group g, in their order, by reading all ids: no
+// atomics, no order that depends on timing. Every group's places follow from the number b
+// of tokens in lower groups alone: with first = roundup(b) + pad g the next group's first
+// is at least first + roundup(count), and with slot b / tile + g its tiles fit as well.
+// Workgroups past n transpose B for the backward call.
+__global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
+{
+    if ((int)blockIdx.x > a.n) {
+        // 64 outputs x 64 ranks
+        __shared__ uint16_t tile[64][66];
+        const int ct = (a.d_out + 63) / 64, rt = (a.rank + 63) / 64;
+        const int i = blockIdx.x - a.n - 1;
+        const int c0 = i % ct * 64, r0 = i / ct % rt * 64, ad = i / ct / rt;
+        const uint16_t *src = a.B + (size_t)ad * a.d_out * a.rank;
+        uint16_t *dst = a.Bt + (size_t)ad * a.d_out * a.rank;
+        for (int e = threadIdx.x; e < 64 * 64; e += kAdSortBlock) {
+            const int o = c0 + e / 64, k = r0 + e % 64;
+            tile[e / 64][e % 64] = o < a.d_out && k < a.rank ? src[(size_t)o * a.rank + k] : 0;
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < 64 * 64; e += kAdSortBlock) {
+            const int o = c0 + e % 64, k = r0 + e / 64;
+            if (o < a.d_out && k < a.rank)
+                dst[(size_t)k * a.d_out + o] = tile[e % 64][e / 64];
+        }
+        return;
+    }
+    const int grp = blockIdx.x;
+    const int per = (a.T + kAdSortBlock - 1) / kAdSortBlock;
+    const int t0 = min(a.T, (int)threadIdx.x * per), t1 = min(a.T, t0 + per);
+    int less = 0, mine = 0, before;
+    for (int t = t0; t < t1; ++t) {
+        const int id = a.ids[t], of = ad_valid(a, id) ? id : a.n;
+        less += of < grp;
+        mine += of == grp;
+    }
+    ad_scan(less, mine, before);  // mine: the group's count
+    const int first = (less + kAdPad - 1) / kAdPad * kAdPad + kAdPad * grp;
+    int at = first + before;
+    for (int t = t0; t < t1; ++t) {
+        const int id = a.ids[t], of = ad_valid(a, id) ? id : a.n;
+        if (of == grp)
+            a.order[at++] = t;
+    }
+    if (threadIdx.x == 0)
+        a.groups[grp] = AdGroup{first, mine};
+    const int slot0 = less / a.tile + grp, slot1 = (less + mine) / a.tile + grp + 1;
+    for (int s = slot0 + threadIdx.x; s < slot1; s += kAdSortBlock) {
+        const int off = (s - slot0) * a.tile;
+        a.tiles[s] = AdTile{grp, first + off, max(0, min(a.tile, mine - off)), 0};
+    }
+}
+
+// The low-rank latents of a tile of MT * 16 tokens and RT * 16 ranks (blockIdx.y the ranks;
+// blockIdx.z: with both, 1 is glat). Eight waves split the contraction in blocks of 128
+// columns, and their sums meet in LDS. The scale is applied here.
+constexpr int kAdShrinkBlock = 512, kAdShrinkWaves = kAdShrinkBlock / cdk::kWave;
+
+template <int MT, int RT>
+__global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, int first_kind)
+{
+    static_assert(MT * RT * cdk::kWave <= kAdShrinkBlock, "one sum per thread");
+    __shared__ f32x4_t sums[kAdShrinkWaves][MT * RT * cdk::kWave];
+    const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
+    const AdTile tile = a.tiles[blockIdx.x / sub];
+    const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
+    if (count <= 0 || tile.group == a.n)
+        return;
+    const bool back = blockIdx.z + first_kind;  // glat
+    const int K = back ? a.d_out : a.d_in;
+    const uint16_t *src = back ? a.dy : a.x;
+    const size_t ld = back ? a.lddy : a.ldx;
+    const uint16_t *fac = (back ? a.Bt : a.A) + (size_t)tile.group * a.rank * K;
+    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int m = lane % 16, g = lane / 16;
+    const int r0 = blockIdx.y * RT * 16;
+    const uint16_t *xp[MT], *fp[RT];
+    bool xok[MT], fok[RT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        xok[i] = i * 16 + m < count;
+        xp[i] = src + (xok[i] ? (size_t)a.order[tile.first + off + i * 16 + m] * ld : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        fok[i] = r0 + i * 16 + m < a.rank;
+        fp[i] = fac + (fok[i] ? (size_t)(r0 + i * 16 + m) * K : 0);
+    }
+    f32x4_t acc[MT][RT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j)
+            acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int kb = wave * 128; kb < K; kb += 128 * kAdShrinkWaves) {
+        u32x4 xv[4][MT], fv[4][RT];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = kb + 32 * u + 8 * g;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                xv[u][i] = load16(or_zero(xok[i] && k < K, xp[i] + k));
+#pragma unroll
+            for (int j = 0; j < RT; ++j)
+                fv[u][j] = load16(or_zero(fok[j] && k < K, fp[j] + k));
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < RT; ++j)
+                    acc[i][j] = mfma16(fv[u][j], xv[u][i], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j)
+            sums[wave][(i * RT + j) * cdk::kWave + lane] = acc[i][j];
+    __syncthreads();
+    if (threadIdx.x >= MT * RT * cdk::kWave)
+        return;
+    f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kAdShrinkWaves; ++w)
+        v += sums[w][threadIdx.x];
+    v *= ad_scale(a, tile.group);
+    // this thread: token i * 16 + m, ranks r .. r + 3
+    const int at = threadIdx.x / cdk::kWave / RT * 16 + m;
+    const int r = r0 + threadIdx.x / cdk::kWave % RT * 16 + g * 4;
+    if (at >= count || r >= a.rank)
+        return;
+    const size_t p = tile.first + off + at;
+    *reinterpret_cast<f32x4_t *>((back ? a.glat : a.lat) + p * a.rank + r) = v;
+    uint16_t *tr = back ? a.glatT : a.latT;
+    if (!tr)
+        return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        uint32_t s[3];
+        ad_split(v[q], s);
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            tr[((size_t)k * a.rank + r + q) * a.positions + p] = (uint16_t)(s[k] >> 16);
+    }
+}
+
+// lat's terms as MFMA operands for a tile's token (m) and K-chunk c
+__device__ __forceinline__ void ad_operand(const AdArgs &a, const float *lat, bool ok, size_t p,
+                                           int r, u32x4 (&t)[3])
+{
+    const float *q = or_zero(ok && r < a.rank, lat + p * a.rank + r);
+    const f32x4_t v[2] = {*reinterpret_cast<const f32x4_t *>(q),
+                          *reinterpret_cast<const f32x4_t *>(ok && r < a.rank ? q + 4 : q)};
+    ad_split8(v, t);
+}
+
+// y = base + B lat for a tile of MT * 16 tokens, KC * 32 ranks. Each wave takes steps of 64
+// outputs: four MFMAs whose rows are permuted (row 16 (m / 4) + 4 j + m % 4) so that a lane ends with 16
+// consecutive outputs of its token.
+template <int MT, int KC>
+__global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
+{
+    const int sub = a.tile / (MT * 16);
+    const AdTile tile = a.tiles[blockIdx.x / sub];
+    const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
+    const bool no = tile.group == a.n;
+    if (count <= 0 || (no && a.base == a.out))
+        return;
+    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int m = lane % 16, g = lane / 16;
+    size_t tok[MT];
+    u32x4 lt[MT][KC][3];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const bool ok = i * 16 + m < count;
+        const size_t p = tile.first + off + i * 16 + m;
+        tok[i] = ok ? a.order[p] : 0;
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+            ad_operand(a, a.lat, ok && !no, p, c * 32 + g * 8, lt[i][c]);
+    }
+    const uint16_t *B = a.B + (no ? 0 : (size_t)tile.group * a.d_out * a.rank);
+#pragma unroll 1
+    for (int o0 = (blockIdx.y * kAdWaves + wave) * 64; o0 < a.d_out; o0 += gridDim.y * kAdWaves * 64) {
+        f32x4_t acc[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!no) {
+            u32x4 b[4][KC];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int o = o0 + 16 * (m / 4) + 4 * j + m % 4;
+#pragma unroll
+                for (int c = 0; c < KC; ++c) {
+                    const int k = c * 32 + g * 8;
+                    b[j][c] = load16(or_zero(o < a.d_out && k < a.rank, B + (size_t)o * a.rank + k));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int c = 0; c < KC; ++c)
+#pragma unroll
+                    for (int s = 2; s >= 0; --s)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+                            acc[i][j] = mfma16(b[j][c], lt[i][c][s], acc[i][j]);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            if (i * 16 + m < count)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int o = o0 + 16 * g + 4 * j;
+                    if (o < a.d_out)
+                        ad_store4(a, tok[i], o, acc[i][j], no);
+                }
+    }
+}
+
+// dx = base + A^T glat: as k_ad_expand, but the factor's rows run along the outputs, so a
+// lane loads 8 ranks x 8 columns and transposes them: steps of 128 columns, eight MFMAs, 32
+// consecutive columns of a token per lane.
+template <int MT, int KC>
 __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
 {
-    const size_t w = (size_t)blockIdx.x * kAdBlock + threadIdx.x;
-    const size_t t = w / a.d_in, i = w % a.d_in;
-    if (t >= (size_t)a.T)
+    const int sub = a.tile / (MT * 16);
+    const AdTile tile = a.tiles[blockIdx.x / sub];
+    const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
+    const bool no = tile.group == a.n;
+    if (count <= 0 || (no && a.base == a.out))
         return;
-    const int id = a.ids[t];
-    float v = 0.0f;
-    if (ad_valid(a, id)) {
-        for (int k = 0; k < a.rank; ++k)
-            v += a.glat[t * a.rank + k] * cdk::bf16_lo(a.A[((size_t)id * a.rank + k) * a.d_in + i]);
-        v *= ad_scale(a, id);
+    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int m = lane % 16, g = lane / 16;
+    size_t tok[MT];
+    u32x4 lt[MT][KC][3];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const bool ok = i * 16 + m < count;
+        const size_t p = tile.first + off + i * 16 + m;
+        tok[i] = ok ? a.order[p] : 0;
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+            ad_operand(a, a.glat, ok && !no, p, c * 32 + g * 8, lt[i][c]);
     }
-    if (a.base)
-        v += ad_load(a.base, a.type, t * a.ldb + i);
-    ad_store(a.out, a.type, t * a.ldo + i, v);
+    const uint16_t *A = a.A + (no ? 0 : (size_t)tile.group * a.d_in * a.rank);
+#pragma unroll 1
+    for (int c0 = (blockIdx.y * kAdWaves + wave) * 128; c0 < a.d_in; c0 += gridDim.y * kAdWaves * 128) {
+        f32x4_t acc[MT][8];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!no) {
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                u32x4 rows[8], cols[8];
+                const bool ok = c * 32 + g * 8 < a.rank && c0 + m * 8 < a.d_in;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    rows[e] = load16(or_zero(ok, A + (size_t)(c * 32 + g * 8 + e) * a.d_in + c0 + m * 8));
+                ad_transpose8(rows, cols);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int s = 2; s >= 0; --s)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+                            acc[i][j] = mfma16(cols[j], lt[i][c][s], acc[i][j]);
+            }
+        }
+        // acc[i][j][q]: column c0 + 8 (4 g + q) + j
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            if (i * 16 + m < count)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = c0 + 8 * (4 * g + q);
+                    if (col < a.d_in) {
+                        ad_store4(a, tok[i], col, f32x4_t{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]}, no);
+                        ad_store4(a, tok[i], col + 4, f32x4_t{acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]}, no);
+                    }
+                }
+    }
 }
 
-// dA (DB false) and dB: one lane per element, over the tokens
-template <bool DB>
-__global__ __launch_bounds__(kAdBlock) void k_ad_grad(const AdArgs a)
+// dA = glat^T x and dB = dy^T lat of one adapter: 128 columns of x or dy and RT * 16 ranks.
+// The contraction runs over the adapter's tokens, 32 at a time: a lane loads 8 tokens x 8
+// columns and transposes them. `split` of the workgroup's four waves share a column tile and
+// take every split-th chunk of tokens; their sums meet in LDS.
+template <int RT, bool DB>
+__device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int split, f32x4_t (&lds)[2][cdk::kWave * 8])
 {
-    const size_t w = (size_t)blockIdx.x * kAdBlock + threadIdx.x;
-    const size_t d = DB ? a.d_out : a.d_in, id = w / (d * a.rank), at = w % (d * a.rank);
-    if (id >= (size_t)a.n)
-        return;
-    const size_t k = DB ? at % a.rank : at / d, i = DB ? at / a.rank : at % d;
-    float v = 0.0f;
-    bool used = false;  // (an adapter without tokens has a zero gradient whatever its scale)
-    for (int t = 0; t < a.T; ++t)
-        if (a.ids[t] == (int)id) {
-            used = true;
-            v += DB ? a.lat[(size_t)t * a.rank + k] * cdk::bf16_lo(a.dy[t * a.lddy + i])
-                    : a.glat[(size_t)t * a.rank + k] * cdk::bf16_lo(a.x[t * a.ldx + i]);
+    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int m = lane % 16, g = lane / 16;
+    const int width = DB ? a.d_out : a.d_in, per = kAdWaves / split;  // column tiles of a workgroup
+    const int tiles = (width + 128 * per - 1) / (128 * per), rgs = (a.rank + RT * 16 - 1) / (RT * 16);
+    const int ad = block / (tiles * rgs), r0 = block / tiles % rgs * RT * 16;
+    const int c0 = (block % tiles * per + wave / split) * 128;
+    const AdGroup grp = a.groups[ad];
+    const uint16_t *src = DB ? a.dy : a.x;
+    const size_t ld = DB ? a.lddy : a.ldx;
+    const uint16_t *fac = DB ? a.latT : a.glatT;
+    const size_t term = (size_t)a.rank * a.positions;
+    const bool cok = c0 + m * 8 < width;
+    f32x4_t acc[RT][8];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int p = wave % split * 32; p < grp.count; p += split * 32) {
+        const int left = grp.count - p - g * 8;  // tokens from this lane's first
+        const int *ord = a.order + grp.first + p + g * 8;
+        u32x4 rows[8], cols[8], f[RT][3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool ok = e < left && cok;
+            rows[e] = load16(or_zero(ok, src + (ok ? (size_t)ord[e] * ld : 0) + c0 + m * 8));
         }
-    (DB ? a.dB : a.dA)[w] = used ? v * ad_scale(a, (int)id) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int s = 0; s < 3; ++s) {
+                const int r = r0 + i * 16 + m;
+                f[i][s] = load16(or_zero(r < a.rank && left > 0,
+                                         fac + s * term + (size_t)r * a.positions + grp.first + p + g * 8));
+            }
+        if (grp.count - p < 32) {  // what lies past the group's end is not a number of this call
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int s = 0; s < 3; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        f[i][s][e] &= (2 * e < left ? 0xffffu : 0u) | (2 * e + 1 < left ? 0xffff0000u : 0u);
+        }
+        ad_transpose8(rows, cols);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int s = 2; s >= 0; --s)
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+                    acc[i][j] = DB ? mfma16(f[i][s], cols[j], acc[i][j]) : mfma16(cols[j], f[i][s], acc[i][j]);
+    }
+    // waves of one column tile: the upper half of them hands its sums to the lower, by halves
+    for (int half = split / 2; half >= 1; half /= 2)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int w = wave % split, to = wave / split * half + w % half;
+            __syncthreads();
+            if (w >= half && w < 2 * half)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    lds[to][j * cdk::kWave + lane] = acc[i][j];
+            __syncthreads();
+            if (w < half)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    acc[i][j] += lds[to][j * cdk::kWave + lane];
+        }
+    if (wave % split)
+        return;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        if constexpr (DB) {  // row o = c0 + 8 m + j, ranks 4 g + q
+            const int r = r0 + i * 16 + g * 4;
+            if (cok && r < a.rank)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<f32x4_t *>(
+                        a.dB + ((size_t)ad * a.d_out + c0 + m * 8 + j) * a.rank + r) = acc[i][j];
+        } else {  // row r = m, columns c0 + 8 (4 g + q) + j
+            const int r = r0 + i * 16 + m;
+            if (r < a.rank)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int col = c0 + 8 * (4 * g + q);
+                    if (col < a.d_in) {
+                        f32x4_t *d = reinterpret_cast<f32x4_t *>(
+                            a.dA + ((size_t)ad * a.rank + r) * a.d_in + col);
+                        d[0] = f32x4_t{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
+                        d[1] = f32x4_t{acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
+                    }
+                }
+        }
+    }
+}
+
+// workgroups [0, nA) compute dA, the others dB
+template <int RT>
+__global__ __launch_bounds__(kAdBlock) void k_ad_outer(const AdArgs a, int nA, int split)
+{
+    __shared__ f32x4_t lds[2][cdk::kWave * 8];
+    if ((int)blockIdx.x < nA)
+        ad_outer<RT, false>(a, blockIdx.x, split, lds);
+    else
+        ad_outer<RT, true>(a, blockIdx.x - nA, split, lds);
+}
+
+__global__ __launch_bounds__(kAdBlock) void k_ad_zero(float *p, size_t n)
+{
+    for (size_t i = (size_t)blockIdx.x * kAdBlock + threadIdx.x; i < n; i += (size_t)gridDim.x * kAdBlock)
+        p[i] = 0.0f;
 }
 
 // rows of `row` bytes at a stride of ld bytes
@@ -190,17 +708,25 @@ bool ad_ld_ok(size_t ld, int width) { return ld >= (size_t)width && ld % 8 == 0 
 
 size_t ad_size(int type) { return type == CD_TYPE_F32 ? sizeof(float) : sizeof(uint16_t); }
 
-unsigned ad_blocks(size_t items, size_t per) { return (unsigned)((items + per - 1) / per); }
-
 }  // namespace
 
 struct cd_adapters {
     int d_in, d_out, rank, n, max_tokens, device;
     unsigned flags;
+    void *ws;  // everything below lies in it
     float *lat, *glat;
+    int *order;
+    AdGroup *groups;
+    AdTile *tiles;
+    uint16_t *Bt, *latT, *glatT;
+    int positions;
 };
 
 namespace {
+
+// Tokens of a tile. Small tiles spread a short batch over the CUs; large ones read the factors
+// less often.
+int ad_tile(int T) { return T < 8192 ? 16 : T < 16384 ? 32 : 64; }
 
 // the arguments that every call has; out_dim: the columns of base and out (0: neither)
 cd_status ad_check(const cd_adapters *p, const AdArgs &a, int out_dim)
@@ -261,14 +787,100 @@ AdArgs ad_args(const cd_adapters *p, const uint16_t *x, size_t ldx, int T, const
     a.type = type;
     a.T = T;
     if (p) {
-        a.lat = p->lat;
-        a.glat = p->glat;
         a.n = p->n;
         a.d_in = p->d_in;
         a.d_out = p->d_out;
         a.rank = p->rank;
+        a.lat = p->lat;
+        a.order = p->order;
+        a.groups = p->groups;
+        a.tiles = p->tiles;
+        a.positions = p->positions;
+        a.tile = ad_tile(T);
     }
     return a;
+}
+
+int ad_ceil(int v, int d) { return (v + d - 1) / d; }
+
+// tiles of the grouped tokens (k_ad_group)
+int ad_slots(const AdArgs &a) { return a.T / a.tile + a.n + 1; }
+
+void ad_group(const AdArgs &a, bool transpose, hipStream_t s)
+{
+    const int more = transpose ? a.n * ad_ceil(a.d_out, 64) * ad_ceil(a.rank, 64) : 0;
+    k_ad_group<<<a.n + 1 + more, kAdSortBlock, 0, s>>>(a);
+}
+
+// kinds: 1 lat, 2 glat, 3 both
+void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
+{
+    const int mt = a.tile / 16, slots = ad_slots(a);
+    const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
+    const int m = std::min(mt, rt == 4 ? 2 : 4);  // sums of a workgroup: one per thread
+    const dim3 grid(slots * (mt / m), ad_ceil(a.rank, rt * 16), kinds == 3 ? 2 : 1);
+    const int first = kinds == 2;
+#define AD_SHRINK(M, R) \
+    if (m == M && rt == R) \
+        k_ad_shrink<M, R><<<grid, kAdShrinkBlock, 0, s>>>(a, first)
+    AD_SHRINK(1, 1);
+    AD_SHRINK(2, 1);
+    AD_SHRINK(4, 1);
+    AD_SHRINK(1, 2);
+    AD_SHRINK(2, 2);
+    AD_SHRINK(4, 2);
+    AD_SHRINK(1, 4);
+    AD_SHRINK(2, 4);
+#undef AD_SHRINK
+}
+
+// Workgroups along the outputs, `step` columns a wave, so that the grid has about 2048 of them.
+unsigned ad_columns(int width, int step, int tiles)
+{
+    const int most = ad_ceil(width, step * kAdWaves);
+    return (unsigned)std::max(1, std::min(most, ad_ceil(2048, tiles)));
+}
+
+// y (back: dx) from the latents
+void ad_expand(const AdArgs &a, bool back, hipStream_t s)
+{
+    const int mt = a.tile / 16, slots = ad_slots(a);
+    const int kc = a.rank <= 32 ? 1 : a.rank <= 64 ? 2 : a.rank <= 128 ? 4 : 8;
+    const int m = std::min(mt, kc <= 2 ? 2 : 1);
+    const int tiles = slots * (mt / m);
+    const dim3 grid(tiles, back ? ad_columns(a.d_in, 128, tiles) : ad_columns(a.d_out, 64, tiles));
+#define AD_EXPAND(M, K) \
+    if (m == M && kc == K) { \
+        if (back) \
+            k_ad_dx<M, K><<<grid, kAdBlock, 0, s>>>(a); \
+        else \
+            k_ad_expand<M, K><<<grid, kAdBlock, 0, s>>>(a); \
+    }
+    AD_EXPAND(1, 1)
+    AD_EXPAND(2, 1)
+    AD_EXPAND(1, 2)
+    AD_EXPAND(2, 2)
+    AD_EXPAND(1, 4)
+    AD_EXPAND(1, 8)
+#undef AD_EXPAND
+}
+
+// dA and dB: with few column tiles the waves of a workgroup share one
+void ad_grads(const AdArgs &a, hipStream_t s)
+{
+    const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
+    const int rgs = ad_ceil(a.rank, rt * 16);
+    const int waves = a.n * rgs * ((a.dA ? ad_ceil(a.d_in, 128) : 0) + (a.dB ? ad_ceil(a.d_out, 128) : 0));
+    const int split = waves >= 1024 ? 1 : waves >= 512 ? 2 : 4;
+    const int cols = 128 * kAdWaves / split;
+    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, cols) : 0;
+    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, cols) : 0;
+    if (rt == 1)
+        k_ad_outer<1><<<nA + nB, kAdBlock, 0, s>>>(a, nA, split);
+    else if (rt == 2)
+        k_ad_outer<2><<<nA + nB, kAdBlock, 0, s>>>(a, nA, split);
+    else
+        k_ad_outer<4><<<nA + nB, kAdBlock, 0, s>>>(a, nA, split);
 }
 
 }  // namespace
@@ -297,14 +909,33 @@ cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapter
     p->max_tokens = max_tokens;
     p->flags = flags;
     p->device = dev;
-    const size_t lat = (size_t)max_tokens * rank * sizeof(float);
-    void *ws = nullptr;
-    if (hip_status(hipMalloc(&ws, flags & CD_ADAPTERS_TRAIN ? 2 * lat : lat)) != CD_OK) {
+    p->positions = (max_tokens + kAdPad - 1) / kAdPad * kAdPad + kAdPad * (n_adapters + 1);
+    const bool train = flags & CD_ADAPTERS_TRAIN;
+    const size_t pos = p->positions, lat = pos * rank * sizeof(float);
+    const size_t terms = 3 * pos * rank * sizeof(uint16_t);
+    const size_t tiles = ((size_t)max_tokens / 16 + n_adapters + 1) * sizeof(AdTile);
+    const size_t groups = (n_adapters + 1) * sizeof(AdGroup);
+    const size_t copy = (size_t)n_adapters * rank * d_out * sizeof(uint16_t);
+    const size_t parts[] = {lat,   pos * sizeof(int),  tiles,             groups,
+                            train ? lat : 0, train ? terms : 0, train ? terms : 0, train ? copy : 0};
+    size_t at[9] = {0};
+    for (int i = 0; i < 8; ++i)
+        at[i + 1] = at[i] + (parts[i] + 255) / 256 * 256;
+    if (hip_status(hipMalloc(&p->ws, at[8])) != CD_OK) {
         delete p;
         return CD_ENOMEM;
     }
-    p->lat = static_cast<float *>(ws);
-    p->glat = flags & CD_ADAPTERS_TRAIN ? p->lat + lat / sizeof(float) : nullptr;
+    char *ws = static_cast<char *>(p->ws);
+    p->lat = reinterpret_cast<float *>(ws + at[0]);
+    p->order = reinterpret_cast<int *>(ws + at[1]);
+    p->tiles = reinterpret_cast<AdTile *>(ws + at[2]);
+    p->groups = reinterpret_cast<AdGroup *>(ws + at[3]);
+    if (train) {
+        p->glat = reinterpret_cast<float *>(ws + at[4]);
+        p->latT = reinterpret_cast<uint16_t *>(ws + at[5]);
+        p->glatT = reinterpret_cast<uint16_t *>(ws + at[6]);
+        p->Bt = reinterpret_cast<uint16_t *>(ws + at[7]);
+    }
     *out = p;
     return CD_OK;
 }
@@ -319,7 +950,7 @@ cd_status countdown_adapters_destroy(cd_adapters *p)
         st = hip_status(hipSetDevice(p->device));
     if (st == CD_OK)
         st = hip_status(hipDeviceSynchronize());
-    if (hip_status(hipFree(p->lat)) != CD_OK)
+    if (hip_status(hipFree(p->ws)) != CD_OK)
         st = CD_EHIP;
     if (dev >= 0)
         (void)hip_status(hipSetDevice(dev));
@@ -346,8 +977,8 @@ cd_status countdown_adapters_project(cd_adapters *p, const uint16_t *x, size_t l
     if (T == 0)
         return CD_OK;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    k_ad_lat<<<ad_blocks((size_t)T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-    k_ad_out<true><<<ad_blocks((size_t)T * a.d_out, kAdWaves), kAdBlock, 0, s>>>(a);
+    k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
+    k_ad_project<<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a);
     return launched(hipGetLastError());
 }
 
@@ -365,8 +996,14 @@ cd_status countdown_adapters_add(cd_adapters *p, const uint16_t *x, size_t ldx, 
     if (st != CD_OK || T == 0)
         return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    k_ad_lat<<<ad_blocks((size_t)T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-    k_ad_out<false><<<ad_blocks((size_t)T * a.d_out, kAdBlock), kAdBlock, 0, s>>>(a);
+    if (T <= kAdDirectTokens) {
+        k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
+        k_ad_up<<<dim3(ad_ceil(a.d_out, kAdBlock), T), kAdBlock, 0, s>>>(a);
+    } else {
+        ad_group(a, false, s);
+        ad_shrink(a, 1, s);
+        ad_expand(a, false, s);
+    }
     return launched(hipGetLastError());
 }
 
@@ -392,16 +1029,26 @@ cd_status countdown_adapters_backward(cd_adapters *p, const uint16_t *x, size_t 
     if (st != CD_OK)
         return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (dB && T > 0)
-        k_ad_lat<<<ad_blocks((size_t)T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-    if ((dx || dA) && T > 0)
-        k_ad_glat<<<ad_blocks((size_t)T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-    if (dx && T > 0)
-        k_ad_dx<<<ad_blocks((size_t)T * a.d_in, kAdBlock), kAdBlock, 0, s>>>(a);
-    if (dA)
-        k_ad_grad<false><<<ad_blocks((size_t)a.n * a.rank * a.d_in, kAdBlock), kAdBlock, 0, s>>>(a);
-    if (dB)
-        k_ad_grad<true><<<ad_blocks((size_t)a.n * a.rank * a.d_out, kAdBlock), kAdBlock, 0, s>>>(a);
+    if (T == 0) {
+        if (dA)
+            k_ad_zero<<<1024, kAdBlock, 0, s>>>(dA, (size_t)a.n * a.rank * a.d_in);
+        if (dB)
+            k_ad_zero<<<1024, kAdBlock, 0, s>>>(dB, (size_t)a.n * a.rank * a.d_out);
+        return launched(hipGetLastError());
+    }
+    const bool back = dx || dA;
+    if (!back && !dB)
+        return CD_OK;
+    a.glat = p->glat;
+    a.Bt = p->Bt;
+    a.latT = p->latT;
+    a.glatT = dA ? p->glatT : nullptr;
+    ad_group(a, back, s);
+    ad_shrink(a, (dB ? 1 : 0) + (back ? 2 : 0), s);
+    if (dx)
+        ad_expand(a, true, s);
+    if (dA || dB)
+        ad_grads(a, s);
     return launched(hipGetLastError());
 }
 
