@@ -107,28 +107,37 @@ __device__ __forceinline__ void ad_transpose8(const u32x4 (&r)[8], u32x4 (&c)[8]
                                             j % 2 ? 0x07060302u : 0x05040100u);
 }
 
-// out = base + v for 4 consecutive columns (no: the token has no adapter, base alone)
-__device__ __forceinline__ void ad_store4(const AdArgs &a, size_t t, int col, f32x4_t v, bool no)
+// base[t][col, col + 8) as it lies (bf16: in r[0] alone); zeros without a base
+__device__ __forceinline__ void ad_base8(const AdArgs &a, bool ok, size_t t, int col, u32x4 (&r)[2])
 {
+    ok = ok && a.base;
     if (a.type == CD_TYPE_F32) {
-        if (a.base) {
-            const f32x4_t b = *reinterpret_cast<const f32x4_t *>(
-                static_cast<const float *>(a.base) + t * a.ldb + col);
-            v = no ? b : v + b;
-        }
-        *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + t * a.ldo + col) = v;
-        return;
-    }
-    uint2 w;
-    if (a.base) {
-        const uint2 b = *reinterpret_cast<const uint2 *>(
-            static_cast<const uint16_t *>(a.base) + t * a.ldb + col);
-        w = no ? b : uint2{ad_pack(v[0] + cdk::bf16_lo(b.x), v[1] + cdk::bf16_hi(b.x)),
-                           ad_pack(v[2] + cdk::bf16_lo(b.y), v[3] + cdk::bf16_hi(b.y))};
+        const float *b = static_cast<const float *>(a.base) + t * a.ldb + col;
+        r[0] = *reinterpret_cast<const u32x4 *>(or_zero(ok, b));
+        r[1] = *reinterpret_cast<const u32x4 *>(or_zero(ok, b + 4));
     } else {
-        w = uint2{ad_pack(v[0], v[1]), ad_pack(v[2], v[3])};
+        r[0] = load16(or_zero(ok, static_cast<const uint16_t *>(a.base) + t * a.ldb + col));
     }
-    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + col) = w;
+}
+
+// out[t][col, col + 8) = base + v (no: the token has no adapter, the base's bits)
+__device__ __forceinline__ void ad_store8(const AdArgs &a, size_t t, int col, const u32x4 (&b)[2],
+                                          const float (&v)[8], bool no)
+{
+    u32x4 w[2];
+    if (a.type == CD_TYPE_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i / 4][i % 4] = no ? b[i / 4][i % 4] : __float_as_uint(__uint_as_float(b[i / 4][i % 4]) + v[i]);
+        u32x4 *o = reinterpret_cast<u32x4 *>(static_cast<float *>(a.out) + t * a.ldo + col);
+        o[0] = w[0];
+        o[1] = w[1];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[0][i] = no ? b[0][i] : ad_pack(cdk::bf16_lo(b[0][i]) + v[2 * i], cdk::bf16_hi(b[0][i]) + v[2 * i + 1]);
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + t * a.ldo + col) = w[0];
+    }
 }
 
 // ---------------------------------------------------------------- decode: token by token
@@ -236,34 +245,7 @@ __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
 
 // ------------------------------------------------- many tokens: grouped by their adapters
 
-constexpr int kAdSortBlock = 1024;
-
-// sums over the workgroup of two counts, the second also as the exclusive prefix before
-// this thread
-__device__ __forceinline__ void ad_scan(int &less, int &mine, int &before)
-{
-    __shared__ int wl[kAdSortBlock / cdk::kWave], wm[kAdSortBlock / cdk::kWave];
-    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
-    int inc = mine;
-#pragma unroll
-    for (int d = 1; d < cdk::kWave; d *= 2) {
-        less += __shfl_xor(less, d);
-        const int up = __shfl_up(inc, d);
-        inc += lane >= d ? up : 0;
-    }
-    if (lane == cdk::kWave - 1) {
-        wl[wave] = less;
-        wm[wave] = inc;
-    }
-    __syncthreads();
-    before = inc - mine;
-    less = mine = 0;
-    for (int i = 0; i < kAdSortBlock / cdk::kWave; ++i) {
-        less += wl[i];
-        before += i < wave ? wm[i] : 0;
-        mine += wm[i];
-    }
-}
+constexpr int kAdSortBlock = 1024, kAdSortWaves = kAdSortBlock / cdk::kWave;
 
 // Workgroup g <= n finds the tokens of group g, in their order, by reading all ids: no
 // atomics, no order that depends on timing. Every group's places follow from the number b
@@ -292,22 +274,58 @@ __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
         }
         return;
     }
+    // a wave counts a run of tokens, 64 at a time, then writes its group's behind those of
+    // the waves before it
+    __shared__ int wl[kAdSortWaves], wm[kAdSortWaves];
     const int grp = blockIdx.x;
-    const int per = (a.T + kAdSortBlock - 1) / kAdSortBlock;
-    const int t0 = min(a.T, (int)threadIdx.x * per), t1 = min(a.T, t0 + per);
-    int less = 0, mine = 0, before;
-    for (int t = t0; t < t1; ++t) {
-        const int id = a.ids[t], of = ad_valid(a, id) ? id : a.n;
-        less += of < grp;
-        mine += of == grp;
+    const int lane = threadIdx.x % cdk::kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave);
+    const int per = (a.T + kAdSortBlock - 1) / kAdSortBlock * cdk::kWave;
+    const int t0 = min(a.T, wave * per), t1 = min(a.T, t0 + per);
+    const auto group_at = [&](int t) {  // past the run: no group
+        const int id = t < t1 ? a.ids[t] : 0;
+        return t >= t1 ? a.n + 1 : ad_valid(a, id) ? id : a.n;
+    };
+    int less = 0, mine = 0;
+    constexpr int kDeep = 8;  // loads in flight
+    for (int t = t0; t < t1; t += kDeep * cdk::kWave) {
+        int of[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+            of[u] = group_at(t + u * cdk::kWave + lane);
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+            less += __popcll(cdk::ballot(of[u] < grp));
+            mine += __popcll(cdk::ballot(of[u] == grp));
+        }
     }
-    ad_scan(less, mine, before);  // mine: the group's count
+    if (lane == 0) {
+        wl[wave] = less;
+        wm[wave] = mine;
+    }
+    __syncthreads();
+    int before = 0;
+    less = mine = 0;
+#pragma unroll
+    for (int i = 0; i < kAdSortWaves; ++i) {
+        less += wl[i];
+        before += i < wave ? wm[i] : 0;
+        mine += wm[i];  // the group's count
+    }
     const int first = (less + kAdPad - 1) / kAdPad * kAdPad + kAdPad * grp;
     int at = first + before;
-    for (int t = t0; t < t1; ++t) {
-        const int id = a.ids[t], of = ad_valid(a, id) ? id : a.n;
-        if (of == grp)
-            a.order[at++] = t;
+    for (int t = t0; t < t1; t += kDeep * cdk::kWave) {
+        int of[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+            of[u] = group_at(t + u * cdk::kWave + lane);
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+            const uint64_t all = cdk::ballot(of[u] == grp);
+            if (of[u] == grp)
+                a.order[at + cdk::lanes_below(all)] = t + u * cdk::kWave + lane;
+            at += __popcll(all);
+        }
     }
     if (threadIdx.x == 0)
         a.groups[grp] = AdGroup{first, mine};
@@ -424,8 +442,9 @@ __device__ __forceinline__ void ad_operand(const AdArgs &a, const float *lat, bo
 }
 
 // y = base + B lat for a tile of MT * 16 tokens, KC * 32 ranks. Each wave takes steps of 64
-// outputs: four MFMAs whose rows are permuted (row 16 (m / 4) + 4 j + m % 4) so that a lane ends with 16
-// consecutive outputs of its token.
+// outputs: four MFMAs whose rows are permuted (row m of MFMA j is output 32 (j / 2) + 8 (m / 4) +
+// 4 (j % 2) + m % 4) so that a lane ends with twice 8 consecutive outputs of its token, and
+// the four lanes of a token with 32.
 template <int MT, int KC>
 __global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
 {
@@ -451,6 +470,14 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
     const uint16_t *B = a.B + (no ? 0 : (size_t)tile.group * a.d_out * a.rank);
 #pragma unroll 1
     for (int o0 = (blockIdx.y * kAdWaves + wave) * 64; o0 < a.d_out; o0 += gridDim.y * kAdWaves * 64) {
+        u32x4 base[MT][2][2];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int o = o0 + 32 * h + 8 * g;
+                ad_base8(a, i * 16 + m < count && o < a.d_out, tok[i], o, base[i][h]);
+            }
         f32x4_t acc[MT][4];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -461,7 +488,7 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
             u32x4 b[4][KC];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int o = o0 + 16 * (m / 4) + 4 * j + m % 4;
+                const int o = o0 + 32 * (j / 2) + 8 * (m / 4) + 4 * (j % 2) + m % 4;
 #pragma unroll
                 for (int c = 0; c < KC; ++c) {
                     const int k = c * 32 + g * 8;
@@ -482,17 +509,21 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
         for (int i = 0; i < MT; ++i)
             if (i * 16 + m < count)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int o = o0 + 16 * g + 4 * j;
+                for (int h = 0; h < 2; ++h) {
+                    const int o = o0 + 32 * h + 8 * g;
+                    const float v[8] = {acc[i][2 * h][0], acc[i][2 * h][1], acc[i][2 * h][2],
+                                        acc[i][2 * h][3], acc[i][2 * h + 1][0], acc[i][2 * h + 1][1],
+                                        acc[i][2 * h + 1][2], acc[i][2 * h + 1][3]};
                     if (o < a.d_out)
-                        ad_store4(a, tok[i], o, acc[i][j], no);
+                        ad_store8(a, tok[i], o, base[i][h], v, no);
                 }
     }
 }
 
 // dx = base + A^T glat: as k_ad_expand, but the factor's rows run along the outputs, so a
-// lane loads 8 ranks x 8 columns and transposes them: steps of 128 columns, eight MFMAs, 32
-// consecutive columns of a token per lane.
+// lane loads 8 ranks x 8 columns and transposes them: steps of 128 columns, eight MFMAs.
+// Row m of MFMA j is column 8 (4 (m % 4) + m / 4) + j, so a lane ends with four times 8
+// consecutive columns and the four lanes of a token with 32.
 template <int MT, int KC>
 __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
 {
@@ -518,6 +549,15 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
     const uint16_t *A = a.A + (no ? 0 : (size_t)tile.group * a.d_in * a.rank);
 #pragma unroll 1
     for (int c0 = (blockIdx.y * kAdWaves + wave) * 128; c0 < a.d_in; c0 += gridDim.y * kAdWaves * 128) {
+        u32x4 base[MT][4][2];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int col = c0 + 8 * (4 * q + g);
+                ad_base8(a, i * 16 + m < count && col < a.d_in, tok[i], col, base[i][q]);
+            }
+        const int cm = c0 + 8 * (4 * (m % 4) + m / 4);  // the columns that this lane loads
         f32x4_t acc[MT][8];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -528,10 +568,10 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
                 u32x4 rows[8], cols[8];
-                const bool ok = c * 32 + g * 8 < a.rank && c0 + m * 8 < a.d_in;
+                const bool ok = c * 32 + g * 8 < a.rank && cm < a.d_in;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    rows[e] = load16(or_zero(ok, A + (size_t)(c * 32 + g * 8 + e) * a.d_in + c0 + m * 8));
+                    rows[e] = load16(or_zero(ok, A + (size_t)(c * 32 + g * 8 + e) * a.d_in + cm));
                 ad_transpose8(rows, cols);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -542,17 +582,16 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
                             acc[i][j] = mfma16(cols[j], lt[i][c][s], acc[i][j]);
             }
         }
-        // acc[i][j][q]: column c0 + 8 (4 g + q) + j
 #pragma unroll
         for (int i = 0; i < MT; ++i)
             if (i * 16 + m < count)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int col = c0 + 8 * (4 * g + q);
-                    if (col < a.d_in) {
-                        ad_store4(a, tok[i], col, f32x4_t{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]}, no);
-                        ad_store4(a, tok[i], col + 4, f32x4_t{acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]}, no);
-                    }
+                    const int col = c0 + 8 * (4 * q + g);
+                    const float v[8] = {acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q],
+                                        acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
+                    if (col < a.d_in)
+                        ad_store8(a, tok[i], col, base[i][q], v, no);
                 }
     }
 }

@@ -202,16 +202,15 @@ def test_clip_launches(host, clip):
         assert clip_call(host, clip, *a, **kw) == 0
         return [k for k, _ in host.launches()]
 
-    both, norm = ["k_clip_norm", "k_clip_scale"], ["k_clip_norm"]
+    both, norm = ["k_clip_norm", "k_clip_scale"], ["k_clip_norm", "k_clip_total"]
     assert kernels([(G0, G0, 1 << 20, 0), (G1, G1, 5, 1)], 1.0) == both
     assert kernels([(G0, G0, 1 << 20, 0)], math.inf) == norm
     assert kernels([(G0, O0, 1 << 20, 0)], math.inf) == both
     assert kernels([(G0, 0, 1 << 20, 0)] * 2, math.inf) == norm  # the norm may count one twice
-    assert kernels([], 1.0) == norm
-    assert kernels([(0, 0, 0, 0)] * 200, 1.0)[:1] == norm
+    assert kernels([], 1.0) == kernels([(0, 0, 0, 0)] * 200, 1.0) == ["k_clip_total"]
     many = [(G0 + 4096 * i, G0 + 4096 * i, 1024, 0) for i in range(200)]
-    assert kernels(many, 1.0) == norm * 3 + ["k_clip_scale"] * 3
-    assert kernels([(G0, O0, 8, 0)], 1.0, norm=None)[:1] == norm
+    assert kernels(many, 1.0) == ["k_clip_norm"] * 3 + ["k_clip_scale"] * 3
+    assert kernels([(G0, O0, 8, 0)], 1.0, norm=None) == both
     assert clip_call(host, clip, [(G0, O0, (1 << 38) + 1, 0)], 1.0) == host.cd.CD_EUNSUPPORTED
     assert host.lib.countdown_clip_grads(clip, None, 1, 1.0, None, None) == host.cd.CD_EINVAL
     assert host.lib.countdown_clip_grads(None, None, 0, 1.0, None, None) == host.cd.CD_EINVAL
