@@ -56,8 +56,7 @@ struct AdArgs {
     AdGroup *groups;  // [n + 1]
     AdTile *tiles;
     uint16_t *Bt;            // [n][rank][d_out], B transposed (training)
-    uint16_t *latT, *glatT;  // [3][rank][positions]: lat and glat split in three bf16 terms
-    int positions;
+    uint16_t *latT, *glatT;  // lat and glat split in three bf16 terms (ad_term_at; training)
     int tile;  // tokens of a tile: 16, 32 or 64
 };
 
@@ -105,6 +104,38 @@ __device__ __forceinline__ void ad_transpose8(const u32x4 (&r)[8], u32x4 (&c)[8]
         for (int i = 0; i < 4; ++i)
             c[j][i] = __builtin_amdgcn_perm(r[2 * i + 1][j / 2], r[2 * i][j / 2],
                                             j % 2 ? 0x07060302u : 0x05040100u);
+}
+
+// The vector memory unit merges four neighbouring lanes: a load in operand layout, 16 rows on
+// 16 neighbouring lanes, takes it 64 cycles a KB (38 GB/s a CU, with two operands less than a
+// CU's share of HBM), one whose lanes follow a row 16. So 16 rows x 128 columns come in four
+// loads of 4 rows x 256 bytes (lane: row 4 i + lane / 16, columns 8 (lane % 16)) and turn
+// into the four operands of those columns in 4 KB of LDS that the wave has to itself. The
+// 16-byte chunks of a row are stored in an order of its own (xor), which spreads 16 rows
+// over the banks.
+constexpr int kAdStage = 256;  // 16-byte chunks
+
+// the wave's number, known to be uniform
+__device__ __forceinline__ int ad_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave); }
+
+__device__ __forceinline__ void ad_wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+__device__ __forceinline__ void ad_stage(u32x4 (&v)[4], u32x4 *lds, int lane)
+{
+    const int m = lane % 16, g = lane / 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        lds[(4 * i + g) * 16 + (m ^ (4 * i + g))] = v[i];
+    ad_wave_sync();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = lds[m * 16 + ((4 * i + g) ^ m)];
+    ad_wave_sync();
 }
 
 // base[t][col, col + 8) as it lies (bf16: in r[0] alone); zeros without a base
@@ -197,33 +228,56 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_up(const AdArgs a)
 }
 
 // y = W x + B lat for up to 16 tokens: a workgroup's eight waves each take an eighth of the
-// columns of 16 rows of W (all of their loads in flight at once), the tokens are the other
-// operand; the waves' sums meet in LDS, where the adapters' part is added.
+// columns of 16 rows of W (128 at a time, the next 128 in flight), the tokens are the other
+// operand; the waves' sums meet in LDS, where the adapters' part is added. Rows past the
+// last and tokens past T repeat the last one: they only reach sums of their own.
 constexpr int kAdProjBlock = 512, kAdProjWaves = kAdProjBlock / cdk::kWave;
 
 __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
 {
-    __shared__ f32x4_t sums[kAdProjWaves][cdk::kWave];
-    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    __shared__ u32x4 lds[kAdProjWaves][kAdStage];
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
     const int o0 = blockIdx.x * 16;
-    const bool row_ok = o0 + m < a.d_out, tok_ok = m < a.T;
-    const uint16_t *w = a.W + (size_t)(o0 + m) * a.d_in, *x = a.x + m * a.ldx;
-    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 1
-    for (int kb = wave * 128; kb < a.d_in; kb += 128 * kAdProjWaves) {
-        u32x4 wv[4], xv[4];
+    const uint16_t *w[4], *x[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int k = kb + 32 * u + 8 * g;
-            wv[u] = load16(or_zero(row_ok && k < a.d_in, w + k));
-            xv[u] = load16(or_zero(tok_ok && k < a.d_in, x + k));
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            acc = mfma16(wv[u], xv[u], acc);
+    for (int i = 0; i < 4; ++i) {
+        w[i] = a.W + (size_t)min(o0 + 4 * i + g, a.d_out - 1) * a.d_in;
+        x[i] = a.x + min(4 * i + g, a.T - 1) * a.ldx;
     }
-    sums[wave][lane] = acc;
+    constexpr int kStep = 128 * kAdProjWaves;
+    u32x4 wv[2][4], xv[2][4];
+    const auto load = [&](int s, int k) {
+        k += 8 * m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            wv[s][i] = load16(or_zero(k < a.d_in, w[i] + k));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i == 0 || 4 * i < a.T)
+                xv[s][i] = load16(or_zero(k < a.d_in, x[i] + k));
+    };
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    load(0, wave * 128);
+#pragma unroll 1
+    for (int kb = wave * 128; kb < a.d_in; kb += 2 * kStep) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int k = kb + s * kStep;
+            if (k >= a.d_in)
+                break;
+            if (k + kStep < a.d_in)
+                load(1 - s, k + kStep);
+            ad_stage(wv[s], lds[wave], lane);
+            ad_stage(xv[s], lds[wave], lane);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                acc = mfma16(wv[s][u], xv[s][u], acc);
+        }
+    }
+    f32x4_t *sums = reinterpret_cast<f32x4_t *>(&lds[0][0]);
+    __syncthreads();
+    sums[threadIdx.x] = acc;
     __syncthreads();
     if (threadIdx.x >= 256)
         return;
@@ -233,7 +287,7 @@ __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
     float v = 0.0f;
 #pragma unroll
     for (int i = 0; i < kAdProjWaves; ++i)
-        v += sums[i][r / 4 * 16 + t][r % 4];
+        v += sums[i * cdk::kWave + r / 4 * 16 + t][r % 4];
     const int id = a.ids[t];
     if (ad_valid(a, id))
         v += ad_row(a, id, o, a.lat + t * a.rank);
@@ -278,8 +332,7 @@ __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
     // the waves before it
     __shared__ int wl[kAdSortWaves], wm[kAdSortWaves];
     const int grp = blockIdx.x;
-    const int lane = threadIdx.x % cdk::kWave;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave);
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int per = (a.T + kAdSortBlock - 1) / kAdSortBlock * cdk::kWave;
     const int t0 = min(a.T, wave * per), t1 = min(a.T, t0 + per);
     const auto group_at = [&](int t) {  // past the run: no group
@@ -336,90 +389,125 @@ __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
     }
 }
 
+// Where the terms of lat lie for the gradients: the operands of 32 positions and 16 ranks
+// (lane: rank r % 16, positions 8 (lane / 16) and on) are one run of 1 KB.
+__device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, int r)
+{
+    const int rts = (a.rank + 15) / 16;
+    return ((p / 32 * 3 + s) * rts + r / 16) * 512 + ((p % 32 / 8) * 16 + r % 16) * 8 + p % 8;
+}
+
 // The low-rank latents of a tile of MT * 16 tokens and RT * 16 ranks (blockIdx.y the ranks;
-// blockIdx.z: with both, 1 is glat). Eight waves split the contraction in blocks of 128
-// columns, and their sums meet in LDS. The scale is applied here.
+// blockIdx.z: with both, 0 is glat). Eight waves split the contraction in blocks of 128
+// columns, and their sums meet in LDS. The scale is applied here. Tokens past the tile's last
+// and ranks past the last repeat another: they only reach sums of their own, which are not
+// stored.
 constexpr int kAdShrinkBlock = 512, kAdShrinkWaves = kAdShrinkBlock / cdk::kWave;
 
 template <int MT, int RT>
-__global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, int first_kind)
+__global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, int kinds)
 {
     static_assert(MT * RT * cdk::kWave <= kAdShrinkBlock, "one sum per thread");
-    __shared__ f32x4_t sums[kAdShrinkWaves][MT * RT * cdk::kWave];
+    constexpr int kSums = MT * RT * cdk::kWave;
+    constexpr int kDepth = MT + RT <= 3 ? 2 : 1;  // blocks in flight
+    __shared__ u32x4 lds[kAdShrinkWaves * (kSums > kAdStage ? kSums : kAdStage)];
     const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
     const AdTile tile = a.tiles[blockIdx.x / sub];
     const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
     if (count <= 0 || tile.group == a.n)
         return;
-    const bool back = blockIdx.z + first_kind;  // glat
+    const bool back = kinds == 3 ? blockIdx.z == 0 : kinds == 2;  // glat
     const int K = back ? a.d_out : a.d_in;
     const uint16_t *src = back ? a.dy : a.x;
     const size_t ld = back ? a.lddy : a.ldx;
     const uint16_t *fac = (back ? a.Bt : a.A) + (size_t)tile.group * a.rank * K;
-    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
     const int r0 = blockIdx.y * RT * 16;
-    const uint16_t *xp[MT], *fp[RT];
-    bool xok[MT], fok[RT];
+    const uint16_t *xp[MT][4], *fp[RT][4];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        xok[i] = i * 16 + m < count;
-        xp[i] = src + (xok[i] ? (size_t)a.order[tile.first + off + i * 16 + m] * ld : 0);
-    }
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        fok[i] = r0 + i * 16 + m < a.rank;
-        fp[i] = fac + (fok[i] ? (size_t)(r0 + i * 16 + m) * K : 0);
-    }
+        for (int q = 0; q < 4; ++q)
+            xp[i][q] = src + a.order[tile.first + off + min(i * 16 + 4 * q + g, count - 1)] * ld;
+#pragma unroll
+    for (int j = 0; j < RT; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            fp[j][q] = fac + (size_t)min(r0 + j * 16 + 4 * q + g, a.rank - 1) * K;
+    u32x4 xv[kDepth][MT][4], fv[kDepth][RT][4];
+    const auto load = [&](int s, int k) {
+        k += 8 * m;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                xv[s][i][q] = load16(or_zero(k < K, xp[i][q] + k));
+#pragma unroll
+        for (int j = 0; j < RT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                fv[s][j][q] = load16(or_zero(k < K, fp[j][q] + k));
+    };
     f32x4_t acc[MT][RT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < RT; ++j)
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 *stage = lds + wave * kAdStage;
+    constexpr int kStep = 128 * kAdShrinkWaves;
+    if (kDepth == 2)
+        load(0, wave * 128);
 #pragma unroll 1
-    for (int kb = wave * 128; kb < K; kb += 128 * kAdShrinkWaves) {
-        u32x4 xv[4][MT], fv[4][RT];
+    for (int kb = wave * 128; kb < K; kb += kDepth * kStep) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int k = kb + 32 * u + 8 * g;
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-                xv[u][i] = load16(or_zero(xok[i] && k < K, xp[i] + k));
+        for (int s = 0; s < kDepth; ++s) {
+            const int k = kb + s * kStep;
+            if (k >= K)
+                break;
+            if (kDepth == 1)
+                load(0, k);
+            else if (k + kStep < K)
+                load(1 - s, k + kStep);
 #pragma unroll
             for (int j = 0; j < RT; ++j)
-                fv[u][j] = load16(or_zero(fok[j] && k < K, fp[j] + k));
+                ad_stage(fv[s][j], stage, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                ad_stage(xv[s][i], stage, lane);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int j = 0; j < RT; ++j)
+                        acc[i][j] = mfma16(fv[s][j][u], xv[s][i][u], acc[i][j]);
+            }
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < RT; ++j)
-                    acc[i][j] = mfma16(fv[u][j], xv[u][i], acc[i][j]);
     }
+    f32x4_t *sums = reinterpret_cast<f32x4_t *>(lds);
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < RT; ++j)
-            sums[wave][(i * RT + j) * cdk::kWave + lane] = acc[i][j];
+            sums[wave * kSums + (i * RT + j) * cdk::kWave + lane] = acc[i][j];
     __syncthreads();
-    if (threadIdx.x >= MT * RT * cdk::kWave)
+    if (threadIdx.x >= kSums)
         return;
     f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < kAdShrinkWaves; ++w)
-        v += sums[w][threadIdx.x];
+        v += sums[w * kSums + threadIdx.x];
     v *= ad_scale(a, tile.group);
     // this thread: token i * 16 + m, ranks r .. r + 3
-    const int at = threadIdx.x / cdk::kWave / RT * 16 + m;
-    const int r = r0 + threadIdx.x / cdk::kWave % RT * 16 + g * 4;
+    const int at = wave / RT * 16 + m;
+    const int r = r0 + wave % RT * 16 + g * 4;
     if (at >= count || r >= a.rank)
         return;
     const size_t p = tile.first + off + at;
     *reinterpret_cast<f32x4_t *>((back ? a.glat : a.lat) + p * a.rank + r) = v;
-    uint16_t *tr = back ? a.glatT : a.latT;
-    if (!tr)
+    uint16_t *terms = back ? a.glatT : a.latT;
+    if (!terms)
         return;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -427,7 +515,7 @@ __global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, in
         ad_split(v[q], s);
 #pragma unroll
         for (int k = 0; k < 3; ++k)
-            tr[((size_t)k * a.rank + r + q) * a.positions + p] = (uint16_t)(s[k] >> 16);
+            terms[ad_term_at(a, p, k, r + q)] = (uint16_t)(s[k] >> 16);
     }
 }
 
@@ -441,137 +529,189 @@ __device__ __forceinline__ void ad_operand(const AdArgs &a, const float *lat, bo
     ad_split8(v, t);
 }
 
-// y = base + B lat for a tile of MT * 16 tokens, KC * 32 ranks. Each wave takes steps of 64
-// outputs: four MFMAs whose rows are permuted (row m of MFMA j is output 32 (j / 2) + 8 (m / 4) +
-// 4 (j % 2) + m % 4) so that a lane ends with twice 8 consecutive outputs of its token, and
-// the four lanes of a token with 32.
+// A wave's tokens and their latents' terms: rows of the MFMA operands
 template <int MT, int KC>
+struct AdTokens {
+    int count;
+    bool no;  // group n: no adapter
+    int group;
+    u32x4 lt[MT][KC][3];
+    int tok[MT][4];  // rows 4 g + q of the results
+
+    __device__ __forceinline__ bool init(const AdArgs &a, const float *lat, int m, int g)
+    {
+        const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
+        const AdTile tile = a.tiles[blockIdx.x / sub];
+        const int off = blockIdx.x % sub * MT * 16;
+        count = tile.count - off;
+        group = tile.group;
+        no = group == a.n;
+        if (count <= 0 || (no && a.base == a.out))
+            return false;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                tok[i][q] = a.order[tile.first + off + min(i * 16 + 4 * g + q, count - 1)];
+#pragma unroll
+            for (int c = 0; c < KC; ++c)
+                ad_operand(a, lat, i * 16 + m < count && !no, tile.first + off + i * 16 + m,
+                           c * 32 + g * 8, lt[i][c]);
+        }
+        return true;
+    }
+    __device__ __forceinline__ bool live(int i, int g, int q) const { return i * 16 + 4 * g + q < count; }
+};
+
+// y = base + B lat for a tile of MT * 16 tokens, KC * 32 ranks. Each wave takes steps of 128
+// outputs: eight MFMAs with the tokens as rows and B's rows as columns. Column m of MFMA
+// j is output 8 m + j (fp32: 4 m + j % 4 of the half j / 4), so that a lane ends with 16
+// bytes of a token's row and 16 neighbouring lanes with 256. B's rows pass through LDS:
+// 32 ranks of 128 outputs, read as they lie.
+template <int MT, int KC, bool F32>
 __global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
 {
-    const int sub = a.tile / (MT * 16);
-    const AdTile tile = a.tiles[blockIdx.x / sub];
-    const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
-    const bool no = tile.group == a.n;
-    if (count <= 0 || (no && a.base == a.out))
-        return;
-    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    constexpr int kPad = F32 ? 4 : 8;  // a chunk more every so many rows: 16 columns on 16 banks
+    __shared__ u32x4 lds[kAdWaves][128 * 4 + 128 / kPad];
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
-    size_t tok[MT];
-    u32x4 lt[MT][KC][3];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const bool ok = i * 16 + m < count;
-        const size_t p = tile.first + off + i * 16 + m;
-        tok[i] = ok ? a.order[p] : 0;
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-            ad_operand(a, a.lat, ok && !no, p, c * 32 + g * 8, lt[i][c]);
-    }
-    const uint16_t *B = a.B + (no ? 0 : (size_t)tile.group * a.d_out * a.rank);
-#pragma unroll 1
-    for (int o0 = (blockIdx.y * kAdWaves + wave) * 64; o0 < a.d_out; o0 += gridDim.y * kAdWaves * 64) {
-        u32x4 base[MT][2][2];
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int o = o0 + 32 * h + 8 * g;
-                ad_base8(a, i * 16 + m < count && o < a.d_out, tok[i], o, base[i][h]);
-            }
-        f32x4_t acc[MT][4];
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!no) {
-            u32x4 b[4][KC];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int o = o0 + 32 * (j / 2) + 8 * (m / 4) + 4 * (j % 2) + m % 4;
-#pragma unroll
-                for (int c = 0; c < KC; ++c) {
-                    const int k = c * 32 + g * 8;
-                    b[j][c] = load16(or_zero(o < a.d_out && k < a.rank, B + (size_t)o * a.rank + k));
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int c = 0; c < KC; ++c)
-#pragma unroll
-                    for (int s = 2; s >= 0; --s)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i)
-                            acc[i][j] = mfma16(b[j][c], lt[i][c][s], acc[i][j]);
-        }
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-            if (i * 16 + m < count)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int o = o0 + 32 * h + 8 * g;
-                    const float v[8] = {acc[i][2 * h][0], acc[i][2 * h][1], acc[i][2 * h][2],
-                                        acc[i][2 * h][3], acc[i][2 * h + 1][0], acc[i][2 * h + 1][1],
-                                        acc[i][2 * h + 1][2], acc[i][2 * h + 1][3]};
-                    if (o < a.d_out)
-                        ad_store8(a, tok[i], o, base[i][h], v, no);
-                }
-    }
-}
-
-// dx = base + A^T glat: as k_ad_expand, but the factor's rows run along the outputs, so a
-// lane loads 8 ranks x 8 columns and transposes them: steps of 128 columns, eight MFMAs.
-// Row m of MFMA j is column 8 (4 (m % 4) + m / 4) + j, so a lane ends with four times 8
-// consecutive columns and the four lanes of a token with 32.
-template <int MT, int KC>
-__global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
-{
-    const int sub = a.tile / (MT * 16);
-    const AdTile tile = a.tiles[blockIdx.x / sub];
-    const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
-    const bool no = tile.group == a.n;
-    if (count <= 0 || (no && a.base == a.out))
+    AdTokens<MT, KC> tk;
+    if (!tk.init(a, a.lat, m, g))
         return;
-    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
-    const int m = lane % 16, g = lane / 16;
-    size_t tok[MT];
-    u32x4 lt[MT][KC][3];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const bool ok = i * 16 + m < count;
-        const size_t p = tile.first + off + i * 16 + m;
-        tok[i] = ok ? a.order[p] : 0;
-#pragma unroll
-        for (int c = 0; c < KC; ++c)
-            ad_operand(a, a.glat, ok && !no, p, c * 32 + g * 8, lt[i][c]);
-    }
-    const uint16_t *A = a.A + (no ? 0 : (size_t)tile.group * a.d_in * a.rank);
+    const uint16_t *B = a.B + (tk.no ? 0 : (size_t)tk.group * a.d_out * a.rank);
+    u32x4 *st = lds[wave];
 #pragma unroll 1
-    for (int c0 = (blockIdx.y * kAdWaves + wave) * 128; c0 < a.d_in; c0 += gridDim.y * kAdWaves * 128) {
-        u32x4 base[MT][4][2];
+    for (int o0 = (blockIdx.y * kAdWaves + wave) * 128; o0 < a.d_out; o0 += gridDim.y * kAdWaves * 128) {
+        // this lane's columns: cols(h) .. + 8 (fp32: 4)
+        u32x4 base[MT][4][F32 ? 2 : 1];
+        const auto cols = [&](int h) { return F32 ? o0 + 64 * h + 4 * m : o0 + 8 * m; };
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = c0 + 8 * (4 * q + g);
-                ad_base8(a, i * 16 + m < count && col < a.d_in, tok[i], col, base[i][q]);
-            }
-        const int cm = c0 + 8 * (4 * (m % 4) + m / 4);  // the columns that this lane loads
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int h = 0; h < (F32 ? 2 : 1); ++h) {
+                    const bool ok = a.base && tk.live(i, g, q) && cols(h) < a.d_out;
+                    const size_t at = (size_t)tk.tok[i][q] * a.ldb + cols(h);
+                    base[i][q][h] =
+                        F32 ? *reinterpret_cast<const u32x4 *>(or_zero(ok, static_cast<const float *>(a.base) + at))
+                            : load16(or_zero(ok, static_cast<const uint16_t *>(a.base) + at));
+                }
         f32x4_t acc[MT][8];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!no) {
+        if (!tk.no)
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                // chunk ch of row `row`; a row past the last repeats it (sums not stored)
+                const int nch = min(4, a.rank / 8 - 4 * c);  // uniform
+                if (nch <= 0)
+                    break;
+                u32x4 v[8];
+                const auto place = [&](int i, int &row, int &ch) {
+                    const int e = i * cdk::kWave + lane;
+                    row = nch == 4 ? e / 4 : nch == 2 ? e / 2 : nch == 1 ? e : e / 3;
+                    ch = e - row * nch;
+                };
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < 2 * nch) {
+                        int row, ch;
+                        place(i, row, ch);
+                        v[i] = load16(B + (size_t)min(o0 + row, a.d_out - 1) * a.rank + (4 * c + ch) * 8);
+                    }
+                ad_wave_sync();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < 2 * nch) {
+                        int row, ch;
+                        place(i, row, ch);
+                        st[row * 4 + ch + row / kPad] = v[i];
+                    }
+                ad_wave_sync();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int row = F32 ? j / 4 * 64 + 4 * m + j % 4 : 8 * m + j;
+                    u32x4 b = st[row * 4 + g + row / kPad];
+                    if (g >= nch)  // (ranks past the last)
+                        b = cdk::zero16();
+#pragma unroll
+                    for (int s = 2; s >= 0; --s)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+                            acc[i][j] = mfma16(tk.lt[i][c][s], b, acc[i][j]);
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (tk.live(i, g, q)) {
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            u32x4 w = base[i][q][h];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                w[e] = tk.no ? w[e] : __float_as_uint(__uint_as_float(w[e]) + acc[i][4 * h + e][q]);
+                            if (cols(h) < a.d_out)
+                                *reinterpret_cast<u32x4 *>(static_cast<float *>(a.out) +
+                                                           (size_t)tk.tok[i][q] * a.ldo + cols(h)) = w;
+                        }
+                    } else {
+                        u32x4 w = base[i][q][0];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = tk.no ? w[e]
+                                         : ad_pack(cdk::bf16_lo(w[e]) + acc[i][2 * e][q],
+                                                   cdk::bf16_hi(w[e]) + acc[i][2 * e + 1][q]);
+                        if (cols(0) < a.d_out)
+                            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) +
+                                                       (size_t)tk.tok[i][q] * a.ldo + cols(0)) = w;
+                    }
+                }
+    }
+}
+
+// dx = base + A^T glat: as k_ad_expand, but the factor's rows run along the outputs, so a
+// lane loads 8 ranks x 8 columns and transposes them in registers: steps of 128 columns,
+// column m of MFMA j is 8 m + j.
+template <int MT, int KC>
+__global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
+{
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
+    const int m = lane % 16, g = lane / 16;
+    AdTokens<MT, KC> tk;
+    if (!tk.init(a, a.glat, m, g))
+        return;
+    const uint16_t *A = a.A + (tk.no ? 0 : (size_t)tk.group * a.d_in * a.rank);
+#pragma unroll 1
+    for (int c0 = (blockIdx.y * kAdWaves + wave) * 128; c0 < a.d_in; c0 += gridDim.y * kAdWaves * 128) {
+        const int col = c0 + 8 * m;
+        const bool cok = col < a.d_in;
+        u32x4 base[MT][4][2];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                ad_base8(a, tk.live(i, g, q) && cok, tk.tok[i][q], col, base[i][q]);
+        f32x4_t acc[MT][8];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (!tk.no)
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
                 u32x4 rows[8], cols[8];
-                const bool ok = c * 32 + g * 8 < a.rank && cm < a.d_in;
+                const bool ok = c * 32 + g * 8 < a.rank && cok;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    rows[e] = load16(or_zero(ok, A + (size_t)(c * 32 + g * 8 + e) * a.d_in + cm));
+                    rows[e] = load16(or_zero(ok, A + (size_t)(c * 32 + g * 8 + e) * a.d_in + col));
                 ad_transpose8(rows, cols);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -579,66 +719,73 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
                     for (int s = 2; s >= 0; --s)
 #pragma unroll
                         for (int i = 0; i < MT; ++i)
-                            acc[i][j] = mfma16(cols[j], lt[i][c][s], acc[i][j]);
+                            acc[i][j] = mfma16(tk.lt[i][c][s], cols[j], acc[i][j]);
             }
-        }
+        if (cok)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-            if (i * 16 + m < count)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int col = c0 + 8 * (4 * q + g);
                     const float v[8] = {acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q],
                                         acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
-                    if (col < a.d_in)
-                        ad_store8(a, tok[i], col, base[i][q], v, no);
+                    if (tk.live(i, g, q))
+                        ad_store8(a, tk.tok[i][q], col, base[i][q], v, tk.no);
                 }
     }
 }
 
-// dA = glat^T x and dB = dy^T lat of one adapter: 128 columns of x or dy and RT * 16 ranks.
-// The contraction runs over the adapter's tokens, 32 at a time: a lane loads 8 tokens x 8
-// columns and transposes them. `split` of the workgroup's four waves share a column tile and
-// take every split-th chunk of tokens; their sums meet in LDS.
-template <int RT, bool DB>
-__device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int split, f32x4_t (&lds)[2][cdk::kWave * 8])
+// dA = glat^T x and dB = dy^T lat of one adapter: 128 columns of x or dy and RT * 16 ranks a
+// workgroup. The contraction runs over the adapter's tokens, 32 at a time: a lane loads 8
+// tokens x 8 columns (the next 32 tokens' in flight) and transposes them. The waves take every
+// WAVES-th 32 tokens; their sums meet in LDS.
+template <int RT, int WAVES, bool DB>
+__device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *lds)
 {
-    const int lane = threadIdx.x % cdk::kWave, wave = threadIdx.x / cdk::kWave;
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
-    const int width = DB ? a.d_out : a.d_in, per = kAdWaves / split;  // column tiles of a workgroup
-    const int tiles = (width + 128 * per - 1) / (128 * per), rgs = (a.rank + RT * 16 - 1) / (RT * 16);
-    const int ad = block / (tiles * rgs), r0 = block / tiles % rgs * RT * 16;
-    const int c0 = (block % tiles * per + wave / split) * 128;
+    const int width = DB ? a.d_out : a.d_in, tiles = (width + 127) / 128;
+    const int rts = (a.rank + 15) / 16, rgs = (rts + RT - 1) / RT;
+    const int ad = block / (tiles * rgs), rt0 = block / tiles % rgs * RT;
+    const int c0 = block % tiles * 128, col = c0 + m * 8;
     const AdGroup grp = a.groups[ad];
     const uint16_t *src = DB ? a.dy : a.x;
     const size_t ld = DB ? a.lddy : a.ldx;
     const uint16_t *fac = DB ? a.latT : a.glatT;
-    const size_t term = (size_t)a.rank * a.positions;
-    const bool cok = c0 + m * 8 < width;
+    const bool cok = col < width;
     f32x4_t acc[RT][8];
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 1
-    for (int p = wave % split * 32; p < grp.count; p += split * 32) {
-        const int left = grp.count - p - g * 8;  // tokens from this lane's first
+    u32x4 rows[8], f[RT][3];
+    // tokens past the group's end load zeros; ranks past the last repeat the last tile's
+    const auto load_rows = [&](int p) {
         const int *ord = a.order + grp.first + p + g * 8;
-        u32x4 rows[8], cols[8], f[RT][3];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool ok = e < left && cok;
-            rows[e] = load16(or_zero(ok, src + (ok ? (size_t)ord[e] * ld : 0) + c0 + m * 8));
+            const bool ok = p + g * 8 + e < grp.count && cok;
+            rows[e] = load16(or_zero(ok, src + (ok ? (size_t)ord[e] * ld : 0) + col));
         }
+    };
+    const auto load_term = [&](int p, int s) {
 #pragma unroll
         for (int i = 0; i < RT; ++i)
+            f[i][s] = load16(fac + (((size_t)(grp.first + p) / 32 * 3 + s) * rts + min(rt0 + i, rts - 1)) * 512 + lane * 8);
+    };
+    int p = wave * 32;
+    if (p < grp.count) {
+        load_rows(p);
 #pragma unroll
-            for (int s = 0; s < 3; ++s) {
-                const int r = r0 + i * 16 + m;
-                f[i][s] = load16(or_zero(r < a.rank && left > 0,
-                                         fac + s * term + (size_t)r * a.positions + grp.first + p + g * 8));
-            }
+        for (int s = 2; s >= 0; --s)
+            load_term(p, s);
+    }
+#pragma unroll 1
+    for (; p < grp.count; p += WAVES * 32) {
+        const int next = p + WAVES * 32;
+        u32x4 cols[8];
+        ad_transpose8(rows, cols);
+        const int left = grp.count - p - g * 8;  // tokens from this lane's first
         if (grp.count - p < 32) {  // what lies past the group's end is not a number of this call
 #pragma unroll
             for (int i = 0; i < RT; ++i)
@@ -648,51 +795,54 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int split, 
                     for (int e = 0; e < 4; ++e)
                         f[i][s][e] &= (2 * e < left ? 0xffffu : 0u) | (2 * e + 1 < left ? 0xffff0000u : 0u);
         }
-        ad_transpose8(rows, cols);
+        if (next < grp.count)
+            load_rows(next);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int s = 2; s >= 0; --s) {
 #pragma unroll
-            for (int s = 2; s >= 0; --s)
+            for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
                     acc[i][j] = DB ? mfma16(f[i][s], cols[j], acc[i][j]) : mfma16(cols[j], f[i][s], acc[i][j]);
+            if (next < grp.count)
+                load_term(next, s);
+        }
     }
-    // waves of one column tile: the upper half of them hands its sums to the lower, by halves
-    for (int half = split / 2; half >= 1; half /= 2)
+    // the upper half of the waves hands its sums to the lower, until one has them all
+#pragma unroll
+    for (int half = WAVES / 2; half >= 1; half /= 2)
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const int w = wave % split, to = wave / split * half + w % half;
             __syncthreads();
-            if (w >= half && w < 2 * half)
+            if (wave >= half && wave < 2 * half)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    lds[to][j * cdk::kWave + lane] = acc[i][j];
+                    lds[((wave - half) * 8 + j) * cdk::kWave + lane] = acc[i][j];
             __syncthreads();
-            if (w < half)
+            if (wave < half)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    acc[i][j] += lds[to][j * cdk::kWave + lane];
+                    acc[i][j] += lds[(wave * 8 + j) * cdk::kWave + lane];
         }
-    if (wave % split)
+    if (wave)
         return;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         if constexpr (DB) {  // row o = c0 + 8 m + j, ranks 4 g + q
-            const int r = r0 + i * 16 + g * 4;
+            const int r = (rt0 + i) * 16 + g * 4;
             if (cok && r < a.rank)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<f32x4_t *>(
-                        a.dB + ((size_t)ad * a.d_out + c0 + m * 8 + j) * a.rank + r) = acc[i][j];
+                    *reinterpret_cast<f32x4_t *>(a.dB + ((size_t)ad * a.d_out + col + j) * a.rank + r) =
+                        acc[i][j];
         } else {  // row r = m, columns c0 + 8 (4 g + q) + j
-            const int r = r0 + i * 16 + m;
+            const int r = (rt0 + i) * 16 + m;
             if (r < a.rank)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int col = c0 + 8 * (4 * g + q);
-                    if (col < a.d_in) {
-                        f32x4_t *d = reinterpret_cast<f32x4_t *>(
-                            a.dA + ((size_t)ad * a.rank + r) * a.d_in + col);
+                    const int c = c0 + 8 * (4 * g + q);
+                    if (c < a.d_in) {
+                        f32x4_t *d = reinterpret_cast<f32x4_t *>(a.dA + ((size_t)ad * a.rank + r) * a.d_in + c);
                         d[0] = f32x4_t{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
                         d[1] = f32x4_t{acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
                     }
@@ -701,15 +851,15 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int split, 
     }
 }
 
-// workgroups [0, nA) compute dA, the others dB
-template <int RT>
-__global__ __launch_bounds__(kAdBlock) void k_ad_outer(const AdArgs a, int nA, int split)
+// workgroups [0, nB) compute dB, the others dA
+template <int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * cdk::kWave) void k_ad_outer(const AdArgs a, int nB)
 {
-    __shared__ f32x4_t lds[2][cdk::kWave * 8];
-    if ((int)blockIdx.x < nA)
-        ad_outer<RT, false>(a, blockIdx.x, split, lds);
+    __shared__ f32x4_t lds[WAVES / 2 * 8 * cdk::kWave];
+    if ((int)blockIdx.x < nB)
+        ad_outer<RT, WAVES, true>(a, blockIdx.x, lds);
     else
-        ad_outer<RT, true>(a, blockIdx.x - nA, split, lds);
+        ad_outer<RT, WAVES, false>(a, blockIdx.x - nB, lds);
 }
 
 __global__ __launch_bounds__(kAdBlock) void k_ad_zero(float *p, size_t n)
@@ -758,7 +908,6 @@ struct cd_adapters {
     AdGroup *groups;
     AdTile *tiles;
     uint16_t *Bt, *latT, *glatT;
-    int positions;
 };
 
 namespace {
@@ -834,7 +983,6 @@ AdArgs ad_args(const cd_adapters *p, const uint16_t *x, size_t ldx, int T, const
         a.order = p->order;
         a.groups = p->groups;
         a.tiles = p->tiles;
-        a.positions = p->positions;
         a.tile = ad_tile(T);
     }
     return a;
@@ -858,10 +1006,9 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
     const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
     const int m = std::min(mt, rt == 4 ? 2 : 4);  // sums of a workgroup: one per thread
     const dim3 grid(slots * (mt / m), ad_ceil(a.rank, rt * 16), kinds == 3 ? 2 : 1);
-    const int first = kinds == 2;
 #define AD_SHRINK(M, R) \
     if (m == M && rt == R) \
-        k_ad_shrink<M, R><<<grid, kAdShrinkBlock, 0, s>>>(a, first)
+        k_ad_shrink<M, R><<<grid, kAdShrinkBlock, 0, s>>>(a, kinds)
     AD_SHRINK(1, 1);
     AD_SHRINK(2, 1);
     AD_SHRINK(4, 1);
@@ -873,10 +1020,10 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
 #undef AD_SHRINK
 }
 
-// Workgroups along the outputs, `step` columns a wave, so that the grid has about 2048 of them.
-unsigned ad_columns(int width, int step, int tiles)
+// Workgroups along the outputs, 128 columns a wave, so that the grid has about 2048 of them.
+unsigned ad_columns(int width, int tiles)
 {
-    const int most = ad_ceil(width, step * kAdWaves);
+    const int most = ad_ceil(width, 128 * kAdWaves);
     return (unsigned)std::max(1, std::min(most, ad_ceil(2048, tiles)));
 }
 
@@ -887,13 +1034,15 @@ void ad_expand(const AdArgs &a, bool back, hipStream_t s)
     const int kc = a.rank <= 32 ? 1 : a.rank <= 64 ? 2 : a.rank <= 128 ? 4 : 8;
     const int m = std::min(mt, kc <= 2 ? 2 : 1);
     const int tiles = slots * (mt / m);
-    const dim3 grid(tiles, back ? ad_columns(a.d_in, 128, tiles) : ad_columns(a.d_out, 64, tiles));
+    const dim3 grid(tiles, ad_columns(back ? a.d_in : a.d_out, tiles));
 #define AD_EXPAND(M, K) \
     if (m == M && kc == K) { \
         if (back) \
             k_ad_dx<M, K><<<grid, kAdBlock, 0, s>>>(a); \
+        else if (a.type == CD_TYPE_F32) \
+            k_ad_expand<M, K, true><<<grid, kAdBlock, 0, s>>>(a); \
         else \
-            k_ad_expand<M, K><<<grid, kAdBlock, 0, s>>>(a); \
+            k_ad_expand<M, K, false><<<grid, kAdBlock, 0, s>>>(a); \
     }
     AD_EXPAND(1, 1)
     AD_EXPAND(2, 1)
@@ -904,22 +1053,25 @@ void ad_expand(const AdArgs &a, bool back, hipStream_t s)
 #undef AD_EXPAND
 }
 
-// dA and dB: with few column tiles the waves of a workgroup share one
+// dA and dB: with few workgroups, more waves in each
 void ad_grads(const AdArgs &a, hipStream_t s)
 {
-    const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
+    const int cols = (a.dA ? ad_ceil(a.d_in, 128) : 0) + (a.dB ? ad_ceil(a.d_out, 128) : 0);
+    const int groups = a.n * cols * ad_ceil(a.rank, 64);
+    const int waves = groups >= 512 ? 4 : 8;  // (64 ranks in each of eight waves do not fit the registers)
+    const int rt = a.rank <= 16 ? 1 : a.rank <= 32 || waves == 8 ? 2 : 4;
     const int rgs = ad_ceil(a.rank, rt * 16);
-    const int waves = a.n * rgs * ((a.dA ? ad_ceil(a.d_in, 128) : 0) + (a.dB ? ad_ceil(a.d_out, 128) : 0));
-    const int split = waves >= 1024 ? 1 : waves >= 512 ? 2 : 4;
-    const int cols = 128 * kAdWaves / split;
-    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, cols) : 0;
-    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, cols) : 0;
-    if (rt == 1)
-        k_ad_outer<1><<<nA + nB, kAdBlock, 0, s>>>(a, nA, split);
-    else if (rt == 2)
-        k_ad_outer<2><<<nA + nB, kAdBlock, 0, s>>>(a, nA, split);
-    else
-        k_ad_outer<4><<<nA + nB, kAdBlock, 0, s>>>(a, nA, split);
+    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 128) : 0;
+    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 128) : 0;
+#define AD_OUTER(R, W) \
+    if (rt == R && waves == W) \
+        k_ad_outer<R, W><<<nA + nB, W * cdk::kWave, 0, s>>>(a, nB)
+    AD_OUTER(1, 4);
+    AD_OUTER(1, 8);
+    AD_OUTER(2, 4);
+    AD_OUTER(2, 8);
+    AD_OUTER(4, 4);
+#undef AD_OUTER
 }
 
 }  // namespace
@@ -948,10 +1100,10 @@ cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapter
     p->max_tokens = max_tokens;
     p->flags = flags;
     p->device = dev;
-    p->positions = (max_tokens + kAdPad - 1) / kAdPad * kAdPad + kAdPad * (n_adapters + 1);
     const bool train = flags & CD_ADAPTERS_TRAIN;
-    const size_t pos = p->positions, lat = pos * rank * sizeof(float);
-    const size_t terms = 3 * pos * rank * sizeof(uint16_t);
+    const size_t pos = (size_t)(max_tokens + kAdPad - 1) / kAdPad * kAdPad + kAdPad * (n_adapters + 1);
+    const size_t lat = pos * rank * sizeof(float);
+    const size_t terms = 3 * pos * ((rank + 15) / 16 * 16) * sizeof(uint16_t);
     const size_t tiles = ((size_t)max_tokens / 16 + n_adapters + 1) * sizeof(AdTile);
     const size_t groups = (n_adapters + 1) * sizeof(AdGroup);
     const size_t copy = (size_t)n_adapters * rank * d_out * sizeof(uint16_t);
