@@ -8,6 +8,7 @@ missing.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 
@@ -118,10 +119,11 @@ _torch = None
 
 
 def _use_torch():
-    global _torch, _BF16, _F32, _raw_stream
+    global _torch, _BF16, _F32, _TYPES, _raw_stream
     import torch
 
     _BF16, _F32 = torch.bfloat16, torch.float32
+    _TYPES = {_F32: CD_TYPE_F32, _BF16: CD_TYPE_BF16}
     try:  # (device index) -> handle of its current stream
         raw, device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 
@@ -561,11 +563,10 @@ def _whole(t, shape, dtype, name, device):
 
 
 def _row_type(t, name) -> int:
-    if t.dtype is _F32:
-        return CD_TYPE_F32
-    if t.dtype is _BF16:
-        return CD_TYPE_BF16
-    raise TypeError(f"{name}: expected float32 or bfloat16, got {t.dtype}")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"{name}: expected float32 or bfloat16, got {t.dtype}")
+    return kind
 
 
 def _pool_args(pool: Adapters, x, ids, A, B, scale):
@@ -696,21 +697,22 @@ def countdown_clip_grads(clip: GradClip, grads, max_norm: float, out=None, norm=
     is computed). A norm that is not finite leaves the gradients as they are."""
     if clip.handle is None:
         raise ValueError("the workspace is closed")
-    if out is None:
-        out = grads
-    elif len(out) != len(grads):
+    if out is not None and len(out) != len(grads):
         raise ValueError(f"out must have as many tensors as grads ({len(grads)}), got {len(out)}")
-    dev, words = clip.device, []
-    for g, o in zip(grads, out):
+    dev, words = clip.device, []  # cd_grad: three 64-bit words, the type in a fourth
+    for i, g in enumerate(grads):
         if g.get_device() != dev or not g.is_contiguous():
             raise ValueError(f"gradients must be contiguous tensors on GPU {dev}")
-        p, n = g.data_ptr(), g.numel()
-        words += (p, p if o is g else _out_ptr(g, o, dev), n, _row_type(g, "gradient"))
+        p, t = g.data_ptr(), g.dtype
+        if t is not _F32 and t is not _BF16:
+            raise TypeError(f"gradients must be float32 or bfloat16, got {t}")
+        words += (p, p if out is None else _out_ptr(g, out[i], dev), g.numel(),
+                  CD_TYPE_F32 if t is _F32 else CD_TYPE_BF16)
+    words = array.array("Q", words)
     if norm is None:
         norm = _torch.empty(1, dtype=_torch.float64, device=f"cuda:{dev}")
-    table = (C.c_uint64 * len(words))(*words)  # cd_grad: three 64-bit words, the type in a fourth
     _check(load_library().countdown_clip_grads(
-        clip.handle, table, len(grads), float(max_norm),
+        clip.handle, words.buffer_info()[0], len(grads), float(max_norm),
         _whole(norm, (1,), _torch.float64, "norm", dev), _stream(stream)), "countdown_clip_grads")
     return norm
 

@@ -14,6 +14,11 @@ constexpr int kAdMaxDim = 65536, kAdMaxRank = 256, kAdMaxAdapters = 1024;
 constexpr int kAdMaxTokens = 1 << 20;
 constexpr int kAdDecodeTokens = 16;  // tokens of countdown_adapters_project
 constexpr int kAdDirectTokens = 32;  // up to here countdown_adapters_add goes token by token
+// Up to so many products a workgroup forms the latents that it needs by itself, in one launch:
+// project 4096 x 4096 at one token, rank 16 (2^16): 10.9 us a call against 12.6 with a launch of their own;
+// add to 8 tokens of 4096, rank 16 (2^16 a token): 9.9 against 12.7.
+constexpr int64_t kAdOwnProject = 1 << 17;
+constexpr int kAdOwnAdd = 1 << 18;
 constexpr int kAdBlock = 256, kAdWaves = kAdBlock / cdk::kWave;
 constexpr int kAdPad = 32;  // tokens of one adapter are padded to the contraction of an MFMA
 
@@ -59,6 +64,9 @@ struct AdArgs {
     uint16_t *latT, *glatT;  // lat and glat split in three bf16 terms (ad_term_at; training)
     int tile;  // tokens of a tile: 16, 32 or 64
 };
+
+// the wave's number, known to be uniform
+__device__ __forceinline__ int ad_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave); }
 
 __device__ __forceinline__ bool ad_valid(const AdArgs &a, int id) { return (unsigned)id < (unsigned)a.n; }
 __device__ __forceinline__ float ad_scale(const AdArgs &a, int id) { return a.scale ? a.scale[id] : 1.0f; }
@@ -115,8 +123,6 @@ __device__ __forceinline__ void ad_transpose8(const u32x4 (&r)[8], u32x4 (&c)[8]
 // over the banks.
 constexpr int kAdStage = 256;  // 16-byte chunks
 
-// the wave's number, known to be uniform
-__device__ __forceinline__ int ad_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave); }
 
 __device__ __forceinline__ void ad_wave_sync()
 {
@@ -173,24 +179,15 @@ __device__ __forceinline__ void ad_store8(const AdArgs &a, size_t t, int col, co
 
 // ---------------------------------------------------------------- decode: token by token
 
-// lat[t][k] = scale A x: one wave per (t, k)
-__global__ __launch_bounds__(kAdBlock) void k_ad_lat(const AdArgs a)
+// scale A x of rank k, over a wave
+__device__ __forceinline__ float ad_latent(const AdArgs &a, int t, int id, int k)
 {
-    const int w = blockIdx.x * kAdWaves + threadIdx.x / cdk::kWave;
-    const int t = w / a.rank, k = w % a.rank;
-    if (t >= a.T)
-        return;
-    const int id = a.ids[t];
-    if (!ad_valid(a, id))
-        return;
     const uint16_t *p = a.x + t * a.ldx, *q = a.A + ((size_t)id * a.rank + k) * a.d_in;
     float s = 0.0f;
 #pragma unroll 4
     for (int i = threadIdx.x % cdk::kWave * 8; i < a.d_in; i += cdk::kColsPerLoad)
         s = cdk::dot8(load16(p + i), load16(q + i), s);
-    s = cdk::wave_sum(s);
-    if (threadIdx.x % cdk::kWave == 0)
-        a.lat[w] = s * ad_scale(a, id);
+    return cdk::wave_sum(s) * ad_scale(a, id);
 }
 
 // sum over the rank of lat[k] B[a][o][k]
@@ -198,6 +195,7 @@ __device__ __forceinline__ float ad_row(const AdArgs &a, int id, int o, const fl
 {
     const uint16_t *b = a.B + ((size_t)id * a.d_out + o) * a.rank;
     float s = 0.0f;
+#pragma unroll 2
     for (int k = 0; k < a.rank; k += 8) {
         const u32x4 v = load16(b + k);
 #pragma unroll
@@ -207,6 +205,35 @@ __device__ __forceinline__ float ad_row(const AdArgs &a, int id, int o, const fl
     return s;
 }
 
+// out[t][o] = base + v (no: the token has no adapter, the base's bits)
+__device__ __forceinline__ void ad_store1(const AdArgs &a, int t, int o, float v, bool no)
+{
+    const size_t i = t * a.ldb + o;
+    if (a.type == CD_TYPE_F32) {
+        const float *b = static_cast<const float *>(a.base);
+        static_cast<float *>(a.out)[t * a.ldo + o] = b ? (no ? b[i] : b[i] + v) : v;
+    } else {
+        const uint16_t *b = static_cast<const uint16_t *>(a.base);
+        const uint16_t w = (uint16_t)ad_pack(b ? v + cdk::bf16_lo(b[i]) : v, 0.0f);
+        static_cast<uint16_t *>(a.out)[t * a.ldo + o] = b && no ? b[i] : w;
+    }
+}
+
+// lat[t][k]: one wave per (t, k)
+__global__ __launch_bounds__(kAdBlock) void k_ad_lat(const AdArgs a)
+{
+    const int w = blockIdx.x * kAdWaves + ad_wave();
+    const int t = w / a.rank, k = w % a.rank;
+    if (t >= a.T)
+        return;
+    const int id = a.ids[t];
+    if (!ad_valid(a, id))
+        return;
+    const float s = ad_latent(a, t, id, k);
+    if (threadIdx.x % cdk::kWave == 0)
+        a.lat[w] = s;
+}
+
 // y = base + B lat: one lane per output, blockIdx.y the token
 __global__ __launch_bounds__(kAdBlock) void k_ad_up(const AdArgs a)
 {
@@ -214,17 +241,28 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_up(const AdArgs a)
     if (o >= a.d_out)
         return;
     const bool no = !ad_valid(a, id);
-    float v = no ? 0.0f : ad_row(a, id, o, a.lat + t * a.rank);
-    if (a.type == CD_TYPE_F32) {
-        const float *b = static_cast<const float *>(a.base);
-        if (b)
-            v = no ? b[t * a.ldb + o] : v + b[t * a.ldb + o];
-        static_cast<float *>(a.out)[t * a.ldo + o] = v;
-    } else {
-        const uint16_t *b = static_cast<const uint16_t *>(a.base);
-        uint16_t w = __builtin_bit_cast(uint16_t, (__bf16)(b ? v + cdk::bf16_lo(b[t * a.ldb + o]) : v));
-        static_cast<uint16_t *>(a.out)[t * a.ldo + o] = no && b ? b[t * a.ldb + o] : w;
+    ad_store1(a, t, o, no ? 0.0f : ad_row(a, id, o, a.lat + t * a.rank), no);
+}
+
+// Both in one launch: every workgroup forms its token's latent again, one rank a wave at a time, for
+// 1024 outputs. A launch less is worth 3 us to the caller's thread and 2 us to the GPU.
+constexpr int kAdTokenBlock = 1024;
+
+__global__ __launch_bounds__(kAdTokenBlock) void k_ad_token(const AdArgs a)
+{
+    __shared__ float lat[kAdMaxRank];
+    const int t = blockIdx.y, o = blockIdx.x * kAdTokenBlock + threadIdx.x, id = a.ids[t];
+    const bool no = !ad_valid(a, id);  // uniform
+    if (!no) {
+        for (int k = ad_wave(); k < a.rank; k += kAdTokenBlock / cdk::kWave) {
+            const float s = ad_latent(a, t, id, k);
+            if (threadIdx.x % cdk::kWave == 0)
+                lat[k] = s;
+        }
+        __syncthreads();
     }
+    if (o < a.d_out)
+        ad_store1(a, t, o, no ? 0.0f : ad_row(a, id, o, lat), no);
 }
 
 // y = W x + B lat for up to 16 tokens: a workgroup's eight waves each take an eighth of the
@@ -233,13 +271,16 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_up(const AdArgs a)
 // last and tokens past T repeat the last one: they only reach sums of their own.
 constexpr int kAdProjBlock = 512, kAdProjWaves = kAdProjBlock / cdk::kWave;
 
+// OWN: every workgroup forms the latents again, while its first columns of W are on their way.
+template <bool OWN>
 __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
 {
     __shared__ u32x4 lds[kAdProjWaves][kAdStage];
+    __shared__ float own[OWN ? kAdDecodeTokens * kAdMaxRank : 1];
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
     const int o0 = blockIdx.x * 16;
-    const uint16_t *w[4], *x[4];
+    const uint16_t *w[4], *x[4];  // this lane's rows
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         w[i] = a.W + (size_t)min(o0 + 4 * i + g, a.d_out - 1) * a.d_in;
@@ -259,6 +300,13 @@ __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
     };
     f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
     load(0, wave * 128);
+    if constexpr (OWN)
+        for (int p = wave; p < a.T * a.rank; p += kAdProjWaves) {
+            const int t = p / a.rank, id = a.ids[t];
+            const float s = ad_valid(a, id) ? ad_latent(a, t, id, p % a.rank) : 0.0f;
+            if (lane == 0)
+                own[p] = s;
+        }
 #pragma unroll 1
     for (int kb = wave * 128; kb < a.d_in; kb += 2 * kStep) {
 #pragma unroll
@@ -290,11 +338,8 @@ __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
         v += sums[i * cdk::kWave + r / 4 * 16 + t][r % 4];
     const int id = a.ids[t];
     if (ad_valid(a, id))
-        v += ad_row(a, id, o, a.lat + t * a.rank);
-    if (a.type == CD_TYPE_F32)
-        static_cast<float *>(a.out)[t * a.ldo + o] = v;
-    else
-        static_cast<uint16_t *>(a.out)[t * a.ldo + o] = __builtin_bit_cast(uint16_t, (__bf16)v);
+        v += ad_row(a, id, o, (OWN ? own : a.lat) + t * a.rank);
+    ad_store1(a, t, o, v, false);
 }
 
 // ------------------------------------------------- many tokens: grouped by their adapters
@@ -340,9 +385,9 @@ __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
         return t >= t1 ? a.n + 1 : ad_valid(a, id) ? id : a.n;
     };
     int less = 0, mine = 0;
-    constexpr int kDeep = 8;  // loads in flight
+    constexpr int kDeep = 16;  // loads in flight
+    int of[kDeep];
     for (int t = t0; t < t1; t += kDeep * cdk::kWave) {
-        int of[kDeep];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u)
             of[u] = group_at(t + u * cdk::kWave + lane);
@@ -368,10 +413,10 @@ __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
     const int first = (less + kAdPad - 1) / kAdPad * kAdPad + kAdPad * grp;
     int at = first + before;
     for (int t = t0; t < t1; t += kDeep * cdk::kWave) {
-        int of[kDeep];
+        if (per > kDeep * cdk::kWave)  // (a single batch is still there)
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u)
-            of[u] = group_at(t + u * cdk::kWave + lane);
+            for (int u = 0; u < kDeep; ++u)
+                of[u] = group_at(t + u * cdk::kWave + lane);
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
             const uint64_t all = cdk::ballot(of[u] == grp);
@@ -405,7 +450,7 @@ __device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, i
 constexpr int kAdShrinkBlock = 512, kAdShrinkWaves = kAdShrinkBlock / cdk::kWave;
 
 template <int MT, int RT>
-__global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, int kinds)
+__global__ __launch_bounds__(kAdShrinkBlock, 2) void k_ad_shrink(const AdArgs a, int kinds)
 {
     static_assert(MT * RT * cdk::kWave <= kAdShrinkBlock, "one sum per thread");
     constexpr int kSums = MT * RT * cdk::kWave;
@@ -424,17 +469,17 @@ __global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, in
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
     const int r0 = blockIdx.y * RT * 16;
-    const uint16_t *xp[MT][4], *fp[RT][4];
+    int xr[MT][4], fr[RT][4];  // this lane's rows
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            xp[i][q] = src + a.order[tile.first + off + min(i * 16 + 4 * q + g, count - 1)] * ld;
+            xr[i][q] = a.order[tile.first + off + min(i * 16 + 4 * q + g, count - 1)];
 #pragma unroll
     for (int j = 0; j < RT; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            fp[j][q] = fac + (size_t)min(r0 + j * 16 + 4 * q + g, a.rank - 1) * K;
+            fr[j][q] = min(r0 + j * 16 + 4 * q + g, a.rank - 1) * K;
     u32x4 xv[kDepth][MT][4], fv[kDepth][RT][4];
     const auto load = [&](int s, int k) {
         k += 8 * m;
@@ -442,12 +487,12 @@ __global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, in
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                xv[s][i][q] = load16(or_zero(k < K, xp[i][q] + k));
+                xv[s][i][q] = load16(or_zero(k < K, src + (size_t)xr[i][q] * ld + k));
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                fv[s][j][q] = load16(or_zero(k < K, fp[j][q] + k));
+                fv[s][j][q] = load16(or_zero(k < K, fac + (unsigned)(fr[j][q] + k)));
     };
     f32x4_t acc[MT][RT];
 #pragma unroll
@@ -456,20 +501,26 @@ __global__ __launch_bounds__(kAdShrinkBlock) void k_ad_shrink(const AdArgs a, in
         for (int j = 0; j < RT; ++j)
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 *stage = lds + wave * kAdStage;
-    constexpr int kStep = 128 * kAdShrinkWaves;
-    if (kDepth == 2)
-        load(0, wave * 128);
+    // this wave's blocks of 128 columns
+    const int mine = ((K + 127) / 128 - wave + kAdShrinkWaves - 1) / kAdShrinkWaves;
+    int at_col = wave * 128;
+    const auto next = [&]() {
+        const int k = at_col;
+        at_col += 128 * kAdShrinkWaves;
+        return k;
+    };
+    if (kDepth == 2 && mine > 0)
+        load(0, next());
 #pragma unroll 1
-    for (int kb = wave * 128; kb < K; kb += kDepth * kStep) {
+    for (int it = 0; it < mine; it += kDepth) {
 #pragma unroll
         for (int s = 0; s < kDepth; ++s) {
-            const int k = kb + s * kStep;
-            if (k >= K)
+            if (it + s >= mine)
                 break;
             if (kDepth == 1)
-                load(0, k);
-            else if (k + kStep < K)
-                load(1 - s, k + kStep);
+                load(0, next());
+            else if (it + s + 1 < mine)
+                load(1 - s, next());
 #pragma unroll
             for (int j = 0; j < RT; ++j)
                 ad_stage(fv[s][j], stage, lane);
@@ -569,7 +620,7 @@ struct AdTokens {
 // bytes of a token's row and 16 neighbouring lanes with 256. B's rows pass through LDS:
 // 32 ranks of 128 outputs, read as they lie.
 template <int MT, int KC, bool F32>
-__global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
+__global__ __launch_bounds__(kAdBlock, KC == 1 ? 4 : KC == 2 ? 3 : 1) void k_ad_expand(const AdArgs a)
 {
     constexpr int kPad = F32 ? 4 : 8;  // a chunk more every so many rows: 16 columns on 16 banks
     __shared__ u32x4 lds[kAdWaves][128 * 4 + 128 / kPad];
@@ -680,7 +731,7 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_expand(const AdArgs a)
 // lane loads 8 ranks x 8 columns and transposes them in registers: steps of 128 columns,
 // column m of MFMA j is 8 m + j.
 template <int MT, int KC>
-__global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
+__global__ __launch_bounds__(kAdBlock, KC == 1 ? 3 : KC == 2 ? 2 : 1) void k_ad_dx(const AdArgs a)
 {
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
@@ -734,19 +785,25 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_dx(const AdArgs a)
     }
 }
 
-// dA = glat^T x and dB = dy^T lat of one adapter: 128 columns of x or dy and RT * 16 ranks a
-// workgroup. The contraction runs over the adapter's tokens, 32 at a time: a lane loads 8
-// tokens x 8 columns (the next 32 tokens' in flight) and transposes them. The waves take every
-// WAVES-th 32 tokens; their sums meet in LDS.
-template <int RT, int WAVES, bool DB>
+// dA = glat^T x and dB = dy^T lat of one adapter. The contraction runs over the adapter's
+// tokens, 32 at a time: a lane loads 8 tokens x 8 columns (the next 32 tokens' in flight) and
+// transposes them. A workgroup has 128 columns; its eight waves are WR parts of RT * 16 ranks
+// and the rest parts of the tokens, whose sums meet in LDS.
+constexpr int kAdGradWaves = 8;
+
+template <int RT, int WR, bool DB>
 __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *lds)
 {
+    constexpr int WT = kAdGradWaves / WR;
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
-    const int width = DB ? a.d_out : a.d_in, tiles = (width + 127) / 128;
-    const int rts = (a.rank + 15) / 16, rgs = (rts + RT - 1) / RT;
-    const int ad = block / (tiles * rgs), rt0 = block / tiles % rgs * RT;
-    const int c0 = block % tiles * 128, col = c0 + m * 8;
+    const int wt = wave / WR, part = wave % WR;  // tokens; ranks
+    const int width = DB ? a.d_out : a.d_in;
+    const int rts = (a.rank + 15) / 16, rgs = (rts + RT * WR - 1) / (RT * WR);
+    // eight neighbouring workgroups (one on each XCD) take neighbouring columns; then come the
+    // other adapters, of whose sizes nothing is known, and the other ranks
+    const int y = block / 8, ad = y % a.n, rt0 = (y / a.n % rgs * WR + part) * RT;
+    const int c0 = (y / a.n / rgs * 8 + block % 8) * 128, col = c0 + m * 8;
     const AdGroup grp = a.groups[ad];
     const uint16_t *src = DB ? a.dy : a.x;
     const size_t ld = DB ? a.lddy : a.ldx;
@@ -760,12 +817,18 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 rows[8], f[RT][3];
     // tokens past the group's end load zeros; ranks past the last repeat the last tile's
+    int4 ord[2];  // the lane's tokens of the next 32
+    const auto load_order = [&](int p) {
+        const int4 *o = reinterpret_cast<const int4 *>(a.order + grp.first + p + g * 8);
+        ord[0] = o[0];
+        ord[1] = o[1];
+    };
     const auto load_rows = [&](int p) {
-        const int *ord = a.order + grp.first + p + g * 8;
+        const int t[8] = {ord[0].x, ord[0].y, ord[0].z, ord[0].w, ord[1].x, ord[1].y, ord[1].z, ord[1].w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool ok = p + g * 8 + e < grp.count && cok;
-            rows[e] = load16(or_zero(ok, src + (ok ? (size_t)ord[e] * ld : 0) + col));
+            rows[e] = load16(or_zero(ok, src + (ok ? (size_t)t[e] * ld : 0) + col));
         }
     };
     const auto load_term = [&](int p, int s) {
@@ -773,16 +836,21 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
         for (int i = 0; i < RT; ++i)
             f[i][s] = load16(fac + (((size_t)(grp.first + p) / 32 * 3 + s) * rts + min(rt0 + i, rts - 1)) * 512 + lane * 8);
     };
-    int p = wave * 32;
+    int p = wt * 32;
     if (p < grp.count) {
+        load_order(p);
         load_rows(p);
+        if (p + WT * 32 < grp.count)
+            load_order(p + WT * 32);
 #pragma unroll
         for (int s = 2; s >= 0; --s)
             load_term(p, s);
     }
 #pragma unroll 1
-    for (; p < grp.count; p += WAVES * 32) {
-        const int next = p + WAVES * 32;
+    for (int p0 = 0; p0 < grp.count; p0 += WT * 32, p += WT * 32) {
+        if (p >= grp.count)
+            continue;
+        const int next = p + WT * 32;
         u32x4 cols[8];
         ad_transpose8(rows, cols);
         const int left = grp.count - p - g * 8;  // tokens from this lane's first
@@ -795,8 +863,11 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
                     for (int e = 0; e < 4; ++e)
                         f[i][s][e] &= (2 * e < left ? 0xffffu : 0u) | (2 * e + 1 < left ? 0xffff0000u : 0u);
         }
-        if (next < grp.count)
+        if (next < grp.count) {
             load_rows(next);
+            if (next + WT * 32 < grp.count)
+                load_order(next + WT * 32);
+        }
 #pragma unroll
         for (int s = 2; s >= 0; --s) {
 #pragma unroll
@@ -808,23 +879,24 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
                 load_term(next, s);
         }
     }
-    // the upper half of the waves hands its sums to the lower, until one has them all
+    // the upper half of the token parts hands its sums to the lower, until one has them all
 #pragma unroll
-    for (int half = WAVES / 2; half >= 1; half /= 2)
+    for (int half = WT / 2; half >= 1; half /= 2)
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
+            f32x4_t *at = lds + ((wt % half * WR + part) * 8) * cdk::kWave + lane;
             __syncthreads();
-            if (wave >= half && wave < 2 * half)
+            if (wt >= half && wt < 2 * half)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    lds[((wave - half) * 8 + j) * cdk::kWave + lane] = acc[i][j];
+                    at[j * cdk::kWave] = acc[i][j];
             __syncthreads();
-            if (wave < half)
+            if (wt < half)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    acc[i][j] += lds[(wave * 8 + j) * cdk::kWave + lane];
+                    acc[i][j] += at[j * cdk::kWave];
         }
-    if (wave)
+    if (wt)
         return;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
@@ -852,14 +924,14 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
 }
 
 // workgroups [0, nB) compute dB, the others dA
-template <int RT, int WAVES>
-__global__ __launch_bounds__(WAVES * cdk::kWave) void k_ad_outer(const AdArgs a, int nB)
+template <int RT, int WR>
+__global__ __launch_bounds__(kAdGradWaves * cdk::kWave, 2) void k_ad_outer(const AdArgs a, int nB)
 {
-    __shared__ f32x4_t lds[WAVES / 2 * 8 * cdk::kWave];
+    __shared__ f32x4_t lds[kAdGradWaves / 2 * 8 * cdk::kWave];
     if ((int)blockIdx.x < nB)
-        ad_outer<RT, WAVES, true>(a, blockIdx.x, lds);
+        ad_outer<RT, WR, true>(a, blockIdx.x, lds);
     else
-        ad_outer<RT, WAVES, false>(a, blockIdx.x - nB, lds);
+        ad_outer<RT, WR, false>(a, blockIdx.x - nB, lds);
 }
 
 __global__ __launch_bounds__(kAdBlock) void k_ad_zero(float *p, size_t n)
@@ -914,7 +986,7 @@ namespace {
 
 // Tokens of a tile. Small tiles spread a short batch over the CUs; large ones read the factors
 // less often.
-int ad_tile(int T) { return T < 8192 ? 16 : T < 16384 ? 32 : 64; }
+int ad_tile(int T) { return T < 8192 ? 16 : 32; }
 
 // the arguments that every call has; out_dim: the columns of base and out (0: neither)
 cd_status ad_check(const cd_adapters *p, const AdArgs &a, int out_dim)
@@ -1004,7 +1076,7 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
 {
     const int mt = a.tile / 16, slots = ad_slots(a);
     const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
-    const int m = std::min(mt, rt == 4 ? 2 : 4);  // sums of a workgroup: one per thread
+    const int m = std::min(mt, 2);  // sums of a workgroup: one per thread
     const dim3 grid(slots * (mt / m), ad_ceil(a.rank, rt * 16), kinds == 3 ? 2 : 1);
 #define AD_SHRINK(M, R) \
     if (m == M && rt == R) \
@@ -1032,7 +1104,7 @@ void ad_expand(const AdArgs &a, bool back, hipStream_t s)
 {
     const int mt = a.tile / 16, slots = ad_slots(a);
     const int kc = a.rank <= 32 ? 1 : a.rank <= 64 ? 2 : a.rank <= 128 ? 4 : 8;
-    const int m = std::min(mt, kc <= 2 ? 2 : 1);
+    const int m = 1;
     const int tiles = slots * (mt / m);
     const dim3 grid(tiles, ad_columns(back ? a.d_in : a.d_out, tiles));
 #define AD_EXPAND(M, K) \
@@ -1053,25 +1125,13 @@ void ad_expand(const AdArgs &a, bool back, hipStream_t s)
 #undef AD_EXPAND
 }
 
-// dA and dB: with few workgroups, more waves in each
+template <int RT, int WR>
 void ad_grads(const AdArgs &a, hipStream_t s)
 {
-    const int cols = (a.dA ? ad_ceil(a.d_in, 128) : 0) + (a.dB ? ad_ceil(a.d_out, 128) : 0);
-    const int groups = a.n * cols * ad_ceil(a.rank, 64);
-    const int waves = groups >= 512 ? 4 : 8;  // (64 ranks in each of eight waves do not fit the registers)
-    const int rt = a.rank <= 16 ? 1 : a.rank <= 32 || waves == 8 ? 2 : 4;
-    const int rgs = ad_ceil(a.rank, rt * 16);
-    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 128) : 0;
-    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 128) : 0;
-#define AD_OUTER(R, W) \
-    if (rt == R && waves == W) \
-        k_ad_outer<R, W><<<nA + nB, W * cdk::kWave, 0, s>>>(a, nB)
-    AD_OUTER(1, 4);
-    AD_OUTER(1, 8);
-    AD_OUTER(2, 4);
-    AD_OUTER(2, 8);
-    AD_OUTER(4, 4);
-#undef AD_OUTER
+    const int rgs = ad_ceil(a.rank, RT * WR * 16);
+    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 8 * 128) * 8 : 0;
+    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 8 * 128) * 8 : 0;
+    k_ad_outer<RT, WR><<<nA + nB, kAdGradWaves * cdk::kWave, 0, s>>>(a, nB);
 }
 
 }  // namespace
@@ -1168,8 +1228,12 @@ cd_status countdown_adapters_project(cd_adapters *p, const uint16_t *x, size_t l
     if (T == 0)
         return CD_OK;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-    k_ad_project<<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a);
+    if ((int64_t)T * a.rank * a.d_in <= kAdOwnProject) {
+        k_ad_project<true><<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a);
+    } else {
+        k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
+        k_ad_project<false><<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a);
+    }
     return launched(hipGetLastError());
 }
 
@@ -1187,7 +1251,9 @@ cd_status countdown_adapters_add(cd_adapters *p, const uint16_t *x, size_t ldx, 
     if (st != CD_OK || T == 0)
         return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (T <= kAdDirectTokens) {
+    if (T <= kAdDirectTokens && a.rank * a.d_in <= kAdOwnAdd) {
+        k_ad_token<<<dim3(ad_ceil(a.d_out, kAdTokenBlock), T), kAdTokenBlock, 0, s>>>(a);
+    } else if (T <= kAdDirectTokens) {
         k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
         k_ad_up<<<dim3(ad_ceil(a.d_out, kAdBlock), T), kAdBlock, 0, s>>>(a);
     } else {
@@ -1238,8 +1304,14 @@ cd_status countdown_adapters_backward(cd_adapters *p, const uint16_t *x, size_t 
     ad_shrink(a, (dB ? 1 : 0) + (back ? 2 : 0), s);
     if (dx)
         ad_expand(a, true, s);
-    if (dA || dB)
-        ad_grads(a, s);
+    if (dA || dB) {
+        if (a.rank <= 16)
+            ad_grads<1, 1>(a, s);
+        else if (a.rank <= 32)
+            ad_grads<2, 1>(a, s);
+        else
+            ad_grads<2, 2>(a, s);
+    }
     return launched(hipGetLastError());
 }
 

@@ -17,42 +17,49 @@
 
 namespace {
 
-constexpr int kClipTensors = 96;        // tensors per launch: the table is a kernel argument (2.8 KB)
+constexpr int kClipTensors = 96;        // tensors per launch: the table is a kernel argument (3 KB)
 constexpr unsigned kClipChunk = 16384;  // elements per step of a workgroup
 constexpr unsigned kClipGroups = 2048;  // workgroups per launch: 8 on each CU
+constexpr unsigned kClipScaleGroups = 768;  // where they also write: 2048 take 250 us for 671 MB, 1024 236, 768 231
 constexpr int kClipBlock = 256;
 
+struct ClipEntry {
+    const void *grad;
+    void *out;
+    uint64_t count;
+    uint32_t chunk0;  // its first chunk
+    uint32_t type;
+};
+
 struct ClipTable {
-    const void *grad[kClipTensors];
-    void *out[kClipTensors];
-    uint64_t count[kClipTensors];
-    uint32_t chunk0[kClipTensors + 1];  // first chunk of each tensor
-    uint8_t type[kClipTensors];
     int n;
+    unsigned chunk;   // elements of a chunk
+    uint64_t chunks;  // of all tensors
+    ClipEntry entry[kClipTensors];
 };
 
 struct ClipChunk {
-    int t;           // tensor
+    int t;           // entry
     uint64_t first;  // its first element
     unsigned n;      // elements
 };
 
-// the tensor and range of chunk c (uniform over the workgroup)
+// the tensor and range of chunk c
 __device__ __forceinline__ ClipChunk clip_chunk(const ClipTable &a, unsigned c)
 {
     int lo = 0, hi = a.n - 1;  // the last tensor whose first chunk is <= c
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (a.chunk0[mid] <= c)
+        if (a.entry[mid].chunk0 <= c)
             lo = mid;
         else
             hi = mid - 1;
     }
     ClipChunk r;
     r.t = lo;
-    r.first = (uint64_t)(c - a.chunk0[lo]) * kClipChunk;
-    const uint64_t left = a.count[lo] - r.first;
-    r.n = left < kClipChunk ? (unsigned)left : kClipChunk;
+    r.first = (uint64_t)(c - a.entry[lo].chunk0) * a.chunk;
+    const uint64_t left = a.entry[lo].count - r.first;
+    r.n = left < a.chunk ? (unsigned)left : a.chunk;
     return r;
 }
 
@@ -68,62 +75,73 @@ __device__ __forceinline__ double square(float v) { return (double)v * (double)v
 __device__ __forceinline__ float clip_value(float v) { return v; }
 __device__ __forceinline__ float clip_value(uint16_t v) { return cdk::bf16_lo(v); }
 template <class T>
-__device__ __forceinline__ double square16(const cdk::u32x4 &v)
+__device__ __forceinline__ void square16(const cdk::u32x4 &v, double (&s)[4])
 {
-    double s = 0.0;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        s += sizeof(T) == 4 ? square(__uint_as_float(v[i]))
-                            : square(cdk::bf16_lo(v[i])) + square(cdk::bf16_hi(v[i]));
-    return s;
+        if constexpr (sizeof(T) == 4) {
+            s[i] += square(__uint_as_float(v[i]));
+        } else {  //
+            s[i] += square(cdk::bf16_lo(v[i]));
+            s[i] += square(cdk::bf16_hi(v[i]));
+        }
 }
 
-template <class T>
-__device__ __forceinline__ double clip_squares(const T *p, unsigned n)
+// (thread `at` of BLOCK, here and below)
+template <int BLOCK, class T>
+__device__ __forceinline__ double clip_squares(const T *p, unsigned n, unsigned at)
 {
     constexpr unsigned kVec = 16 / sizeof(T);
     const unsigned lead = clip_lead(p, n), vecs = (n - lead) / kVec, done = lead + vecs * kVec;
     const cdk::u32x4 *v = reinterpret_cast<const cdk::u32x4 *>(p + lead);
-    double s = 0.0;
-    if (threadIdx.x < lead)
-        s += square(clip_value(p[threadIdx.x]));
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    if (at < lead)
+        s[0] += square(clip_value(p[at]));
 #pragma unroll 8
-    for (unsigned i = threadIdx.x; i < vecs; i += kClipBlock)
-        s += square16<T>(v[i]);
-    if (threadIdx.x < n - done)
-        s += square(clip_value(p[done + threadIdx.x]));
-    return s;
+    for (unsigned i = at; i < vecs; i += BLOCK)
+        square16<T>(v[i], s);
+    if (at < n - done)
+        s[1] += square(clip_value(p[done + at]));
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// sum over the workgroup, in thread 0
+// sum over the workgroup, in every thread (butterflies: the same bits everywhere)
+template <int BLOCK>
 __device__ __forceinline__ double clip_block_sum(double s)
 {
-    __shared__ double waves[kClipBlock / cdk::kWave];
+    constexpr int kWaves = BLOCK / cdk::kWave;
+    __shared__ double waves[kWaves];
 #pragma unroll
     for (int d = 1; d < cdk::kWave; d *= 2)
         s += __shfl_xor(s, d);
-    __syncthreads();
     if (threadIdx.x % cdk::kWave == 0)
         waves[threadIdx.x / cdk::kWave] = s;
     __syncthreads();
-    s = 0.0;
-    if (threadIdx.x == 0)
-        for (int w = 0; w < kClipBlock / cdk::kWave; ++w)
-            s += waves[w];
+    s = waves[threadIdx.x % kWaves];
+#pragma unroll
+    for (int d = 1; d < kWaves; d *= 2)
+        s += __shfl_xor(s, d);
     return s;
 }
 
-// sums of squares by workgroup
-__global__ __launch_bounds__(kClipBlock) void k_clip_norm(const ClipTable a, double *part)
+// sum of squares of every step-th chunk from `first` on, over BLOCK threads' own parts
+template <int BLOCK>
+__device__ __forceinline__ double clip_sum(const ClipTable &a, unsigned first, unsigned step, unsigned at)
 {
     double s = 0.0;
-    for (unsigned c = blockIdx.x; c < a.chunk0[a.n]; c += gridDim.x) {
+    for (unsigned c = first; c < a.chunks; c += step) {
         const ClipChunk k = clip_chunk(a, c);
-        s += a.type[k.t] == CD_TYPE_F32
-                 ? clip_squares(static_cast<const float *>(a.grad[k.t]) + k.first, k.n)
-                 : clip_squares(static_cast<const uint16_t *>(a.grad[k.t]) + k.first, k.n);
+        const void *grad = a.entry[k.t].grad;
+        s += a.entry[k.t].type == CD_TYPE_F32
+                 ? clip_squares<BLOCK>(static_cast<const float *>(grad) + k.first, k.n, at)
+                 : clip_squares<BLOCK>(static_cast<const uint16_t *>(grad) + k.first, k.n, at);
     }
-    s = clip_block_sum(s);
+    return s;
+}
+
+__global__ __launch_bounds__(kClipBlock) void k_clip_norm(const ClipTable a, double *part)
+{
+    const double s = clip_block_sum<kClipBlock>(clip_sum<kClipBlock>(a, blockIdx.x, gridDim.x, threadIdx.x));
     if (threadIdx.x == 0)
         part[blockIdx.x] = s;
 }
@@ -133,15 +151,10 @@ __global__ __launch_bounds__(kClipBlock) void k_clip_norm(const ClipTable a, dou
 // makes every other flush its L2 first (2032 of them: 70 us for 67 MB of gradients).
 __device__ __forceinline__ double clip_total(const double *part, unsigned parts)
 {
-    __shared__ double total;
     double s = 0.0;
     for (unsigned i = threadIdx.x; i < parts; i += kClipBlock)
         s += part[i];
-    s = clip_block_sum(s);
-    if (threadIdx.x == 0)
-        total = sqrt(s);
-    __syncthreads();
-    return total;
+    return sqrt(clip_block_sum<kClipBlock>(s));
 }
 
 __global__ __launch_bounds__(kClipBlock) void k_clip_total(const double *part, unsigned parts,
@@ -150,6 +163,12 @@ __global__ __launch_bounds__(kClipBlock) void k_clip_total(const double *part, u
     const double norm = clip_total(part, parts);
     if (threadIdx.x == 0)
         *norm_out = norm;
+}
+
+// a norm that is not finite scales nothing
+__device__ __forceinline__ float clip_coef(double norm, double max_norm)
+{
+    return norm > max_norm && norm < (double)INFINITY ? (float)(max_norm / norm) : 1.0f;
 }
 
 __device__ __forceinline__ uint32_t bf16_bits(float v)
@@ -171,27 +190,47 @@ __device__ __forceinline__ cdk::u32x4 scale16(cdk::u32x4 v, float coef)
 }
 
 // coef 1 copies the bits (a NaN's among them)
-template <class T>
-__device__ __forceinline__ void clip_scale(const T *p, T *o, unsigned n, float coef)
+template <int BLOCK, class T>
+__device__ __forceinline__ void clip_scale(const T *p, T *o, unsigned n, float coef, unsigned at)
 {
     constexpr unsigned kVec = 16 / sizeof(T);
     const bool same = coef == 1.0f;
     if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
-        for (unsigned i = threadIdx.x; i < n; i += kClipBlock)
+        for (unsigned i = at; i < n; i += BLOCK)
             o[i] = same ? p[i] : clip_round(clip_value(p[i]) * coef, T{});
         return;
     }
     const unsigned lead = clip_lead(p, n), vecs = (n - lead) / kVec, done = lead + vecs * kVec;
     const cdk::u32x4 *v = reinterpret_cast<const cdk::u32x4 *>(p + lead);
     cdk::u32x4 *w = reinterpret_cast<cdk::u32x4 *>(o + lead);
-    if (threadIdx.x < lead)
-        o[threadIdx.x] = same ? p[threadIdx.x] : clip_round(clip_value(p[threadIdx.x]) * coef, T{});
+    if (at < lead)
+        o[at] = same ? p[at] : clip_round(clip_value(p[at]) * coef, T{});
 #pragma unroll 8
-    for (unsigned i = threadIdx.x; i < vecs; i += kClipBlock)
+    for (unsigned i = at; i < vecs; i += BLOCK)
         w[i] = same ? v[i] : scale16<T>(v[i], coef);
-    if (threadIdx.x < n - done)
-        o[done + threadIdx.x] =
-            same ? p[done + threadIdx.x] : clip_round(clip_value(p[done + threadIdx.x]) * coef, T{});
+    if (at < n - done)
+        o[done + at] =
+            same ? p[done + at] : clip_round(clip_value(p[done + at]) * coef, T{});
+}
+
+template <int BLOCK>
+__device__ __forceinline__ void clip_scale_all(const ClipTable &a, float coef, unsigned first,
+                                               unsigned step, unsigned at)
+{
+    for (unsigned c = first; c < a.chunks; c += step) {
+        // the last chunks first: the norm read them last, they may still be in the last cache
+        const ClipChunk k = clip_chunk(a, (unsigned)a.chunks - 1 - c);
+        const void *grad = a.entry[k.t].grad;
+        void *out = a.entry[k.t].out;
+        if (!out || (coef == 1.0f && out == grad))
+            continue;
+        if (a.entry[k.t].type == CD_TYPE_F32)
+            clip_scale<BLOCK>(static_cast<const float *>(grad) + k.first,
+                              static_cast<float *>(out) + k.first, k.n, coef, at);
+        else
+            clip_scale<BLOCK>(static_cast<const uint16_t *>(grad) + k.first,
+                              static_cast<uint16_t *>(out) + k.first, k.n, coef, at);
+    }
 }
 
 __global__ __launch_bounds__(kClipBlock) void k_clip_scale(const ClipTable a, const double *part,
@@ -201,20 +240,25 @@ __global__ __launch_bounds__(kClipBlock) void k_clip_scale(const ClipTable a, co
     const double norm = clip_total(part, parts);
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0)
         *norm_out = norm;
-    // a norm that is not finite scales nothing
-    const float coef =
-        norm > max_norm && norm < (double)INFINITY ? (float)(max_norm / norm) : 1.0f;
-    for (unsigned c = blockIdx.x; c < a.chunk0[a.n]; c += gridDim.x) {
-        const ClipChunk k = clip_chunk(a, c);
-        if (!a.out[k.t] || (coef == 1.0f && a.out[k.t] == a.grad[k.t]))
-            continue;
-        if (a.type[k.t] == CD_TYPE_F32)
-            clip_scale(static_cast<const float *>(a.grad[k.t]) + k.first,
-                       static_cast<float *>(a.out[k.t]) + k.first, k.n, coef);
-        else
-            clip_scale(static_cast<const uint16_t *>(a.grad[k.t]) + k.first,
-                       static_cast<uint16_t *>(a.out[k.t]) + k.first, k.n, coef);
-    }
+    clip_scale_all<kClipBlock>(a, clip_coef(norm, max_norm), blockIdx.x, gridDim.x, threadIdx.x);
+}
+
+// Few elements: one workgroup does it all in one launch, each of its waves on chunks of its
+// own (a smaller chunk, so that every wave has one)
+constexpr int kClipOneBlock = 1024;
+constexpr unsigned kClipOneChunk = 4096, kClipOneChunks = 32;
+
+__global__ __launch_bounds__(kClipOneBlock) void k_clip_one(const ClipTable a, double max_norm,
+                                                            double *norm_out)
+{
+    constexpr int kWaves = kClipOneBlock / cdk::kWave;
+    const unsigned lane = threadIdx.x % cdk::kWave;
+    const unsigned wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave);
+    const double s = clip_sum<cdk::kWave>(a, wave, kWaves, lane);
+    const double norm = sqrt(clip_block_sum<kClipOneBlock>(s));
+    if (norm_out && threadIdx.x == 0)
+        *norm_out = norm;
+    clip_scale_all<cdk::kWave>(a, clip_coef(norm, max_norm), wave, kWaves, lane);
 }
 
 size_t clip_size(int type) { return type == CD_TYPE_F32 ? sizeof(float) : sizeof(uint16_t); }
@@ -319,6 +363,7 @@ cd_status countdown_clip_grads(cd_clip *p, const cd_grad *grads, int n, double m
         return CD_EINVAL;
     const bool scaled = max_norm < (double)INFINITY;
     bool writes = false;
+    uint64_t elements = 0;
     for (int i = 0; i < n; ++i) {
         const cd_grad &g = grads[i];
         if (g.type != CD_TYPE_F32 && g.type != CD_TYPE_BF16)
@@ -331,6 +376,7 @@ cd_status countdown_clip_grads(cd_clip *p, const cd_grad *grads, int n, double m
             return CD_EINVAL;
         if (g.count > ((uint64_t)1 << 38))  // a launch's chunks are counted in 32 bits
             return CD_EUNSUPPORTED;
+        elements += g.count;
         writes |= g.out && (scaled || g.out != g.grad);
     }
     try {
@@ -345,27 +391,38 @@ cd_status countdown_clip_grads(cd_clip *p, const cd_grad *grads, int n, double m
     if (dev != p->device)
         return CD_EINVAL;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    // The norm of every launch's tensors, then the scaling; a launch's table holds the
-    // tensors that are not empty.
+    // the next tensors that are not empty, as many as a launch takes, in chunks of `chunk`
+    // elements; returns the number of chunks
+    const auto fill = [&](ClipTable &a, int &i, unsigned chunk) {
+        uint64_t chunks = 0;
+        a.n = 0;
+        a.chunk = chunk;
+        for (; i < n && a.n < kClipTensors; ++i) {
+            if (!grads[i].count)
+                continue;
+            a.entry[a.n++] = ClipEntry{grads[i].grad, grads[i].out, grads[i].count,
+                                       (uint32_t)chunks, (uint32_t)grads[i].type};
+            chunks += (grads[i].count + chunk - 1) / chunk;
+        }
+        a.chunks = chunks;
+        return chunks;
+    };
+    ClipTable a;
+    if (elements <= (uint64_t)kClipOneChunk * kClipOneChunks) {
+        int i = 0;
+        const uint64_t chunks = fill(a, i, kClipOneChunk);
+        if (i == n && chunks && chunks <= kClipOneChunks) {
+            k_clip_one<<<1, kClipOneBlock, 0, s>>>(a, max_norm, norm);
+            return launched(hipGetLastError());
+        }
+    }
+    // the norm of every launch's tensors, then the scaling
     unsigned parts = 0;
     for (int pass = 0; pass < (writes ? 2 : 1); ++pass) {
         int i = 0;
         do {
-            ClipTable a;
-            a.n = 0;
-            uint64_t chunks = 0;
-            for (; i < n && a.n < kClipTensors; ++i) {
-                if (!grads[i].count)
-                    continue;
-                a.grad[a.n] = grads[i].grad;
-                a.out[a.n] = grads[i].out;
-                a.count[a.n] = grads[i].count;
-                a.type[a.n] = (uint8_t)grads[i].type;
-                a.chunk0[a.n++] = (uint32_t)chunks;
-                chunks += (grads[i].count + kClipChunk - 1) / kClipChunk;
-            }
-            a.chunk0[a.n] = (uint32_t)chunks;
-            const unsigned grid = (unsigned)std::min<uint64_t>(chunks, kClipGroups);
+            const uint64_t chunks = fill(a, i, kClipChunk);
+            const unsigned grid = (unsigned)std::min<uint64_t>(chunks, pass ? kClipScaleGroups : kClipGroups);
             if (!grid)
                 continue;
             if (pass == 0) {

@@ -119,9 +119,11 @@ SHAPES = [  # T, d_in, d_out, rank, adapters, ids
     (16, 4096, 256, 8, 64, "mixed"),
     (16, 256, 688, 16, 3, "none"),
     (5, 2504, 1000, 32, 4, "mixed"),
+    (3, 4096, 1064, 72, 2, "mixed"),
 ]
 LONG = [
     (17, 256, 688, 16, 3, "mixed"),
+    (32, 4096, 72, 80, 3, "mixed"),
     (33, 72, 40, 8, 2, "mixed"),
     (64, 520, 264, 128, 4, "runs"),
     (65, 264, 520, 16, 1, "one"),

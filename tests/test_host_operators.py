@@ -203,14 +203,18 @@ def test_clip_launches(host, clip):
         return [k for k, _ in host.launches()]
 
     both, norm = ["k_clip_norm", "k_clip_scale"], ["k_clip_norm", "k_clip_total"]
-    assert kernels([(G0, G0, 1 << 20, 0), (G1, G1, 5, 1)], 1.0) == both
-    assert kernels([(G0, G0, 1 << 20, 0)], math.inf) == norm
-    assert kernels([(G0, O0, 1 << 20, 0)], math.inf) == both
-    assert kernels([(G0, 0, 1 << 20, 0)] * 2, math.inf) == norm  # the norm may count one twice
+    one, big = ["k_clip_one"], 1 << 20
+    assert kernels([(G0, G0, big, 0), (G1, G1, 5, 1)], 1.0) == both
+    assert kernels([(G0, G0, big, 0)], math.inf) == norm
+    assert kernels([(G0, O0, big, 0)], math.inf) == both
+    assert kernels([(G0, 0, big, 0)] * 2, math.inf) == norm  # the norm may count one twice
     assert kernels([], 1.0) == kernels([(0, 0, 0, 0)] * 200, 1.0) == ["k_clip_total"]
     many = [(G0 + 4096 * i, G0 + 4096 * i, 1024, 0) for i in range(200)]
     assert kernels(many, 1.0) == ["k_clip_norm"] * 3 + ["k_clip_scale"] * 3
-    assert kernels([(G0, O0, 8, 0)], 1.0, norm=None) == both
+    assert kernels(many[:33], 1.0) == both and kernels(many[:32], 1.0) == one
+    assert kernels([(G0, 0, 8, 0)], math.inf) == one
+    assert kernels([(G0, O0, big, 0)], 1.0, norm=None) == both
+    assert kernels([(G0, O0, 8, 0)], 1.0, norm=None) == one
     assert clip_call(host, clip, [(G0, O0, (1 << 38) + 1, 0)], 1.0) == host.cd.CD_EUNSUPPORTED
     assert host.lib.countdown_clip_grads(clip, None, 1, 1.0, None, None) == host.cd.CD_EINVAL
     assert host.lib.countdown_clip_grads(None, None, 0, 1.0, None, None) == host.cd.CD_EINVAL
