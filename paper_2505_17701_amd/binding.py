@@ -691,8 +691,8 @@ def countdown_clip_destroy(clip: GradClip) -> None:
 
 
 def countdown_clip_grads(clip: GradClip, grads, max_norm: float, out=None, norm=None, stream=None):
-    """The global norm of a list of fp32 / bf16 gradients, as a new fp64 device tensor [1] (or
-    into ``norm``), and the gradients scaled by min(1, max_norm / norm): in place, or into the
+    """The global norm of a list of fp32 / bf16 gradients, as a new 0-dim fp64 device tensor (or
+    into ``norm``, one fp64 element), and the gradients scaled by min(1, max_norm / norm): in place, or into the
     tensors of the list ``out``. ``max_norm`` inf scales nothing (without ``out`` only the norm
     is computed). A norm that is not finite leaves the gradients as they are."""
     if clip.handle is None:
@@ -710,10 +710,12 @@ def countdown_clip_grads(clip: GradClip, grads, max_norm: float, out=None, norm=
                   CD_TYPE_F32 if t is _F32 else CD_TYPE_BF16)
     words = array.array("Q", words)
     if norm is None:
-        norm = _torch.empty(1, dtype=_torch.float64, device=f"cuda:{dev}")
+        norm = _torch.empty((), dtype=_torch.float64, device=f"cuda:{dev}")
+    elif norm.numel() != 1 or norm.dtype is not _torch.float64 or norm.get_device() != dev:
+        raise ValueError(f"norm must be one float64 element on GPU {dev}")
     _check(load_library().countdown_clip_grads(
-        clip.handle, words.buffer_info()[0], len(grads), float(max_norm),
-        _whole(norm, (1,), _torch.float64, "norm", dev), _stream(stream)), "countdown_clip_grads")
+        clip.handle, words.buffer_info()[0], len(grads), float(max_norm), norm.data_ptr(),
+        _stream(stream)), "countdown_clip_grads")
     return norm
 
 

@@ -20,6 +20,7 @@ constexpr int kAdDirectTokens = 32;  // up to here countdown_adapters_add goes t
 constexpr int64_t kAdOwnProject = 1 << 17;
 constexpr int kAdOwnAdd = 1 << 18;
 constexpr int kAdBlock = 256, kAdWaves = kAdBlock / cdk::kWave;
+constexpr size_t kAdPartFloats = (size_t)128 * 1024 * 32;  // place for workgroups' sums (16 MiB)
 constexpr int kAdPad = 32;  // tokens of one adapter are padded to the contraction of an MFMA
 
 using cdk::f32x4_t;
@@ -62,7 +63,8 @@ struct AdArgs {
     AdTile *tiles;
     uint16_t *Bt;            // [n][rank][d_out], B transposed (training)
     uint16_t *latT, *glatT;  // lat and glat split in three bf16 terms (ad_term_at; training)
-    int tile;  // tokens of a tile: 16, 32 or 64
+    int tile;    // tokens of a tile: 16 or 32
+    float *part; // sums of workgroups that share a gradient's tokens (training)
 };
 
 // the wave's number, known to be uniform
@@ -354,22 +356,30 @@ constexpr int kAdSortBlock = 1024, kAdSortWaves = kAdSortBlock / cdk::kWave;
 __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
 {
     if ((int)blockIdx.x > a.n) {
-        // 64 outputs x 64 ranks
-        __shared__ uint16_t tile[64][66];
-        const int ct = (a.d_out + 63) / 64, rt = (a.rank + 63) / 64;
+        // 128 outputs x 64 ranks, 8 ranks or 8 outputs a thread
+        __shared__ uint16_t tile[128][66];
+        const int ct = (a.d_out + 127) / 128, rt = (a.rank + 63) / 64;
         const int i = blockIdx.x - a.n - 1;
-        const int c0 = i % ct * 64, r0 = i / ct % rt * 64, ad = i / ct / rt;
+        const int c0 = i % ct * 128, r0 = i / ct % rt * 64, ad = i / ct / rt;
         const uint16_t *src = a.B + (size_t)ad * a.d_out * a.rank;
         uint16_t *dst = a.Bt + (size_t)ad * a.d_out * a.rank;
-        for (int e = threadIdx.x; e < 64 * 64; e += kAdSortBlock) {
-            const int o = c0 + e / 64, k = r0 + e % 64;
-            tile[e / 64][e % 64] = o < a.d_out && k < a.rank ? src[(size_t)o * a.rank + k] : 0;
+        {
+            const int o = threadIdx.x / 8, k = threadIdx.x % 8 * 8;
+            if (c0 + o < a.d_out && r0 + k < a.rank) {
+                const u32x4 v = load16(src + (size_t)(c0 + o) * a.rank + r0 + k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<uint32_t *>(&tile[o][k + 2 * e]) = v[e];
+            }
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < 64 * 64; e += kAdSortBlock) {
-            const int o = c0 + e % 64, k = r0 + e / 64;
-            if (o < a.d_out && k < a.rank)
-                dst[(size_t)k * a.d_out + o] = tile[e % 64][e / 64];
+        const int o = threadIdx.x % 16 * 8, k = threadIdx.x / 16;
+        if (c0 + o < a.d_out && r0 + k < a.rank) {
+            u32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = tile[o + 2 * e][k] | (uint32_t)tile[o + 2 * e + 1][k] << 16;
+            *reinterpret_cast<u32x4 *>(dst + (size_t)(r0 + k) * a.d_out + c0 + o) = v;
         }
         return;
     }
@@ -381,7 +391,7 @@ __global__ __launch_bounds__(kAdSortBlock) void k_ad_group(const AdArgs a)
     const int per = (a.T + kAdSortBlock - 1) / kAdSortBlock * cdk::kWave;
     const int t0 = min(a.T, wave * per), t1 = min(a.T, t0 + per);
     const auto group_at = [&](int t) {  // past the run: no group
-        const int id = t < t1 ? a.ids[t] : 0;
+        const int id = a.ids[min(t, a.T - 1)];
         return t >= t1 ? a.n + 1 : ad_valid(a, id) ? id : a.n;
     };
     int less = 0, mine = 0;
@@ -450,11 +460,11 @@ __device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, i
 constexpr int kAdShrinkBlock = 512, kAdShrinkWaves = kAdShrinkBlock / cdk::kWave;
 
 template <int MT, int RT>
-__global__ __launch_bounds__(kAdShrinkBlock, 2) void k_ad_shrink(const AdArgs a, int kinds)
+__global__ __launch_bounds__(kAdShrinkBlock, MT + RT <= 4 ? 4 : 2) void k_ad_shrink(const AdArgs a, int kinds)
 {
     static_assert(MT * RT * cdk::kWave <= kAdShrinkBlock, "one sum per thread");
     constexpr int kSums = MT * RT * cdk::kWave;
-    constexpr int kDepth = MT + RT <= 3 ? 2 : 1;  // blocks in flight
+    constexpr int kDepth = MT + RT <= 2 ? 2 : 1;  // blocks in flight
     __shared__ u32x4 lds[kAdShrinkWaves * (kSums > kAdStage ? kSums : kAdStage)];
     const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
     const AdTile tile = a.tiles[blockIdx.x / sub];
@@ -482,7 +492,7 @@ __global__ __launch_bounds__(kAdShrinkBlock, 2) void k_ad_shrink(const AdArgs a,
             fr[j][q] = min(r0 + j * 16 + 4 * q + g, a.rank - 1) * K;
     u32x4 xv[kDepth][MT][4], fv[kDepth][RT][4];
     const auto load = [&](int s, int k) {
-        k += 8 * m;
+        k += 8 * (m);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -501,26 +511,22 @@ __global__ __launch_bounds__(kAdShrinkBlock, 2) void k_ad_shrink(const AdArgs a,
         for (int j = 0; j < RT; ++j)
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 *stage = lds + wave * kAdStage;
-    // this wave's blocks of 128 columns
-    const int mine = ((K + 127) / 128 - wave + kAdShrinkWaves - 1) / kAdShrinkWaves;
-    int at_col = wave * 128;
-    const auto next = [&]() {
-        const int k = at_col;
-        at_col += 128 * kAdShrinkWaves;
-        return k;
-    };
-    if (kDepth == 2 && mine > 0)
-        load(0, next());
+    constexpr int kStep = 128 * kAdShrinkWaves;
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d)
+        if (wave * 128 + d * kStep < K)
+            load(d, wave * 128 + d * kStep);
 #pragma unroll 1
-    for (int it = 0; it < mine; it += kDepth) {
+    for (int kb = wave * 128; kb < K; kb += kDepth * kStep) {
 #pragma unroll
         for (int s = 0; s < kDepth; ++s) {
-            if (it + s >= mine)
+            const int k = kb + s * kStep;
+            if (k >= K)
                 break;
             if (kDepth == 1)
-                load(0, next());
-            else if (it + s + 1 < mine)
-                load(1 - s, next());
+                load(0, k);
+            else if (k + (kDepth - 1) * kStep < K)
+                load((s + kDepth - 1) % kDepth, k + (kDepth - 1) * kStep);
 #pragma unroll
             for (int j = 0; j < RT; ++j)
                 ad_stage(fv[s][j], stage, lane);
@@ -580,96 +586,97 @@ __device__ __forceinline__ void ad_operand(const AdArgs &a, const float *lat, bo
     ad_split8(v, t);
 }
 
-// A wave's tokens and their latents' terms: rows of the MFMA operands
-template <int MT, int KC>
+// A wave's 16 tokens and their latents' terms, the rows of its MFMAs: KC * 32 ranks, KC 0: any
+// number, fetched again (from L2) where they are used, since they would not fit the registers
+template <int KC>
 struct AdTokens {
-    int count;
+    int count, group;
     bool no;  // group n: no adapter
-    int group;
-    u32x4 lt[MT][KC][3];
-    int tok[MT][4];  // rows 4 g + q of the results
+    u32x4 lt[KC ? KC : 1][3];
+    int first, tok[4];  // rows 4 g + q of the results
 
-    __device__ __forceinline__ bool init(const AdArgs &a, const float *lat, int m, int g)
+    // part: of tile / 16 in each tile; false: nothing to do
+    __device__ __forceinline__ bool init(const AdArgs &a, const float *lat, int part, int m, int g)
     {
-        const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
-        const AdTile tile = a.tiles[blockIdx.x / sub];
-        const int off = blockIdx.x % sub * MT * 16;
-        count = tile.count - off;
+        const int sub = a.tile / 16;
+        const AdTile tile = a.tiles[part / sub];
+        first = tile.first + part % sub * 16;
+        count = tile.count - part % sub * 16;
         group = tile.group;
         no = group == a.n;
         if (count <= 0 || (no && a.base == a.out))
             return false;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
+        for (int q = 0; q < 4; ++q)
+            tok[q] = a.order[first + min(4 * g + q, count - 1)];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                tok[i][q] = a.order[tile.first + off + min(i * 16 + 4 * g + q, count - 1)];
-#pragma unroll
-            for (int c = 0; c < KC; ++c)
-                ad_operand(a, lat, i * 16 + m < count && !no, tile.first + off + i * 16 + m,
-                           c * 32 + g * 8, lt[i][c]);
-        }
+        for (int c = 0; c < KC; ++c)
+            fetch(a, lat, c, m, g);
         return true;
     }
-    __device__ __forceinline__ bool live(int i, int g, int q) const { return i * 16 + 4 * g + q < count; }
+    __device__ __forceinline__ void fetch(const AdArgs &a, const float *lat, int c, int m, int g)
+    {
+        ad_operand(a, lat, m < count && !no, first + m, c * 32 + g * 8, lt[KC ? c : 0]);
+    }
+    __device__ __forceinline__ bool live(int g, int q) const { return 4 * g + q < count; }
 };
 
-// y = base + B lat for a tile of MT * 16 tokens, KC * 32 ranks. Each wave takes steps of 128
-// outputs: eight MFMAs with the tokens as rows and B's rows as columns. Column m of MFMA
-// j is output 8 m + j (fp32: 4 m + j % 4 of the half j / 4), so that a lane ends with 16
-// bytes of a token's row and 16 neighbouring lanes with 256. B's rows pass through LDS:
-// 32 ranks of 128 outputs, read as they lie.
-template <int MT, int KC, bool F32>
-__global__ __launch_bounds__(kAdBlock, KC == 1 ? 4 : KC == 2 ? 3 : 1) void k_ad_expand(const AdArgs a)
+// y = base + B lat for 16 tokens, KC * 32 ranks. Each wave takes steps of 128 outputs: eight
+// MFMAs with the tokens as rows and B's rows as columns. Column m of MFMA j is output 8 m + j
+// (fp32: 4 m + j % 4 of the half j / 4), so that a lane ends with 16 bytes of a token's row
+// and 16 neighbouring lanes with 256. B's rows pass through LDS: 32 ranks of 128 outputs,
+// read as they lie. Bound by memory: 16384 tokens of 4096 bf16 outputs, 268 MB, in 58 us
+// (4.6 TB/s; a copy runs at 4.8). 32 tokens a wave read B half as often, but need the
+// registers of a second wave on the SIMD: 64 to 91 us.
+template <int KC, bool F32>
+__global__ __launch_bounds__(kAdBlock, KC == 1 && !F32 ? 4 : 3) void k_ad_expand(const AdArgs a)
 {
+    constexpr int kHalves = F32 ? 2 : 1;
     constexpr int kPad = F32 ? 4 : 8;  // a chunk more every so many rows: 16 columns on 16 banks
     __shared__ u32x4 lds[kAdWaves][128 * 4 + 128 / kPad];
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
-    AdTokens<MT, KC> tk;
-    if (!tk.init(a, a.lat, m, g))
+    AdTokens<KC> tk;
+    if (!tk.init(a, a.lat, blockIdx.x, m, g))
         return;
     const uint16_t *B = a.B + (tk.no ? 0 : (size_t)tk.group * a.d_out * a.rank);
     u32x4 *st = lds[wave];
 #pragma unroll 1
     for (int o0 = (blockIdx.y * kAdWaves + wave) * 128; o0 < a.d_out; o0 += gridDim.y * kAdWaves * 128) {
         // this lane's columns: cols(h) .. + 8 (fp32: 4)
-        u32x4 base[MT][4][F32 ? 2 : 1];
         const auto cols = [&](int h) { return F32 ? o0 + 64 * h + 4 * m : o0 + 8 * m; };
+        u32x4 base[4][kHalves];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int h = 0; h < kHalves; ++h) {
+                const bool ok = a.base && tk.live(g, q) && cols(h) < a.d_out;
+                const size_t at = (size_t)tk.tok[q] * a.ldb + cols(h);
+                base[q][h] =
+                    F32 ? *reinterpret_cast<const u32x4 *>(or_zero(ok, static_cast<const float *>(a.base) + at))
+                        : load16(or_zero(ok, static_cast<const uint16_t *>(a.base) + at));
+            }
+        f32x4_t acc[8];
 #pragma unroll
-                for (int h = 0; h < (F32 ? 2 : 1); ++h) {
-                    const bool ok = a.base && tk.live(i, g, q) && cols(h) < a.d_out;
-                    const size_t at = (size_t)tk.tok[i][q] * a.ldb + cols(h);
-                    base[i][q][h] =
-                        F32 ? *reinterpret_cast<const u32x4 *>(or_zero(ok, static_cast<const float *>(a.base) + at))
-                            : load16(or_zero(ok, static_cast<const uint16_t *>(a.base) + at));
-                }
-        f32x4_t acc[MT][8];
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < 8; ++j)
+            acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         if (!tk.no)
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                // chunk ch of row `row`; a row past the last repeats it (sums not stored)
-                const int nch = min(4, a.rank / 8 - 4 * c);  // uniform
+#pragma unroll KC ? KC : 1
+            for (int c = 0; c < (KC ? KC : (a.rank + 31) / 32); ++c) {
+                if (!KC)
+                    tk.fetch(a, a.lat, c, m, g);
+                const int nch = min(4, a.rank / 8 - 4 * c);  // chunks of a row; uniform
                 if (nch <= 0)
                     break;
-                u32x4 v[8];
                 const auto place = [&](int i, int &row, int &ch) {
                     const int e = i * cdk::kWave + lane;
                     row = nch == 4 ? e / 4 : nch == 2 ? e / 2 : nch == 1 ? e : e / 3;
                     ch = e - row * nch;
                 };
+                u32x4 v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < 2 * nch) {
+                    if (i < 2 * nch) {  // (a row past the last repeats it: sums not stored)
                         int row, ch;
                         place(i, row, ch);
                         v[i] = load16(B + (size_t)min(o0 + row, a.d_out - 1) * a.rank + (4 * c + ch) * 8);
@@ -691,73 +698,62 @@ __global__ __launch_bounds__(kAdBlock, KC == 1 ? 4 : KC == 2 ? 3 : 1) void k_ad_
                         b = cdk::zero16();
 #pragma unroll
                     for (int s = 2; s >= 0; --s)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i)
-                            acc[i][j] = mfma16(tk.lt[i][c][s], b, acc[i][j]);
+                        acc[j] = mfma16(tk.lt[KC ? c : 0][s], b, acc[j]);
                 }
             }
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (tk.live(i, g, q)) {
-                    if constexpr (F32) {
+            for (int h = 0; h < kHalves; ++h) {
+                if (!tk.live(g, q) || cols(h) >= a.d_out)
+                    continue;
+                u32x4 w = base[q][h];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            u32x4 w = base[i][q][h];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                w[e] = tk.no ? w[e] : __float_as_uint(__uint_as_float(w[e]) + acc[i][4 * h + e][q]);
-                            if (cols(h) < a.d_out)
-                                *reinterpret_cast<u32x4 *>(static_cast<float *>(a.out) +
-                                                           (size_t)tk.tok[i][q] * a.ldo + cols(h)) = w;
-                        }
-                    } else {
-                        u32x4 w = base[i][q][0];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = tk.no ? w[e]
-                                         : ad_pack(cdk::bf16_lo(w[e]) + acc[i][2 * e][q],
-                                                   cdk::bf16_hi(w[e]) + acc[i][2 * e + 1][q]);
-                        if (cols(0) < a.d_out)
-                            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) +
-                                                       (size_t)tk.tok[i][q] * a.ldo + cols(0)) = w;
-                    }
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (!tk.no)
+                        w[e] = F32 ? __float_as_uint(__uint_as_float(w[e]) + acc[4 * h + e][q])
+                                   : ad_pack(cdk::bf16_lo(w[e]) + acc[2 * e][q],
+                                             cdk::bf16_hi(w[e]) + acc[2 * e + 1][q]);
+                const size_t at = (size_t)tk.tok[q] * a.ldo + cols(h);
+                if constexpr (F32)
+                    *reinterpret_cast<u32x4 *>(static_cast<float *>(a.out) + at) = w;
+                else
+                    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + at) = w;
+            }
     }
 }
+
+constexpr int kAdBackWaves = 8;  // of the workgroups that compute the gradients
 
 // dx = base + A^T glat: as k_ad_expand, but the factor's rows run along the outputs, so a
 // lane loads 8 ranks x 8 columns and transposes them in registers: steps of 128 columns,
 // column m of MFMA j is 8 m + j.
-template <int MT, int KC>
-__global__ __launch_bounds__(kAdBlock, KC == 1 ? 3 : KC == 2 ? 2 : 1) void k_ad_dx(const AdArgs a)
+template <int KC>
+__device__ __forceinline__ void ad_dx(const AdArgs &a, int part, int slice, int slices)
 {
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
-    AdTokens<MT, KC> tk;
-    if (!tk.init(a, a.glat, m, g))
+    AdTokens<KC> tk;
+    if (!tk.init(a, a.glat, part, m, g))
         return;
     const uint16_t *A = a.A + (tk.no ? 0 : (size_t)tk.group * a.d_in * a.rank);
 #pragma unroll 1
-    for (int c0 = (blockIdx.y * kAdWaves + wave) * 128; c0 < a.d_in; c0 += gridDim.y * kAdWaves * 128) {
+    for (int c0 = (slice * kAdBackWaves + wave) * 128; c0 < a.d_in; c0 += slices * kAdBackWaves * 128) {
         const int col = c0 + 8 * m;
         const bool cok = col < a.d_in;
-        u32x4 base[MT][4][2];
+        u32x4 base[4][2];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int q = 0; q < 4; ++q)
+            ad_base8(a, tk.live(g, q) && cok, tk.tok[q], col, base[q]);
+        f32x4_t acc[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                ad_base8(a, tk.live(i, g, q) && cok, tk.tok[i][q], col, base[i][q]);
-        f32x4_t acc[MT][8];
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < 8; ++j)
+            acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         if (!tk.no)
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
+#pragma unroll KC ? KC : 1
+            for (int c = 0; c < (KC ? KC : (a.rank + 31) / 32); ++c) {
+                if (!KC)
+                    tk.fetch(a, a.glat, c, m, g);
                 u32x4 rows[8], cols[8];
                 const bool ok = c * 32 + g * 8 < a.rank && cok;
 #pragma unroll
@@ -768,41 +764,38 @@ __global__ __launch_bounds__(kAdBlock, KC == 1 ? 3 : KC == 2 ? 2 : 1) void k_ad_
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int s = 2; s >= 0; --s)
-#pragma unroll
-                        for (int i = 0; i < MT; ++i)
-                            acc[i][j] = mfma16(tk.lt[i][c][s], cols[j], acc[i][j]);
+                        acc[j] = mfma16(tk.lt[KC ? c : 0][s], cols[j], acc[j]);
             }
         if (cok)
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float v[8] = {acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q],
-                                        acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
-                    if (tk.live(i, g, q))
-                        ad_store8(a, tk.tok[i][q], col, base[i][q], v, tk.no);
-                }
+            for (int q = 0; q < 4; ++q) {
+                const float v[8] = {acc[0][q], acc[1][q], acc[2][q], acc[3][q],
+                                    acc[4][q], acc[5][q], acc[6][q], acc[7][q]};
+                if (tk.live(g, q))
+                    ad_store8(a, tk.tok[q], col, base[q], v, tk.no);
+            }
     }
 }
 
 // dA = glat^T x and dB = dy^T lat of one adapter. The contraction runs over the adapter's
 // tokens, 32 at a time: a lane loads 8 tokens x 8 columns (the next 32 tokens' in flight) and
 // transposes them. A workgroup has 128 columns; its eight waves are WR parts of RT * 16 ranks
-// and the rest parts of the tokens, whose sums meet in LDS.
-constexpr int kAdGradWaves = 8;
-
+// and the rest parts of the tokens, whose sums meet in LDS. Where that leaves CUs without a
+// workgroup, `parts` workgroups share the tokens as well, each with sums of its own in
+// a.part, and k_ad_sum adds them in order.
 template <int RT, int WR, bool DB>
-__device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *lds)
+__device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int parts, f32x4_t *lds)
 {
-    constexpr int WT = kAdGradWaves / WR;
+    constexpr int WT = kAdBackWaves / WR;
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
     const int wt = wave / WR, part = wave % WR;  // tokens; ranks
+    const int tokens = block / 8 % parts;        // of the workgroups that share them
     const int width = DB ? a.d_out : a.d_in;
     const int rts = (a.rank + 15) / 16, rgs = (rts + RT * WR - 1) / (RT * WR);
     // eight neighbouring workgroups (one on each XCD) take neighbouring columns; then come the
     // other adapters, of whose sizes nothing is known, and the other ranks
-    const int y = block / 8, ad = y % a.n, rt0 = (y / a.n % rgs * WR + part) * RT;
+    const int y = block / 8 / parts, ad = y % a.n, rt0 = (y / a.n % rgs * WR + part) * RT;
     const int c0 = (y / a.n / rgs * 8 + block % 8) * 128, col = c0 + m * 8;
     const AdGroup grp = a.groups[ad];
     const uint16_t *src = DB ? a.dy : a.x;
@@ -817,40 +810,41 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 rows[8], f[RT][3];
     // tokens past the group's end load zeros; ranks past the last repeat the last tile's
-    int4 ord[2];  // the lane's tokens of the next 32
+    const int next = parts * WT * 32;  // from one of this wave's 32 tokens to the next
+    int4 ord[2];  // the lane's tokens, of those loaded next
     const auto load_order = [&](int p) {
+        if (p >= grp.count)
+            return;
         const int4 *o = reinterpret_cast<const int4 *>(a.order + grp.first + p + g * 8);
         ord[0] = o[0];
         ord[1] = o[1];
     };
     const auto load_rows = [&](int p) {
+        if (p >= grp.count)
+            return;
         const int t[8] = {ord[0].x, ord[0].y, ord[0].z, ord[0].w, ord[1].x, ord[1].y, ord[1].z, ord[1].w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool ok = p + g * 8 + e < grp.count && cok;
             rows[e] = load16(or_zero(ok, src + (ok ? (size_t)t[e] * ld : 0) + col));
         }
+        load_order(p + next);
     };
     const auto load_term = [&](int p, int s) {
+        if (p >= grp.count)
+            return;
 #pragma unroll
         for (int i = 0; i < RT; ++i)
             f[i][s] = load16(fac + (((size_t)(grp.first + p) / 32 * 3 + s) * rts + min(rt0 + i, rts - 1)) * 512 + lane * 8);
     };
-    int p = wt * 32;
-    if (p < grp.count) {
-        load_order(p);
-        load_rows(p);
-        if (p + WT * 32 < grp.count)
-            load_order(p + WT * 32);
+    const int p0 = (tokens * WT + wt) * 32;
+    load_order(p0);
+    load_rows(p0);
 #pragma unroll
-        for (int s = 2; s >= 0; --s)
-            load_term(p, s);
-    }
+    for (int s = 2; s >= 0; --s)
+        load_term(p0, s);
 #pragma unroll 1
-    for (int p0 = 0; p0 < grp.count; p0 += WT * 32, p += WT * 32) {
-        if (p >= grp.count)
-            continue;
-        const int next = p + WT * 32;
+    for (int p = p0; p < grp.count; p += next) {
         u32x4 cols[8];
         ad_transpose8(rows, cols);
         const int left = grp.count - p - g * 8;  // tokens from this lane's first
@@ -863,11 +857,7 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
                     for (int e = 0; e < 4; ++e)
                         f[i][s][e] &= (2 * e < left ? 0xffffu : 0u) | (2 * e + 1 < left ? 0xffff0000u : 0u);
         }
-        if (next < grp.count) {
-            load_rows(next);
-            if (next + WT * 32 < grp.count)
-                load_order(next + WT * 32);
-        }
+        load_rows(p + next);
 #pragma unroll
         for (int s = 2; s >= 0; --s) {
 #pragma unroll
@@ -875,8 +865,7 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
 #pragma unroll
                 for (int i = 0; i < RT; ++i)
                     acc[i][j] = DB ? mfma16(f[i][s], cols[j], acc[i][j]) : mfma16(cols[j], f[i][s], acc[i][j]);
-            if (next < grp.count)
-                load_term(next, s);
+            load_term(p + next, s);
         }
     }
     // the upper half of the token parts hands its sums to the lower, until one has them all
@@ -898,6 +887,9 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
         }
     if (wt)
         return;
+    const size_t whole = (size_t)a.n * a.rank * width;
+    float *dst = parts > 1 ? a.part + (DB || !a.dB ? 0 : (size_t)parts * a.n * a.rank * a.d_out) + tokens * whole
+                           : DB ? a.dB : a.dA;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         if constexpr (DB) {  // row o = c0 + 8 m + j, ranks 4 g + q
@@ -905,7 +897,7 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
             if (cok && r < a.rank)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<f32x4_t *>(a.dB + ((size_t)ad * a.d_out + col + j) * a.rank + r) =
+                    *reinterpret_cast<f32x4_t *>(dst + ((size_t)ad * a.d_out + col + j) * a.rank + r) =
                         acc[i][j];
         } else {  // row r = m, columns c0 + 8 (4 g + q) + j
             const int r = (rt0 + i) * 16 + m;
@@ -914,7 +906,7 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
                 for (int q = 0; q < 4; ++q) {
                     const int c = c0 + 8 * (4 * g + q);
                     if (c < a.d_in) {
-                        f32x4_t *d = reinterpret_cast<f32x4_t *>(a.dA + ((size_t)ad * a.rank + r) * a.d_in + c);
+                        f32x4_t *d = reinterpret_cast<f32x4_t *>(dst + ((size_t)ad * a.rank + r) * a.d_in + c);
                         d[0] = f32x4_t{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
                         d[1] = f32x4_t{acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
                     }
@@ -923,15 +915,35 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, f32x4_t *ld
     }
 }
 
-// workgroups [0, nB) compute dB, the others dA
-template <int RT, int WR>
-__global__ __launch_bounds__(kAdGradWaves * cdk::kWave, 2) void k_ad_outer(const AdArgs a, int nB)
+// Workgroups [0, nB) compute dB, the next nA dA, the others dx (`slices` of its columns): one
+// launch for small calls' sake, and the kinds wait for different things.
+template <int RT, int WR, int KC>
+__global__ __launch_bounds__(kAdBackWaves * cdk::kWave, 2) void k_ad_back(const AdArgs a, int nB, int nA,
+                                                                      int parts, int slices)
 {
-    __shared__ f32x4_t lds[kAdGradWaves / 2 * 8 * cdk::kWave];
-    if ((int)blockIdx.x < nB)
-        ad_outer<RT, WR, true>(a, blockIdx.x, lds);
+    __shared__ f32x4_t lds[kAdBackWaves / 2 * 8 * cdk::kWave];
+    const int b = blockIdx.x;
+    if (b < nB)
+        ad_outer<RT, WR, true>(a, b, parts, lds);
+    else if (b < nB + nA)
+        ad_outer<RT, WR, false>(a, b - nB, parts, lds);
     else
-        ad_outer<RT, WR, false>(a, blockIdx.x - nB, lds);
+        ad_dx<KC>(a, (b - nB - nA) / slices, (b - nB - nA) % slices, slices);
+}
+
+// dB and dA (nb and na elements) from their parts
+__global__ __launch_bounds__(kAdBlock) void k_ad_sum(const float *part, int parts, float *dB, size_t nb,
+                                                     float *dA, size_t na)
+{
+    for (size_t i = ((size_t)blockIdx.x * kAdBlock + threadIdx.x) * 4; i < nb + na; i += (size_t)gridDim.x * kAdBlock * 4) {
+        const bool b = i < nb;
+        const float *p = b ? part + i : part + parts * nb + (i - nb);
+        f32x4_t v = *reinterpret_cast<const f32x4_t *>(p);
+#pragma unroll 4
+        for (int k = 1; k < parts; ++k)
+            v += *reinterpret_cast<const f32x4_t *>(p + k * (b ? nb : na));
+        *reinterpret_cast<f32x4_t *>(b ? dB + i : dA + (i - nb)) = v;
+    }
 }
 
 __global__ __launch_bounds__(kAdBlock) void k_ad_zero(float *p, size_t n)
@@ -980,6 +992,7 @@ struct cd_adapters {
     AdGroup *groups;
     AdTile *tiles;
     uint16_t *Bt, *latT, *glatT;
+    float *part;
 };
 
 namespace {
@@ -1067,7 +1080,7 @@ int ad_slots(const AdArgs &a) { return a.T / a.tile + a.n + 1; }
 
 void ad_group(const AdArgs &a, bool transpose, hipStream_t s)
 {
-    const int more = transpose ? a.n * ad_ceil(a.d_out, 64) * ad_ceil(a.rank, 64) : 0;
+    const int more = transpose ? a.n * ad_ceil(a.d_out, 128) * ad_ceil(a.rank, 64) : 0;
     k_ad_group<<<a.n + 1 + more, kAdSortBlock, 0, s>>>(a);
 }
 
@@ -1092,46 +1105,57 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
 #undef AD_SHRINK
 }
 
-// Workgroups along the outputs, 128 columns a wave, so that the grid has about 2048 of them.
-unsigned ad_columns(int width, int tiles)
+// Slices of the columns, 128 to each of `waves` waves, so that `parts` tiles make about 2048 workgroups.
+int ad_slices(int width, int waves, int parts)
 {
-    const int most = ad_ceil(width, 128 * kAdWaves);
-    return (unsigned)std::max(1, std::min(most, ad_ceil(2048, tiles)));
+    return std::max(1, std::min(ad_ceil(width, 128 * waves), ad_ceil(2048, parts)));
 }
 
-// y (back: dx) from the latents
-void ad_expand(const AdArgs &a, bool back, hipStream_t s)
+// y from the latents
+void ad_expand(const AdArgs &a, hipStream_t s)
 {
-    const int mt = a.tile / 16, slots = ad_slots(a);
-    const int kc = a.rank <= 32 ? 1 : a.rank <= 64 ? 2 : a.rank <= 128 ? 4 : 8;
-    const int m = 1;
-    const int tiles = slots * (mt / m);
-    const dim3 grid(tiles, ad_columns(back ? a.d_in : a.d_out, tiles));
-#define AD_EXPAND(M, K) \
-    if (m == M && kc == K) { \
-        if (back) \
-            k_ad_dx<M, K><<<grid, kAdBlock, 0, s>>>(a); \
-        else if (a.type == CD_TYPE_F32) \
-            k_ad_expand<M, K, true><<<grid, kAdBlock, 0, s>>>(a); \
-        else \
-            k_ad_expand<M, K, false><<<grid, kAdBlock, 0, s>>>(a); \
+    const int parts = ad_slots(a) * (a.tile / 16);
+    const dim3 grid(parts, ad_slices(a.d_out, kAdWaves, parts));
+#define AD_EXPAND(K) \
+    if (a.type == CD_TYPE_F32) \
+        k_ad_expand<K, true><<<grid, kAdBlock, 0, s>>>(a); \
+    else \
+        k_ad_expand<K, false><<<grid, kAdBlock, 0, s>>>(a)
+    if (a.rank <= 32) {
+        AD_EXPAND(1);
+    } else if (a.rank <= 64) {
+        AD_EXPAND(2);
+    } else {
+        AD_EXPAND(0);
     }
-    AD_EXPAND(1, 1)
-    AD_EXPAND(2, 1)
-    AD_EXPAND(1, 2)
-    AD_EXPAND(2, 2)
-    AD_EXPAND(1, 4)
-    AD_EXPAND(1, 8)
 #undef AD_EXPAND
 }
 
-template <int RT, int WR>
-void ad_grads(const AdArgs &a, hipStream_t s)
+// dx, dA and dB, as far as they are wanted, from the latents
+template <int RT, int WR, int KC>
+void ad_back(const AdArgs &a, hipStream_t s)
 {
+    constexpr int WT = kAdBackWaves / WR;
     const int rgs = ad_ceil(a.rank, RT * WR * 16);
-    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 8 * 128) * 8 : 0;
-    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 8 * 128) * 8 : 0;
-    k_ad_outer<RT, WR><<<nA + nB, kAdGradWaves * cdk::kWave, 0, s>>>(a, nB);
+    const int tA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 128) : 0;
+    const int tB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 128) : 0;
+    // With fewer gradient tiles than half the CUs, the tokens are shared: at least two times 32
+    // for each wave, and no more parts than fit their place.
+    const size_t whole = (size_t)a.n * a.rank * ((a.dA ? a.d_in : 0) + (a.dB ? a.d_out : 0));
+    int parts = 1;
+    if (tA + tB > 0 && tA + tB <= 128)
+        parts = std::max(1, (int)std::min<size_t>({(size_t)(256 / (tA + tB)), (size_t)(a.T / (2 * 32 * WT)),
+                                                   kAdPartFloats / whole}));
+    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 8 * 128) * 8 * parts : 0;
+    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 8 * 128) * 8 * parts : 0;
+    const int tiles = ad_slots(a) * (a.tile / 16);
+    const int slices = a.out ? ad_slices(a.d_in, kAdBackWaves, tiles) : 1;
+    const int nX = a.out ? tiles * slices : 0;
+    k_ad_back<RT, WR, KC><<<nB + nA + nX, kAdBackWaves * cdk::kWave, 0, s>>>(a, nB, nA, parts, slices);
+    if (parts > 1)
+        k_ad_sum<<<std::min<size_t>(1024, (whole / 4 + kAdBlock - 1) / kAdBlock), kAdBlock, 0, s>>>(
+            a.part, parts, a.dB, a.dB ? (size_t)a.n * a.rank * a.d_out : 0, a.dA,
+            a.dA ? (size_t)a.n * a.rank * a.d_in : 0);
 }
 
 }  // namespace
@@ -1168,11 +1192,12 @@ cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapter
     const size_t groups = (n_adapters + 1) * sizeof(AdGroup);
     const size_t copy = (size_t)n_adapters * rank * d_out * sizeof(uint16_t);
     const size_t parts[] = {lat,   pos * sizeof(int),  tiles,             groups,
-                            train ? lat : 0, train ? terms : 0, train ? terms : 0, train ? copy : 0};
-    size_t at[9] = {0};
-    for (int i = 0; i < 8; ++i)
+                            train ? lat : 0, train ? terms : 0, train ? terms : 0, train ? copy : 0,
+                            train ? kAdPartFloats * sizeof(float) : 0};
+    size_t at[10] = {0};
+    for (int i = 0; i < 9; ++i)
         at[i + 1] = at[i] + (parts[i] + 255) / 256 * 256;
-    if (hip_status(hipMalloc(&p->ws, at[8])) != CD_OK) {
+    if (hip_status(hipMalloc(&p->ws, at[9])) != CD_OK) {
         delete p;
         return CD_ENOMEM;
     }
@@ -1186,6 +1211,7 @@ cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapter
         p->latT = reinterpret_cast<uint16_t *>(ws + at[5]);
         p->glatT = reinterpret_cast<uint16_t *>(ws + at[6]);
         p->Bt = reinterpret_cast<uint16_t *>(ws + at[7]);
+        p->part = reinterpret_cast<float *>(ws + at[8]);
     }
     *out = p;
     return CD_OK;
@@ -1259,7 +1285,7 @@ cd_status countdown_adapters_add(cd_adapters *p, const uint16_t *x, size_t ldx, 
     } else {
         ad_group(a, false, s);
         ad_shrink(a, 1, s);
-        ad_expand(a, false, s);
+        ad_expand(a, s);
     }
     return launched(hipGetLastError());
 }
@@ -1300,18 +1326,17 @@ cd_status countdown_adapters_backward(cd_adapters *p, const uint16_t *x, size_t 
     a.Bt = p->Bt;
     a.latT = p->latT;
     a.glatT = dA ? p->glatT : nullptr;
+    a.part = p->part;
     ad_group(a, back, s);
     ad_shrink(a, (dB ? 1 : 0) + (back ? 2 : 0), s);
-    if (dx)
-        ad_expand(a, true, s);
-    if (dA || dB) {
-        if (a.rank <= 16)
-            ad_grads<1, 1>(a, s);
-        else if (a.rank <= 32)
-            ad_grads<2, 1>(a, s);
-        else
-            ad_grads<2, 2>(a, s);
-    }
+    if (a.rank <= 16)
+        ad_back<1, 1, 1>(a, s);
+    else if (a.rank <= 32)
+        ad_back<2, 1, 1>(a, s);
+    else if (a.rank <= 64)
+        ad_back<2, 2, 2>(a, s);
+    else
+        ad_back<2, 2, 0>(a, s);
     return launched(hipGetLastError());
 }
 

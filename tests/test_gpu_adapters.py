@@ -133,6 +133,8 @@ LONG = [
     (1000, 264, 136, 16, 1000, "mixed"),
     (1500, 1032, 520, 32, 5, "runs"),
     (200, 64, 64, 16, 4, "none"),
+    (4300, 72, 264, 40, 1, "runs"),
+    (2100, 520, 136, 16, 3, "mixed"),
 ]
 
 

@@ -62,7 +62,7 @@ def test_norm_and_clip(cd, sizes, types):
     with cd.GradClip(len(sizes)) as clip:
         keep = [t.clone() for t in grads]
         norm = cd.countdown_clip_grads(clip, grads, math.inf)
-        assert norm.dtype == torch.float64 and norm.shape == (1,)
+        assert norm.dtype == torch.float64 and norm.shape == ()
         check_norm(norm, keep)
         assert all(torch.equal(a, b) for a, b in zip(grads, keep))
         top = float(norm) * 0.37
@@ -160,7 +160,7 @@ def test_graph_replays(cd):
     grads = make(5, [5000, 70001, 3], (F32, BF16))
     out = [torch.empty_like(t) for t in grads]
     clip, other = cd.GradClip(3), cd.GradClip(3)
-    norm = torch.empty(1, dtype=torch.float64, device="cuda")
+    norm = torch.empty((), dtype=torch.float64, device="cuda")
     stream = torch.cuda.Stream()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=stream):
@@ -193,6 +193,9 @@ def test_refusals(cd):
             ([a], 1.0, [b.bfloat16()], ValueError), ([a], 1.0, [a, b], ValueError)]:
         with pytest.raises(err):
             cd.countdown_clip_grads(clip, grads, top, out=out)
+    for norm in (torch.empty(2, dtype=torch.float64, device="cuda"), torch.empty(1, device="cuda")):
+        with pytest.raises(ValueError):
+            cd.countdown_clip_grads(clip, [a], 1.0, norm=norm)
     assert bool((a == 1).all()) and bool((b == 1).all())
     assert float(cd.countdown_clip_grads(clip, [a, a], math.inf)) == math.sqrt(32.0)  # counted twice
     clip.close()
