@@ -13,12 +13,6 @@ namespace {
 constexpr int kAdMaxDim = 65536, kAdMaxRank = 256, kAdMaxAdapters = 1024;
 constexpr int kAdMaxTokens = 1 << 20;
 constexpr int kAdDecodeTokens = 16;  // tokens of countdown_adapters_project
-constexpr int kAdDirectTokens = 32;  // up to here countdown_adapters_add goes token by token
-// Up to so many products a workgroup forms the latents that it needs by itself, in one launch:
-// project 4096 x 4096 at one token, rank 16 (2^16): 10.9 us a call against 12.6 with a launch of their own;
-// add to 8 tokens of 4096, rank 16 (2^16 a token): 9.9 against 12.7.
-constexpr int64_t kAdOwnProject = 1 << 17;
-constexpr int kAdOwnAdd = 1 << 18;
 constexpr int kAdBlock = 256, kAdWaves = kAdBlock / cdk::kWave;
 constexpr size_t kAdPartFloats = (size_t)128 * 1024 * 32;  // place for workgroups' sums (16 MiB)
 constexpr int kAdPad = 32;  // tokens of one adapter are padded to the contraction of an MFMA
@@ -179,17 +173,24 @@ __device__ __forceinline__ void ad_store8(const AdArgs &a, size_t t, int col, co
     }
 }
 
-// ---------------------------------------------------------------- decode: token by token
+// --------------------------------------------------------- few tokens: one by one
 
 // scale A x of rank k, over a wave
 __device__ __forceinline__ float ad_latent(const AdArgs &a, int t, int id, int k)
 {
-    const uint16_t *p = a.x + t * a.ldx, *q = a.A + ((size_t)id * a.rank + k) * a.d_in;
+    const uint16_t *p = a.x + (size_t)t * a.ldx, *q = a.A + ((size_t)id * a.rank + k) * a.d_in;
     float s = 0.0f;
 #pragma unroll 4
     for (int i = threadIdx.x % cdk::kWave * 8; i < a.d_in; i += cdk::kColsPerLoad)
         s = cdk::dot8(load16(p + i), load16(q + i), s);
     return cdk::wave_sum(s) * ad_scale(a, id);
+}
+
+template <bool NT>
+__device__ __forceinline__ u32x4 ad_load16(const uint16_t *p)
+{
+    const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
+    return NT ? __builtin_nontemporal_load(q) : *q;
 }
 
 // sum over the rank of lat[k] B[a][o][k]
@@ -210,14 +211,14 @@ __device__ __forceinline__ float ad_row(const AdArgs &a, int id, int o, const fl
 // out[t][o] = base + v (no: the token has no adapter, the base's bits)
 __device__ __forceinline__ void ad_store1(const AdArgs &a, int t, int o, float v, bool no)
 {
-    const size_t i = t * a.ldb + o;
+    const size_t i = (size_t)t * a.ldb + o;
     if (a.type == CD_TYPE_F32) {
         const float *b = static_cast<const float *>(a.base);
-        static_cast<float *>(a.out)[t * a.ldo + o] = b ? (no ? b[i] : b[i] + v) : v;
+        static_cast<float *>(a.out)[(size_t)t * a.ldo + o] = b ? (no ? b[i] : b[i] + v) : v;
     } else {
         const uint16_t *b = static_cast<const uint16_t *>(a.base);
         const uint16_t w = (uint16_t)ad_pack(b ? v + cdk::bf16_lo(b[i]) : v, 0.0f);
-        static_cast<uint16_t *>(a.out)[t * a.ldo + o] = b && no ? b[i] : w;
+        static_cast<uint16_t *>(a.out)[(size_t)t * a.ldo + o] = b && no ? b[i] : w;
     }
 }
 
@@ -236,24 +237,24 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_lat(const AdArgs a)
         a.lat[w] = s;
 }
 
-// y = base + B lat: one lane per output, blockIdx.y the token
+// y = base + B lat: one lane per output, blockIdx.x the token
 __global__ __launch_bounds__(kAdBlock) void k_ad_up(const AdArgs a)
 {
-    const int t = blockIdx.y, o = blockIdx.x * kAdBlock + threadIdx.x, id = a.ids[t];
+    const int t = blockIdx.x, o = blockIdx.y * kAdBlock + threadIdx.x, id = a.ids[t];
     if (o >= a.d_out)
         return;
     const bool no = !ad_valid(a, id);
     ad_store1(a, t, o, no ? 0.0f : ad_row(a, id, o, a.lat + t * a.rank), no);
 }
 
-// Both in one launch: every workgroup forms its token's latent again, one rank a wave at a time, for
-// 1024 outputs. A launch less is worth 3 us to the caller's thread and 2 us to the GPU.
+// Both in one launch: every workgroup forms its token's latent again, one rank a wave at a
+// time, for 1024 outputs. A launch costs the caller's thread 2.9 us and the GPU 1 to 2.
 constexpr int kAdTokenBlock = 1024;
 
 __global__ __launch_bounds__(kAdTokenBlock) void k_ad_token(const AdArgs a)
 {
     __shared__ float lat[kAdMaxRank];
-    const int t = blockIdx.y, o = blockIdx.x * kAdTokenBlock + threadIdx.x, id = a.ids[t];
+    const int t = blockIdx.x, o = blockIdx.y * kAdTokenBlock + threadIdx.x, id = a.ids[t];
     const bool no = !ad_valid(a, id);  // uniform
     if (!no) {
         for (int k = ad_wave(); k < a.rank; k += kAdTokenBlock / cdk::kWave) {
@@ -274,7 +275,8 @@ __global__ __launch_bounds__(kAdTokenBlock) void k_ad_token(const AdArgs a)
 constexpr int kAdProjBlock = 512, kAdProjWaves = kAdProjBlock / cdk::kWave;
 
 // OWN: every workgroup forms the latents again, while its first columns of W are on their way.
-template <bool OWN>
+// NT: W past the caches.
+template <bool OWN, bool NT>
 __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
 {
     __shared__ u32x4 lds[kAdProjWaves][kAdStage];
@@ -288,20 +290,23 @@ __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
         w[i] = a.W + (size_t)min(o0 + 4 * i + g, a.d_out - 1) * a.d_in;
         x[i] = a.x + min(4 * i + g, a.T - 1) * a.ldx;
     }
-    constexpr int kStep = 128 * kAdProjWaves;
+    // this wave's columns
+    const int per = (a.d_in + 128 * kAdProjWaves - 1) / (128 * kAdProjWaves) * 128;
+    const int k0 = wave * per, kend = min(a.d_in, k0 + per);
     u32x4 wv[2][4], xv[2][4];
     const auto load = [&](int s, int k) {
         k += 8 * m;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            wv[s][i] = load16(or_zero(k < a.d_in, w[i] + k));
+            wv[s][i] = ad_load16<NT>(or_zero(k < a.d_in, w[i] + k));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i == 0 || 4 * i < a.T)
                 xv[s][i] = load16(or_zero(k < a.d_in, x[i] + k));
     };
     f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    load(0, wave * 128);
+    if (k0 < kend)
+        load(0, k0);
     if constexpr (OWN)
         for (int p = wave; p < a.T * a.rank; p += kAdProjWaves) {
             const int t = p / a.rank, id = a.ids[t];
@@ -310,14 +315,14 @@ __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
                 own[p] = s;
         }
 #pragma unroll 1
-    for (int kb = wave * 128; kb < a.d_in; kb += 2 * kStep) {
+    for (int kb = k0; kb < kend; kb += 256) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int k = kb + s * kStep;
-            if (k >= a.d_in)
+            const int k = kb + s * 128;
+            if (k >= kend)
                 break;
-            if (k + kStep < a.d_in)
-                load(1 - s, k + kStep);
+            if (k + 128 < kend)
+                load(1 - s, k + 128);
             ad_stage(wv[s], lds[wave], lane);
             ad_stage(xv[s], lds[wave], lane);
 #pragma unroll
@@ -1096,10 +1101,8 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
         k_ad_shrink<M, R><<<grid, kAdShrinkBlock, 0, s>>>(a, kinds)
     AD_SHRINK(1, 1);
     AD_SHRINK(2, 1);
-    AD_SHRINK(4, 1);
     AD_SHRINK(1, 2);
     AD_SHRINK(2, 2);
-    AD_SHRINK(4, 2);
     AD_SHRINK(1, 4);
     AD_SHRINK(2, 4);
 #undef AD_SHRINK
@@ -1137,14 +1140,14 @@ void ad_back(const AdArgs &a, hipStream_t s)
 {
     constexpr int WT = kAdBackWaves / WR;
     const int rgs = ad_ceil(a.rank, RT * WR * 16);
-    const int tA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 128) : 0;
-    const int tB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 128) : 0;
     // With fewer gradient tiles than half the CUs, the tokens are shared: at least two times 32
-    // for each wave, and no more parts than fit their place.
-    const size_t whole = (size_t)a.n * a.rank * ((a.dA ? a.d_in : 0) + (a.dB ? a.d_out : 0));
+    // for each wave, and no more parts than fit their place. (Counted for dA and dB, whichever is
+    // wanted: the sums' order is the same alone and together.)
+    const int tiles128 = a.n * rgs * (ad_ceil(a.d_in, 128) + ad_ceil(a.d_out, 128));
+    const size_t whole = (size_t)a.n * a.rank * (a.d_in + a.d_out);
     int parts = 1;
-    if (tA + tB > 0 && tA + tB <= 128)
-        parts = std::max(1, (int)std::min<size_t>({(size_t)(256 / (tA + tB)), (size_t)(a.T / (2 * 32 * WT)),
+    if (tiles128 <= 128 && (a.dA || a.dB))
+        parts = std::max(1, (int)std::min<size_t>({(size_t)(256 / tiles128), (size_t)(a.T / (2 * 32 * WT)),
                                                    kAdPartFloats / whole}));
     const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 8 * 128) * 8 * parts : 0;
     const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 8 * 128) * 8 * parts : 0;
@@ -1254,12 +1257,22 @@ cd_status countdown_adapters_project(cd_adapters *p, const uint16_t *x, size_t l
     if (T == 0)
         return CD_OK;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if ((int64_t)T * a.rank * a.d_in <= kAdOwnProject) {
-        k_ad_project<true><<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a);
-    } else {
+    // Few latents every workgroup forms for itself: 4096 x 4096 at one token, rank 16 (2^16 products)
+    // 11.0 us a call against 12.6 with a launch of their own.
+    const bool own = (int64_t)T * a.rank * a.d_in <= 1 << 17;
+    // A W that would sweep most of the last-level cache goes past it: 117 MB (4096 x 14336, 8
+    // tokens) 24.7 us against 27.1; 48 MB that was still there from the last call, 14.9 against 11.9.
+    const bool nt = (size_t)a.d_in * a.d_out * sizeof(uint16_t) > ((size_t)64 << 20);
+    if (!own)
         k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-        k_ad_project<false><<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a);
-    }
+#define AD_PROJECT(O, N) \
+    if (own == O && nt == N) \
+        k_ad_project<O, N><<<ad_ceil(a.d_out, 16), kAdProjBlock, 0, s>>>(a)
+    AD_PROJECT(false, false);
+    AD_PROJECT(false, true);
+    AD_PROJECT(true, false);
+    AD_PROJECT(true, true);
+#undef AD_PROJECT
     return launched(hipGetLastError());
 }
 
@@ -1277,11 +1290,20 @@ cd_status countdown_adapters_add(cd_adapters *p, const uint16_t *x, size_t ldx, 
     if (st != CD_OK || T == 0)
         return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (T <= kAdDirectTokens && a.rank * a.d_in <= kAdOwnAdd) {
-        k_ad_token<<<dim3(ad_ceil(a.d_out, kAdTokenBlock), T), kAdTokenBlock, 0, s>>>(a);
-    } else if (T <= kAdDirectTokens) {
+    // How the tokens are taken (us a call, fp32 y, tokens 8 / 64 / 256 / 1024):
+    //                          one launch            two launches          grouped
+    //   4096 -> 4096, rank 16   8.4  8.3 12.5  41.6  11.2 11.5 11.0  28.0  14.8 15.4 15.7 21.5
+    //   1024 -> 4096, rank 64   8.3  9.2 27.0 101.3  10.8 10.7 22.1  77.7  16.1 17.2 17.8 23.7
+    //   4096 -> 4096, rank 64  13.0 19.0 49.2 179.9   9.8 10.9 31.8  97.3  21.0 21.7 22.9 33.2
+    // By token, every one reads its adapter again: once, or A again for each 1024 outputs, 16
+    // ranks at a time. The bounds below are where the columns cross.
+    const int64_t down = (int64_t)a.rank * a.d_in, up = (int64_t)a.rank * a.d_out;
+    const int slices = ad_ceil(a.d_out, kAdTokenBlock);
+    if (a.rank <= 64 && down <= 3 << 16 && T * (slices * down + up) < 3 << 24) {
+        k_ad_token<<<dim3(T, slices), kAdTokenBlock, 0, s>>>(a);
+    } else if (T * (down + up) <= 1 << 26) {
         k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
-        k_ad_up<<<dim3(ad_ceil(a.d_out, kAdBlock), T), kAdBlock, 0, s>>>(a);
+        k_ad_up<<<dim3(T, ad_ceil(a.d_out, kAdBlock)), kAdBlock, 0, s>>>(a);
     } else {
         ad_group(a, false, s);
         ad_shrink(a, 1, s);

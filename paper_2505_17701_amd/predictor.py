@@ -6,7 +6,8 @@ path (countdown_ffn_topk with the ideal D coefficient). The predictor scores
 s_hat = x . theta_A . theta_B (rank d_rank) and is trained with binary cross
 entropy on the logits and AdamW, as in the paper's training table; at
 inference a neuron is predicted alive when s_hat > thld (0 for the trained
-logit). Training is plain PyTorch: only inference runs on the HIP kernels.
+logit). Training is plain PyTorch but for clipping by the global gradient norm
+(max_norm, countdown_clip_grads); inference runs on the HIP kernels.
 
 Layout: the returned predictor is in the kernels' layout, A_t [d_rank][d_model]
 and B_t [d_ff][d_rank], bf16.
@@ -21,6 +22,7 @@ only rescales the score, which the threshold absorbs).
 """
 from __future__ import annotations
 
+import math
 import time
 
 import numpy as np
@@ -63,12 +65,54 @@ def f1_score(pred, true) -> float:
     return 2.0 * tp / (2.0 * tp + fp + fn) if tp + fp + fn else 1.0
 
 
+class _Stepper:
+    """opt.step(), with max_norm after clipping the parameters' gradients to that global
+    norm (countdown_clip_grads). A step whose norm is not finite is skipped."""
+
+    def __init__(self, opt, params, max_norm):
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError(f"max_norm must be positive, got {max_norm}")
+        self.opt, self.params, self.max_norm = opt, params, max_norm
+        self.norms, self.skipped, self.clip = [], 0, None
+        if max_norm is not None:
+            import torch
+
+            from . import binding as cd
+
+            self.device = torch.cuda.device(params[0].device)
+            with self.device:
+                self.clip = cd.GradClip(max_tensors=len(params))
+
+    def step(self):
+        if self.clip is not None:
+            from . import binding as cd
+
+            with self.device:
+                norm = float(cd.countdown_clip_grads(self.clip, [p.grad for p in self.params],
+                                                     self.max_norm))
+            self.norms.append(norm)
+            if not math.isfinite(norm):
+                self.skipped += 1
+                return
+        self.opt.step()
+
+    def log(self) -> dict:
+        return {} if self.clip is None else {"grad_norms": self.norms,
+                                             "skipped_steps": self.skipped}
+
+    def close(self):
+        if self.clip is not None:
+            self.clip.close()
+
+
 def train_low_rank(X, masks, d_rank: int, epochs: int = 10, lr: float = 1e-3, batch: int = 16,
-                   seed: int = 42, weight_decay: float = 0.01):
+                   seed: int = 42, weight_decay: float = 0.01, max_norm: float | None = None):
     """Fit s_hat = x . theta_A . theta_B to the masks with BCE-with-logits and AdamW.
 
-    X: [N, d_model] bf16 tokens on the GPU; masks: [N, d_ff] bool. Returns
-    (A_t [d_rank, d_model] bf16, B_t [d_ff, d_rank] bf16, log dict)."""
+    X: [N, d_model] bf16 tokens on the GPU; masks: [N, d_ff] bool. With max_norm the
+    gradients of each step are clipped to that global norm; the log then has the norm of
+    every step ("grad_norms") and the number of steps skipped for a norm that was not finite
+    ("skipped_steps"). Returns (A_t [d_rank, d_model] bf16, B_t [d_ff, d_rank] bf16, log dict)."""
     import torch
 
     g = torch.Generator(device=X.device).manual_seed(seed)
@@ -80,6 +124,7 @@ def train_low_rank(X, masks, d_rank: int, epochs: int = 10, lr: float = 1e-3, ba
     theta_b = (torch.randn(d_rank, dff, generator=g, device=X.device) / d_rank ** 0.5)
     theta_b.requires_grad_()
     opt = torch.optim.AdamW([theta_a, theta_b], lr=lr, weight_decay=weight_decay)
+    stepper = _Stepper(opt, [theta_a, theta_b], max_norm)
     loss_fn = torch.nn.BCEWithLogitsLoss()
     losses = []
     t0 = time.time()
@@ -92,14 +137,15 @@ def train_low_rank(X, masks, d_rank: int, epochs: int = 10, lr: float = 1e-3, ba
             loss = loss_fn(logits, yf[j])
             opt.zero_grad(set_to_none=True)
             loss.backward()
-            opt.step()
+            stepper.step()
             tot += float(loss.detach())
             nb += 1
         losses.append(tot / nb)
     torch.cuda.synchronize()
+    stepper.close()
     A_t = theta_a.detach().t().contiguous().to(torch.bfloat16)
     B_t = theta_b.detach().t().contiguous().to(torch.bfloat16)
-    return A_t, B_t, {"epoch_loss": losses, "seconds": time.time() - t0}
+    return A_t, B_t, {"epoch_loss": losses, "seconds": time.time() - t0, **stepper.log()}
 
 
 def calibrated_threshold(A_t, B_t, X, k: float) -> float:
@@ -126,10 +172,10 @@ def ternarize(W):
 
 
 def train_ternary(X, masks, epochs: int = 10, lr: float = 1e-3, batch: int = 16, seed: int = 42,
-                  weight_decay: float = 0.01):
+                  weight_decay: float = 0.01, max_norm: float | None = None):
     """Fit s_hat = x . (gamma * ternary(W)) to the masks (BCE-with-logits, AdamW, the
-    straight-through estimator). X: [N, d_model] bf16 on the GPU; masks [N, d_ff] bool.
-    Returns (theta_t int8 numpy [d_ff, d_model], log dict)."""
+    straight-through estimator). X: [N, d_model] bf16 on the GPU; masks [N, d_ff] bool;
+    max_norm as in train_low_rank. Returns (theta_t int8 numpy [d_ff, d_model], log dict)."""
     import torch
 
     g = torch.Generator(device=X.device).manual_seed(seed)
@@ -139,6 +185,7 @@ def train_ternary(X, masks, epochs: int = 10, lr: float = 1e-3, batch: int = 16,
     yf = masks.float()
     W = (torch.randn(dff, dm, generator=g, device=X.device) / dm ** 0.5).requires_grad_()
     opt = torch.optim.AdamW([W], lr=lr, weight_decay=weight_decay)
+    stepper = _Stepper(opt, [W], max_norm)
     loss_fn = torch.nn.BCEWithLogitsLoss()
     losses = []
     t0 = time.time()
@@ -152,14 +199,15 @@ def train_ternary(X, masks, epochs: int = 10, lr: float = 1e-3, batch: int = 16,
             loss = loss_fn(xf[j] @ Wq.t(), yf[j])
             opt.zero_grad(set_to_none=True)
             loss.backward()
-            opt.step()
+            stepper.step()
             tot += float(loss.detach())
             nb += 1
         losses.append(tot / nb)
     torch.cuda.synchronize()
+    stepper.close()
     theta_t = ternarize(W.detach())[0].to(torch.int8).cpu().numpy()
     return theta_t, {"epoch_loss": losses, "seconds": time.time() - t0,
-                     "zero_frac": float((theta_t == 0).mean())}
+                     "zero_frac": float((theta_t == 0).mean()), **stepper.log()}
 
 
 def calibrated_threshold_tern(theta_p, X, k: float, d_ff: int) -> float:

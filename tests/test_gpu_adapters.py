@@ -136,6 +136,16 @@ LONG = [
     (4300, 72, 264, 40, 1, "runs"),
     (2100, 520, 136, 16, 3, "mixed"),
 ]
+BIG = [  # more work than is done token by token; every width of the rank's tiles
+    (9000, 264, 680, 8, 3, "runs"),
+    (4300, 264, 712, 16, 1, "one"),
+    (3000, 520, 424, 24, 40, "mixed"),
+    (2200, 648, 328, 32, 9, "runs"),
+    (2600, 520, 136, 40, 7, "mixed"),
+    (1100, 264, 520, 80, 5, "runs"),
+    (600, 264, 184, 256, 3, "mixed"),
+    (2100, 264, 248, 64, 6, "none"),
+]
 
 
 @pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
@@ -157,7 +167,7 @@ def test_project(cd, shape, y_type):
 
 
 @pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("shape", SHAPES + LONG)
+@pytest.mark.parametrize("shape", SHAPES + LONG + BIG)
 def test_add(cd, shape, y_type):
     c = Case(2, *shape)
     delta, mag = c.delta()
@@ -181,7 +191,7 @@ def test_add(cd, shape, y_type):
 
 
 @pytest.mark.parametrize("dx_type", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("shape", SHAPES + LONG)
+@pytest.mark.parametrize("shape", SHAPES + LONG + BIG[:1] + BIG[-2:])
 def test_backward(cd, shape, dx_type):
     c = Case(3, *shape)
     want = c.grads()
@@ -240,9 +250,10 @@ def test_gradients_against_differences(cd):
                 assert abs((up - down) / 8 - float(gflat[i])) <= tol
 
 
-def test_strides_leave_the_rest(cd):
+@pytest.mark.parametrize("T,rank", [(37, 24), (2200, 80)])
+def test_strides_leave_the_rest(cd, T, rank):
     """x, base, y, dy and dx as column slices of wider tensors; y and base two slices of one."""
-    c = Case(6, 37, 264, 136, 24, 4)
+    c = Case(6, T, 264, 136, rank, 4)
     d = c.dev()
     wide = torch.full((c.T, 4096), 7.0, device="cuda")
     xs = torch.full((c.T + 2, 512), 9.0, dtype=torch.bfloat16, device="cuda")
@@ -250,7 +261,7 @@ def test_strides_leave_the_rest(cd):
     x.copy_(d.x)
     base, y = wide[:, 8:8 + c.do], wide[:, 256:256 + c.do]
     base.copy_(d.base)
-    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=64, train=True) as pool:
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=T, train=True) as pool:
         args = (d.ids, d.A, d.B, d.scale)
         plain = cd.countdown_adapters_add(pool, d.x, *args, base=d.base)
         cd.countdown_adapters_add(pool, x, *args, base=base, y=y)
@@ -275,10 +286,10 @@ def test_strides_leave_the_rest(cd):
         assert bool((wide == 7.0).all())
 
 
-@pytest.mark.parametrize("T", [9, 200])
-def test_bad_numbers_stay_where_they_are(cd, T):
+@pytest.mark.parametrize("T,rank", [(9, 16), (200, 16), (2050, 88), (2500, 80)])
+def test_bad_numbers_stay_where_they_are(cd, T, rank):
     """NaN and infinity in one token, and in an adapter that no token uses, reach nothing else."""
-    c = Case(7, T, 264, 136, 16, 4)
+    c = Case(7, T, 264, 136, rank, 4)
     c.ids = torch.arange(T, dtype=torch.int32) % 3 - 1  # -1, 0, 1; adapters 2 and 3 unused
     c.A[3], c.B[3], c.scale[3] = float("nan"), float("inf"), float("nan")
     c.A[2], c.B[2] = float("inf"), float("nan")
@@ -320,11 +331,11 @@ def test_empty_call(cd):
         assert dx.shape == (0, c.di) and not dA.any() and not dB.any()
 
 
-@pytest.mark.parametrize("T", [8, 150])
-def test_graph_replays_with_other_values(cd, T):
+@pytest.mark.parametrize("T,rank", [(8, 24), (150, 24), (1300, 72)])
+def test_graph_replays_with_other_values(cd, T, rank):
     """A captured add + backward, replayed with other tokens, adapters and ids behind the same
     pointers, eager calls of another pool between the replays."""
-    first = Case(9, T, 264, 520, 24, 5)
+    first = Case(9, T, 264, 520, rank, 5)
     d = first.dev()
     args = (d.ids, d.A, d.B, d.scale)
     pool = cd.Adapters(first.di, first.do, first.r, first.n, max_tokens=T, train=True)
@@ -343,7 +354,7 @@ def test_graph_replays_with_other_values(cd, T):
         cd.countdown_adapters_backward(pool, d.x, d.dy, *args, dx=dx, dA=dA, dB=dB)
         cd.countdown_adapters_project(pool, xs, d.W, idss, d.A, d.B, d.scale, y=p)
     for seed in (10, 11, 12, 13):
-        new = Case(seed, T, 264, 520, 24, 5, how=("mixed", "runs", "none", "one")[seed % 4]).dev()
+        new = Case(seed, T, 264, 520, rank, 5, how=("mixed", "runs", "none", "one")[seed % 4]).dev()
         for k in ("x", "dy", "ids", "A", "B", "scale", "base", "W"):
             getattr(d, k).copy_(getattr(new, k))
         want = [cd.countdown_adapters_add(eager, d.x, *args, base=d.base),
@@ -361,8 +372,8 @@ def test_graph_replays_with_other_values(cd, T):
 
 
 def test_two_pools_on_two_streams(cd):
-    cases = [Case(20 + i, 150, 264, 520, 16, 3).dev() for i in range(2)]
-    pools = [cd.Adapters(264, 520, 16, 3, max_tokens=150, train=True) for _ in range(2)]
+    cases = [Case(20 + i, 1300, 264, 520, 72, 3).dev() for i in range(2)]
+    pools = [cd.Adapters(264, 520, 72, 3, max_tokens=1300, train=True) for _ in range(2)]
     want = [[cd.countdown_adapters_add(p, c.x, c.ids, c.A, c.B, c.scale, base=c.base),
              *cd.countdown_adapters_backward(p, c.x, c.dy, c.ids, c.A, c.B, c.scale)]
             for p, c in zip(pools, cases)]

@@ -80,6 +80,37 @@ def test_a_failed_allocation_leaves_nothing(host):
     assert host.lib.host_hip_live_allocations() == live
 
 
+def test_launches_by_the_work(host):
+    """One launch for little work, two by token, three with the tokens grouped."""
+    def kernels(call, sizes, **kw):
+        st, h = create(host, *sizes, 1)
+        assert st == 0
+        host.launches()
+        assert call(host, h, ldx=sizes[0], **kw) == 0
+        out = [k.split("<")[0] for k, _ in host.launches()]
+        assert host.lib.countdown_adapters_destroy(h) == 0
+        return out
+
+    by_token, grouped = ["k_ad_lat", "k_ad_up"], ["k_ad_group", "k_ad_shrink", "k_ad_expand"]
+    for sizes, T, want in [((4096, 4096, 16, 16), 8, ["k_ad_token"]),
+                           ((4096, 4096, 16, 16), 128, ["k_ad_token"]),
+                           ((4096, 4096, 16, 16), 400, by_token),
+                           ((4096, 4096, 16, 16), 1024, grouped),
+                           ((4096, 4096, 64, 16), 1, by_token),
+                           ((512, 1024, 128, 4), 1, by_token),
+                           ((4096, 14336, 64, 8), 57, grouped),
+                           ((8, 8, 8, 1), 200000, ["k_ad_token"])]:
+        assert kernels(add, (*sizes, T), T=T, ldb=sizes[1], ldy=sizes[1]) == want, (sizes, T)
+    for sizes, T, want in [((4096, 4096, 16, 8), 1, ["k_ad_project"]),
+                           ((4096, 4096, 16, 8), 8, ["k_ad_lat", "k_ad_project"])]:
+        assert kernels(project, (*sizes, T), T=T, ldy=sizes[1]) == want
+    back = ["k_ad_group", "k_ad_shrink", "k_ad_back"]
+    for sizes, T, want in [((256, 688, 8, 3), 37, back), ((4096, 4096, 16, 4), 4096, back),
+                           ((520, 1080, 40, 1), 4877, back + ["k_ad_sum"])]:
+        kw = dict(T=T, lddy=sizes[1], ldb=sizes[0], lddx=sizes[0])
+        assert kernels(backward, (*sizes, T), **kw) == want
+
+
 def test_calls_allocate_nothing(host, pool):
     live = host.lib.host_hip_live_allocations()
     assert add(host, pool) == 0 and project(host, pool) == 0 and backward(host, pool) == 0
