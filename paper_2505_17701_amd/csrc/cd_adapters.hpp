@@ -119,7 +119,6 @@ __device__ __forceinline__ void ad_transpose8(const u32x4 (&r)[8], u32x4 (&c)[8]
 // over the banks.
 constexpr int kAdStage = 256;  // 16-byte chunks
 
-
 __device__ __forceinline__ void ad_wave_sync()
 {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -266,6 +265,142 @@ __global__ __launch_bounds__(kAdTokenBlock) void k_ad_token(const AdArgs a)
     }
     if (o < a.d_out)
         ad_store1(a, t, o, no ? 0.0f : ad_row(a, id, o, lat), no);
+}
+
+// The backward call on few tokens, without grouping: a workgroup per token forms lat
+// (blockIdx.y + kind 0) and glat (1), the next launch everything else.
+constexpr int kAdFewTokens = 16;
+constexpr int kAdFewRanks = 32;  // of glat, summed at a time
+
+__global__ __launch_bounds__(kAdTokenBlock) void k_ad_few_latents(const AdArgs a, int kind)
+{
+    __shared__ float sums[kAdTokenBlock / cdk::kWave][kAdFewRanks];
+    const int t = blockIdx.x, id = a.ids[t], wave = ad_wave(), lane = threadIdx.x % cdk::kWave;
+    if (!ad_valid(a, id))
+        return;
+    if (blockIdx.y + kind == 0) {
+        for (int k = wave; k < a.rank; k += kAdTokenBlock / cdk::kWave) {
+            const float s = ad_latent(a, t, id, k);
+            if (lane == 0)
+                a.lat[t * a.rank + k] = s;
+        }
+        return;
+    }
+    const uint16_t *B = a.B + (size_t)id * a.d_out * a.rank, *dy = a.dy + (size_t)t * a.lddy;
+    for (int r0 = 0; r0 < a.rank; r0 += kAdFewRanks) {
+        float acc[kAdFewRanks];
+#pragma unroll
+        for (int k = 0; k < kAdFewRanks; ++k)
+            acc[k] = 0.0f;
+#pragma unroll 2
+        for (int o = threadIdx.x; o < a.d_out; o += kAdTokenBlock) {
+            const float d = cdk::bf16_lo(dy[o]);
+#pragma unroll
+            for (int c = 0; c < kAdFewRanks / 8; ++c) {
+                const u32x4 b = load16(or_zero(r0 + 8 * c < a.rank, B + (size_t)o * a.rank + r0 + 8 * c));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[8 * c + 2 * e] += d * cdk::bf16_lo(b[e]);
+                    acc[8 * c + 2 * e + 1] += d * cdk::bf16_hi(b[e]);
+                }
+            }
+        }
+        __syncthreads();  // (the last ranks' sums are read)
+#pragma unroll
+        for (int k = 0; k < kAdFewRanks; ++k) {
+            const float s = cdk::wave_sum(acc[k]);
+            if (lane == 0)
+                sums[wave][k] = s;
+        }
+        __syncthreads();
+        if (threadIdx.x < kAdFewRanks && r0 + (int)threadIdx.x < a.rank) {
+            float s = 0.0f;
+            for (int w = 0; w < kAdTokenBlock / cdk::kWave; ++w)
+                s += sums[w][threadIdx.x];
+            a.glat[t * a.rank + r0 + threadIdx.x] = s * ad_scale(a, id);
+        }
+    }
+}
+
+// += f times the 8 bf16 of v
+__device__ __forceinline__ void ad_axpy8(float f, const u32x4 &v, float (&acc)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        acc[2 * e] += f * cdk::bf16_lo(v[e]);
+        acc[2 * e + 1] += f * cdk::bf16_hi(v[e]);
+    }
+}
+
+// Workgroups [0, nB) dB, the next nA dA, the others dx; a lane has 8 elements of a row.
+__global__ __launch_bounds__(kAdBlock) void k_ad_few_back(const AdArgs a, int nB, int nA)
+{
+    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    const int b = blockIdx.x;
+    if (b < nB + nA) {  // uniform: one adapter, whose tokens are added in their order
+        const bool second = b < nB;
+        const int per = (second ? nB : nA) / a.n, i = second ? b : b - nB;
+        const int ad = i / per, width = second ? a.d_out * (a.rank / 8) : a.rank * (a.d_in / 8);
+        const int at = i % per * kAdBlock + threadIdx.x, lane = threadIdx.x % cdk::kWave;
+        static_assert(kAdFewTokens <= cdk::kWave, "a lane for each token");
+        const uint64_t mine = cdk::ballot(lane < a.T && a.ids[min(lane, a.T - 1)] == ad);
+        if (at >= width)
+            return;
+        const int row = second ? at / (a.rank / 8) : at / (a.d_in / 8);  // output o, or rank k
+        const int col = (second ? at % (a.rank / 8) : at % (a.d_in / 8)) * 8;
+        for (uint64_t left = mine; left;) {  // four tokens' loads in flight
+            float f[4];
+            u32x4 v[4];
+            float l[4][8];
+            int m = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool ok = left != 0;
+                const int t = ok ? __builtin_ctzll(left) : 0;
+                left &= left - 1;
+                m += ok;
+                if (second) {
+                    f[q] = cdk::bf16_lo(*or_zero(ok, a.dy + (size_t)t * a.lddy + row));
+                    const float *p = a.lat + t * a.rank + col;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        l[q][e] = ok ? p[e] : 0.0f;
+                } else {
+                    f[q] = *or_zero(ok, a.glat + t * a.rank + row);
+                    v[q] = load16(or_zero(ok, a.x + (size_t)t * a.ldx + col));
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (q < m) {
+                    if (second)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            acc[e] += f[q] * l[q][e];
+                    else
+                        ad_axpy8(f[q], v[q], acc);
+                }
+        }
+        float *dst = second ? a.dB + ((size_t)ad * a.d_out + row) * a.rank + col
+                            : a.dA + ((size_t)ad * a.rank + row) * a.d_in + col;
+        reinterpret_cast<f32x4_t *>(dst)[0] = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
+        reinterpret_cast<f32x4_t *>(dst)[1] = f32x4_t{acc[4], acc[5], acc[6], acc[7]};
+        return;
+    }
+    const int per = (a.d_in / 8 + kAdBlock - 1) / kAdBlock, i = b - nB - nA;
+    const int t = i / per, col = (i % per * kAdBlock + threadIdx.x) * 8, id = a.ids[t];
+    if (col >= a.d_in)
+        return;
+    const bool no = !ad_valid(a, id);
+    u32x4 base[2];
+    ad_base8(a, true, t, col, base);
+    if (!no) {
+        const uint16_t *A = a.A + (size_t)id * a.rank * a.d_in + col;
+#pragma unroll 4
+        for (int k = 0; k < a.rank; ++k)
+            ad_axpy8(a.glat[t * a.rank + k], load16(A + (size_t)k * a.d_in), acc);
+    }
+    ad_store8(a, t, col, base, acc, no);
 }
 
 // y = W x + B lat for up to 16 tokens: a workgroup's eight waves each take an eighth of the
@@ -461,7 +596,12 @@ __device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, i
 // blockIdx.z: with both, 0 is glat). Eight waves split the contraction in blocks of 128
 // columns, and their sums meet in LDS. The scale is applied here. Tokens past the tile's last
 // and ranks past the last repeat another: they only reach sums of their own, which are not
-// stored.
+// stored. At rank 32 bound by reading x (16384 tokens of 4096 in 36 us, 34 without the
+// factor's loads; the last call's 134 MB of outputs are written back meanwhile), at rank 64
+// by the factor as well, which each tile reads again (8192 tokens of 4096 and 14336: 90 us, 70
+// without). Neither more blocks in flight nor more waves change that, and tiles of one adapter
+// on one XCD, whose L2 would hold the factor, cost more on the side of x (110 us): tiles that
+// run at the same time then lie far apart.
 constexpr int kAdShrinkBlock = 512, kAdShrinkWaves = kAdShrinkBlock / cdk::kWave;
 
 template <int MT, int RT>
@@ -497,7 +637,7 @@ __global__ __launch_bounds__(kAdShrinkBlock, MT + RT <= 4 ? 4 : 2) void k_ad_shr
             fr[j][q] = min(r0 + j * 16 + 4 * q + g, a.rank - 1) * K;
     u32x4 xv[kDepth][MT][4], fv[kDepth][RT][4];
     const auto load = [&](int s, int k) {
-        k += 8 * (m);
+        k += 8 * m;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -1349,6 +1489,19 @@ cd_status countdown_adapters_backward(cd_adapters *p, const uint16_t *x, size_t 
     a.latT = p->latT;
     a.glatT = dA ? p->glatT : nullptr;
     a.part = p->part;
+    // Two launches instead of three while a workgroup reads a token's factors in a moment (us a
+    // call, tokens 1 / 8 / 16, grouped 64): 4096 -> 4096 rank 16, four adapters 15.7 16.2 16.4
+    // against 17.9 19.0 19.2; 688 -> 256 rank 64 16.4 16.9 17.3 against 18.7; 1024 -> 3000 rank 64
+    // 26.0 27.0 28.6 against 20.6 21.7 21.3. With more tokens of one adapter its row's sum is a
+    // long chain: 4096 -> 4096 rank 8, one adapter, 32 tokens 21.4 against 18.5.
+    if (T <= kAdFewTokens && (int64_t)a.rank * std::max(a.d_in, a.d_out) <= 1 << 17) {
+        k_ad_few_latents<<<dim3(T, back && dB ? 2 : 1), kAdTokenBlock, 0, s>>>(a, dB ? 0 : 1);
+        const int nB = dB ? a.n * ad_ceil(a.d_out * (a.rank / 8), kAdBlock) : 0;
+        const int nA = dA ? a.n * ad_ceil(a.rank * (a.d_in / 8), kAdBlock) : 0;
+        const int nX = dx ? T * ad_ceil(a.d_in / 8, kAdBlock) : 0;
+        k_ad_few_back<<<nB + nA + nX, kAdBlock, 0, s>>>(a, nB, nA);
+        return launched(hipGetLastError());
+    }
     ad_group(a, back, s);
     ad_shrink(a, (dB ? 1 : 0) + (back ? 2 : 0), s);
     if (a.rank <= 16)

@@ -106,7 +106,9 @@ def test_launches_by_the_work(host):
         assert kernels(project, (*sizes, T), T=T, ldy=sizes[1]) == want
     back = ["k_ad_group", "k_ad_shrink", "k_ad_back"]
     for sizes, T, want in [((256, 688, 8, 3), 37, back), ((4096, 4096, 16, 4), 4096, back),
-                           ((520, 1080, 40, 1), 4877, back + ["k_ad_sum"])]:
+                           ((520, 1080, 40, 1), 4877, back + ["k_ad_sum"]),
+                           ((4096, 4096, 16, 4), 16, ["k_ad_few_latents", "k_ad_few_back"]),
+                           ((4096, 4096, 16, 4), 17, back), ((1024, 3000, 64, 4), 8, back)]:
         kw = dict(T=T, lddy=sizes[1], ldb=sizes[0], lddx=sizes[0])
         assert kernels(backward, (*sizes, T), **kw) == want
 
