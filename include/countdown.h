@@ -332,7 +332,10 @@ cd_status countdown_stream_read(const void *src, size_t bytes, uint32_t *sink, v
  * convention -1) it uses none, and A, B and scale are not read for it. An
  * adapter of a smaller rank is stored with zero rows of A (columns of B).
  *   lat_t = A_a x_t,   delta_t = scale_a B_a lat_t   (0 without an adapter).
- * Products and sums are fp32; lat is not rounded below fp32.
+ * Products and sums are fp32; lat and glat are not rounded below fp32 (where a bf16
+ * matrix product takes them, they enter as three exact bf16 terms). Numbers that
+ * are not finite stay within their token and their adapter: what they reach is
+ * not finite, infinity or NaN.
  *
  * Conventions beyond those at the top of this file:
  *  - ids int32[T] and scale are 4-byte aligned device arrays, all other
@@ -364,12 +367,14 @@ typedef struct cd_adapters cd_adapters;
 #define CD_ADAPTERS_TRAIN 1u  /* also allocate the workspace of the backward call */
 
 /*
- * Create the workspace of a pool's calls on the current device. d_in and d_out:
+ * Create the workspace of a pool's calls on the current device; the weights stay
+ * with the caller and may change between calls. d_in and d_out:
  * positive multiples of 8 up to 65536; rank: a multiple of 8 up to 256;
  * 1 <= n_adapters <= 1024; 1 <= max_tokens <= 2^20. CD_EINVAL for malformed
  * sizes and unknown flags, CD_EUNSUPPORTED beyond those limits (both before any
  * HIP call), CD_ENOMEM / CD_EHIP when allocation fails. *out is set only on
- * success. Holds rank floats per token, with CD_ADAPTERS_TRAIN twice that.
+ * success. The workspace takes about 4 rank + 5 bytes per token; with
+ * CD_ADAPTERS_TRAIN 20 rank + 5, as many bytes as B, and 16 MiB.
  */
 cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapters, int max_tokens,
                                     unsigned flags, cd_adapters **out);
