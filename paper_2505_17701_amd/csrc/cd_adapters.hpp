@@ -593,7 +593,7 @@ __device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, i
 }
 
 // The low-rank latents of a tile of MT * 16 tokens and RT * 16 ranks (blockIdx.y the ranks;
-// blockIdx.z: with both, 0 is glat). Eight waves split the contraction in blocks of 128
+// blockIdx.z: with both, 0 is glat). The waves split the contraction in blocks of 128
 // columns, and their sums meet in LDS. The scale is applied here. Tokens past the tile's last
 // and ranks past the last repeat another: they only reach sums of their own, which are not
 // stored. At rank 32 bound by reading x (16384 tokens of 4096 in 36 us, 34 without the
@@ -602,15 +602,13 @@ __device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, i
 // without). Neither more blocks in flight nor more waves change that, and tiles of one adapter
 // on one XCD, whose L2 would hold the factor, cost more on the side of x (110 us): tiles that
 // run at the same time then lie far apart.
-constexpr int kAdShrinkBlock = 512, kAdShrinkWaves = kAdShrinkBlock / cdk::kWave;
-
-template <int MT, int RT>
-__global__ __launch_bounds__(kAdShrinkBlock, MT + RT <= 4 ? 4 : 2) void k_ad_shrink(const AdArgs a, int kinds)
+template <int MT, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * cdk::kWave, MT + RT <= 4 ? 4 : 2) void k_ad_shrink(const AdArgs a, int kinds)
 {
-    static_assert(MT * RT * cdk::kWave <= kAdShrinkBlock, "one sum per thread");
+    static_assert(MT * RT <= WAVES, "one sum per thread");
     constexpr int kSums = MT * RT * cdk::kWave;
     constexpr int kDepth = MT + RT <= 2 ? 2 : 1;  // blocks in flight
-    __shared__ u32x4 lds[kAdShrinkWaves * (kSums > kAdStage ? kSums : kAdStage)];
+    __shared__ u32x4 lds[WAVES * (kSums > kAdStage ? kSums : kAdStage)];
     const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
     const AdTile tile = a.tiles[blockIdx.x / sub];
     const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
@@ -656,7 +654,7 @@ __global__ __launch_bounds__(kAdShrinkBlock, MT + RT <= 4 ? 4 : 2) void k_ad_shr
         for (int j = 0; j < RT; ++j)
             acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 *stage = lds + wave * kAdStage;
-    constexpr int kStep = 128 * kAdShrinkWaves;
+    constexpr int kStep = 128 * WAVES;
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d)
         if (wave * 128 + d * kStep < K)
@@ -698,7 +696,7 @@ __global__ __launch_bounds__(kAdShrinkBlock, MT + RT <= 4 ? 4 : 2) void k_ad_shr
         return;
     f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < kAdShrinkWaves; ++w)
+    for (int w = 0; w < WAVES; ++w)
         v += sums[w * kSums + threadIdx.x];
     v *= ad_scale(a, tile.group);
     // this thread: token i * 16 + m, ranks r .. r + 3
@@ -1237,19 +1235,26 @@ void ad_group(const AdArgs &a, bool transpose, hipStream_t s)
 // kinds: 1 lat, 2 glat, 3 both
 void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
 {
-    const int mt = a.tile / 16, slots = ad_slots(a);
-    const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
-    const int m = std::min(mt, 2);  // sums of a workgroup: one per thread
-    const dim3 grid(slots * (mt / m), ad_ceil(a.rank, rt * 16), kinds == 3 ? 2 : 1);
-#define AD_SHRINK(M, R) \
-    if (m == M && rt == R) \
-        k_ad_shrink<M, R><<<grid, kAdShrinkBlock, 0, s>>>(a, kinds)
-    AD_SHRINK(1, 1);
-    AD_SHRINK(2, 1);
-    AD_SHRINK(1, 2);
-    AD_SHRINK(2, 2);
-    AD_SHRINK(1, 4);
-    AD_SHRINK(2, 4);
+    const int mt = a.tile / 16, slots = ad_slots(a), both = kinds == 3 ? 2 : 1;
+    // While 16 ranks a workgroup make no more of them than CUs: so, with sixteen waves each. Rank 32
+    // over 13528 columns, 32 tokens (backward, us a call) 24.7 against 29.9, 512 tokens 29.1
+    // against 33.8; rank 48 over 4096, 512 tokens (246 workgroups) 32.4 against 33.3, 1024 tokens
+    // (438) 43.0 against 39.4. (The backward call counts both latents, whichever it needs: a
+    // gradient's sums are the same alone and together.)
+    const bool few = slots * (a.dy ? 2 : 1) * ad_ceil(a.rank, 16) <= 256;
+    const int rt = a.rank <= 16 || few ? 1 : a.rank <= 32 ? 2 : 4;
+    const int m = std::min(mt, 2);  // sums of a workgroup: at most one per thread
+    const dim3 grid(slots * (mt / m), ad_ceil(a.rank, rt * 16), both);
+#define AD_SHRINK(M, R, W) \
+    if (m == M && rt == R && few == (W == 16)) \
+        k_ad_shrink<M, R, W><<<grid, W * cdk::kWave, 0, s>>>(a, kinds)
+    AD_SHRINK(1, 1, 16);
+    AD_SHRINK(1, 1, 8);
+    AD_SHRINK(1, 2, 8);
+    AD_SHRINK(1, 4, 8);
+    AD_SHRINK(2, 1, 8);
+    AD_SHRINK(2, 2, 8);
+    AD_SHRINK(2, 4, 8);
 #undef AD_SHRINK
 }
 
