@@ -394,6 +394,58 @@ def test_two_pools_on_two_streams(cd):
         p.close()
 
 
+@pytest.mark.parametrize("T,rank", [(3, 24), (45, 24), (1301, 72), (2600, 16)])
+def test_nothing_stays_from_the_call_before(cd, T, rank):
+    """A pool after a longer call full of NaN gives a fresh pool's bits, and so do two graphs
+    that share it, replayed in turn."""
+    long = Case(40, 5000, 264, 520, rank, 5).dev()
+    pool = cd.Adapters(264, 520, rank, 5, max_tokens=5000, train=True)
+    cases = [Case(41 + i, T - i, 264, 520, rank, 5, how=how).dev()
+             for i, how in enumerate(("mixed", "runs"))]
+
+    def calls(p, c):
+        args = (c.ids, c.A, c.B, c.scale)
+        return [cd.countdown_adapters_add(p, c.x, *args, base=c.base),
+                *cd.countdown_adapters_backward(p, c.x, c.dy, *args),
+                cd.countdown_adapters_project(p, c.x[:16], c.W, c.ids[:16], *args[1:])]
+
+    want = []
+    for c in cases:
+        fresh = cd.Adapters(264, 520, rank, 5, max_tokens=T, train=True)
+        want.append(calls(fresh, c))
+        torch.cuda.synchronize()
+        fresh.close()
+
+    def spoil():
+        calls(pool, long)
+        torch.cuda.synchronize()
+
+    long.x.fill_(float("nan"))
+    long.dy.fill_(float("nan"))
+    for w, c in zip(want, cases):
+        spoil()
+        for a, b in zip(w, calls(pool, c)):
+            assert torch.equal(a, b)
+    graphs, got = [], []
+    stream = torch.cuda.Stream()
+    for c in cases:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            got.append(calls(pool, c))
+    for _ in range(3):
+        spoil()
+        for ts in got:
+            for t in ts:
+                t.fill_(7.0)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for w, v in zip(want, got):
+            for a, b in zip(w, v):
+                assert torch.equal(a, b)
+    pool.close()
+
+
 def test_binding_refusals(cd):
     c = Case(30, 8, 64, 72, 8, 2)
     d = c.dev()
