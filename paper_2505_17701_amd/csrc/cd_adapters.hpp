@@ -28,7 +28,7 @@ using cdk::u32x4;
 struct AdGroup {
     int first, count;
 };
-// A tile of tokens of one group (count 0: an unused slot).
+// A tile of tokens of one group (count 0: an unused slot), or all of them.
 struct AdTile {
     int group, first, count, pad;
 };
@@ -55,6 +55,7 @@ struct AdArgs {
     int *order;       // token at each position
     AdGroup *groups;  // [n + 1]
     AdTile *tiles;
+    AdTile *by_size;  // all tokens of each adapter, those with most of them first (training)
     uint16_t *Bt;            // [n][rank][d_out], B transposed (training)
     uint16_t *latT, *glatT;  // lat and glat split in three bf16 terms (ad_term_at; training)
     int tile;    // tokens of a tile: 16 or 32
@@ -592,6 +593,30 @@ __device__ __forceinline__ size_t ad_term_at(const AdArgs &a, size_t p, int s, i
     return ((p / 32 * 3 + s) * rts + r / 16) * 512 + ((p % 32 / 8) * 16 + r % 16) * 8 + p % 8;
 }
 
+// a.by_size for 64 adapters, a lane each: its place is the number of adapters that come before
+// it, of which every wave counts a part.
+template <int WAVES>
+__device__ __forceinline__ void ad_by_size(const AdArgs &a, int block, int *before)
+{
+    const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
+    const int i = block * cdk::kWave + lane;
+    const AdGroup mine = a.groups[min(i, a.n - 1)];
+    int place = 0;
+#pragma unroll 8
+    for (int j = wave; j < a.n; j += WAVES) {
+        const int other = a.groups[j].count;
+        place += other > mine.count || (other == mine.count && j < i);
+    }
+    before[threadIdx.x] = place;
+    __syncthreads();
+    if (wave || i >= a.n)
+        return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w)
+        place += before[w * cdk::kWave + lane];
+    a.by_size[place] = AdTile{i, mine.first, mine.count, 0};
+}
+
 // The low-rank latents of a tile of MT * 16 tokens and RT * 16 ranks (blockIdx.y the ranks;
 // blockIdx.z: with both, 0 is glat). The waves split the contraction in blocks of 128
 // columns, and their sums meet in LDS. The scale is applied here. Tokens past the tile's last
@@ -610,6 +635,12 @@ __global__ __launch_bounds__(WAVES * cdk::kWave, MT + RT <= 4 ? 4 : 2) void k_ad
     constexpr int kDepth = MT + RT <= 2 ? 2 : 1;  // blocks in flight
     __shared__ u32x4 lds[WAVES * (kSums > kAdStage ? kSums : kAdStage)];
     const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
+    const int spare = blockIdx.x - (a.T / a.tile + a.n + 1) * sub;  // workgroups past the tiles: a.by_size
+    if (spare >= 0) {
+        if (blockIdx.y == 0 && blockIdx.z == 0)
+            ad_by_size<WAVES>(a, spare, reinterpret_cast<int *>(lds));
+        return;
+    }
     const AdTile tile = a.tiles[blockIdx.x / sub];
     const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
     if (count <= 0 || tile.group == a.n)
@@ -932,7 +963,7 @@ __device__ __forceinline__ void ad_dx(const AdArgs &a, int part, int slice, int 
 // 16 ranks in each of four waves fetch the columns four times through L1 (170); two tiles of
 // columns a workgroup, 4 waves, or 64 tokens in flight change little (118 to 139).
 template <int RT, int WR, bool DB>
-__device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int parts, f32x4_t *lds)
+__device__ __forceinline__ void ad_outer(const AdArgs &a, const AdTile &grp, int block, int parts, f32x4_t *lds)
 {
     constexpr int WT = kAdBackWaves / WR;
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
@@ -941,11 +972,9 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int parts, 
     const int tokens = block / 8 % parts;        // of the workgroups that share them
     const int width = DB ? a.d_out : a.d_in;
     const int rts = (a.rank + 15) / 16, rgs = (rts + RT * WR - 1) / (RT * WR);
-    // eight neighbouring workgroups (one on each XCD) take neighbouring columns; then come the
-    // other adapters, of whose sizes nothing is known, and the other ranks
-    const int y = block / 8 / parts, ad = y % a.n, rt0 = (y / a.n % rgs * WR + part) * RT;
-    const int c0 = (y / a.n / rgs * 8 + block % 8) * 128, col = c0 + m * 8;
-    const AdGroup grp = a.groups[ad];
+    // eight neighbouring workgroups (one on each XCD) take neighbouring columns
+    const int y = block / 8 / parts, rt0 = (y % rgs * WR + part) * RT;
+    const int c0 = (y / rgs * 8 + block % 8) * 128, col = c0 + m * 8;
     const uint16_t *src = DB ? a.dy : a.x;
     const size_t ld = DB ? a.lddy : a.ldx;
     const uint16_t *fac = DB ? a.latT : a.glatT;
@@ -1045,7 +1074,7 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int parts, 
             if (cok && r < a.rank)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<f32x4_t *>(dst + ((size_t)ad * a.d_out + col + j) * a.rank + r) =
+                    *reinterpret_cast<f32x4_t *>(dst + ((size_t)grp.group * a.d_out + col + j) * a.rank + r) =
                         acc[i][j];
         } else {  // row r = m, columns c0 + 8 (4 g + q) + j
             const int r = (rt0 + i) * 16 + m;
@@ -1054,7 +1083,7 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int parts, 
                 for (int q = 0; q < 4; ++q) {
                     const int c = c0 + 8 * (4 * g + q);
                     if (c < a.d_in) {
-                        f32x4_t *d = reinterpret_cast<f32x4_t *>(dst + ((size_t)ad * a.rank + r) * a.d_in + c);
+                        f32x4_t *d = reinterpret_cast<f32x4_t *>(dst + ((size_t)grp.group * a.rank + r) * a.d_in + c);
                         d[0] = f32x4_t{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
                         d[1] = f32x4_t{acc[i][4][q], acc[i][5][q], acc[i][6][q], acc[i][7][q]};
                     }
@@ -1063,20 +1092,30 @@ __device__ __forceinline__ void ad_outer(const AdArgs &a, int block, int parts, 
     }
 }
 
-// Workgroups [0, nB) compute dB, the next nA dA, the others dx (`slices` of its columns): one
-// launch for small calls' sake, and the kinds wait for different things.
+// Workgroups take the adapters by their tokens, the most first: nB for dB and nA for dA of each.
+// The others compute dx (`slices` of its columns). One launch for small calls' sake, and
+// because the kinds wait for different things. A workgroup goes over all tokens of its
+// adapter, so one of a large adapter must not start late; and those that run together read
+// the same terms. Against the adapters in their own order, side by side (us a launch): 8192 tokens of
+// 4096 and 14336, rank 64, 16 uneven requests of 8 adapters 134 against 170; 4096 tokens of
+// 4096, rank 16, 4 adapters 31.9 against 38.6. 1024 adapters of 8 tokens each lose (us a call):
+// 1243 against 1192.
 template <int RT, int WR, int KC>
 __global__ __launch_bounds__(kAdBackWaves * cdk::kWave, 2) void k_ad_back(const AdArgs a, int nB, int nA,
                                                                       int parts, int slices)
 {
     __shared__ f32x4_t lds[kAdBackWaves / 2 * 8 * cdk::kWave];
-    const int b = blockIdx.x;
-    if (b < nB)
-        ad_outer<RT, WR, true>(a, b, parts, lds);
-    else if (b < nB + nA)
-        ad_outer<RT, WR, false>(a, b - nB, parts, lds);
+    const int b = blockIdx.x, grads = (nB + nA) * a.n;
+    if (b >= grads) {
+        ad_dx<KC>(a, (b - grads) / slices, (b - grads) % slices, slices);
+        return;
+    }
+    const AdTile grp = a.by_size[b / (nB + nA)];
+    const int i = b % (nB + nA);
+    if (i < nB)
+        ad_outer<RT, WR, true>(a, grp, i, parts, lds);
     else
-        ad_dx<KC>(a, (b - nB - nA) / slices, (b - nB - nA) % slices, slices);
+        ad_outer<RT, WR, false>(a, grp, i - nB, parts, lds);
 }
 
 // dB and dA (nb and na elements) from their parts
@@ -1139,6 +1178,7 @@ struct cd_adapters {
     int *order;
     AdGroup *groups;
     AdTile *tiles;
+    AdTile *by_size;
     uint16_t *Bt, *latT, *glatT;
     float *part;
 };
@@ -1244,7 +1284,7 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
     const bool few = slots * (a.dy ? 2 : 1) * ad_ceil(a.rank, 16) <= 256;
     const int rt = a.rank <= 16 || few ? 1 : a.rank <= 32 ? 2 : 4;
     const int m = std::min(mt, 2);  // sums of a workgroup: at most one per thread
-    const dim3 grid(slots * (mt / m), ad_ceil(a.rank, rt * 16), both);
+    const dim3 grid(slots * (mt / m) + (a.by_size ? ad_ceil(a.n, cdk::kWave) : 0), ad_ceil(a.rank, rt * 16), both);
 #define AD_SHRINK(M, R, W) \
     if (m == M && rt == R && few == (W == 16)) \
         k_ad_shrink<M, R, W><<<grid, W * cdk::kWave, 0, s>>>(a, kinds)
@@ -1299,12 +1339,12 @@ void ad_back(const AdArgs &a, hipStream_t s)
     if (tiles128 <= 128 && (a.dA || a.dB))
         parts = std::max(1, (int)std::min<size_t>({(size_t)(256 / tiles128), (size_t)(a.T / (2 * 32 * WT)),
                                                    kAdPartFloats / whole}));
-    const int nA = a.dA ? a.n * rgs * ad_ceil(a.d_in, 8 * 128) * 8 * parts : 0;
-    const int nB = a.dB ? a.n * rgs * ad_ceil(a.d_out, 8 * 128) * 8 * parts : 0;
+    const int nA = a.dA ? rgs * ad_ceil(a.d_in, 8 * 128) * 8 * parts : 0;
+    const int nB = a.dB ? rgs * ad_ceil(a.d_out, 8 * 128) * 8 * parts : 0;
     const int tiles = ad_slots(a) * (a.tile / 16);
     const int slices = a.out ? ad_slices(a.d_in, kAdBackWaves, tiles) : 1;
     const int nX = a.out ? tiles * slices : 0;
-    k_ad_back<RT, WR, KC><<<nB + nA + nX, kAdBackWaves * cdk::kWave, 0, s>>>(a, nB, nA, parts, slices);
+    k_ad_back<RT, WR, KC><<<a.n * (nB + nA) + nX, kAdBackWaves * cdk::kWave, 0, s>>>(a, nB, nA, parts, slices);
     if (parts > 1)
         k_ad_sum<<<std::min<size_t>(1024, (whole / 4 + kAdBlock - 1) / kAdBlock), kAdBlock, 0, s>>>(
             a.part, parts, a.dB, a.dB ? (size_t)a.n * a.rank * a.d_out : 0, a.dA,
@@ -1346,11 +1386,12 @@ cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapter
     const size_t copy = (size_t)n_adapters * rank * d_out * sizeof(uint16_t);
     const size_t parts[] = {lat,   pos * sizeof(int),  tiles,             groups,
                             train ? lat : 0, train ? terms : 0, train ? terms : 0, train ? copy : 0,
-                            train ? kAdPartFloats * sizeof(float) : 0};
-    size_t at[10] = {0};
-    for (int i = 0; i < 9; ++i)
+                            train ? kAdPartFloats * sizeof(float) : 0,
+                            train ? n_adapters * sizeof(AdTile) : 0};
+    size_t at[11] = {0};
+    for (int i = 0; i < 10; ++i)
         at[i + 1] = at[i] + (parts[i] + 255) / 256 * 256;
-    if (hip_status(hipMalloc(&p->ws, at[9])) != CD_OK) {
+    if (hip_status(hipMalloc(&p->ws, at[10])) != CD_OK) {
         delete p;
         return CD_ENOMEM;
     }
@@ -1365,6 +1406,7 @@ cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapter
         p->glatT = reinterpret_cast<uint16_t *>(ws + at[6]);
         p->Bt = reinterpret_cast<uint16_t *>(ws + at[7]);
         p->part = reinterpret_cast<float *>(ws + at[8]);
+        p->by_size = reinterpret_cast<AdTile *>(ws + at[9]);
     }
     *out = p;
     return CD_OK;
@@ -1499,6 +1541,7 @@ cd_status countdown_adapters_backward(cd_adapters *p, const uint16_t *x, size_t 
     a.latT = p->latT;
     a.glatT = dA ? p->glatT : nullptr;
     a.part = p->part;
+    a.by_size = dA || dB ? p->by_size : nullptr;
     // Two launches instead of three while a workgroup reads a token's factors in a moment (us a
     // call, tokens 1 / 8 / 16, grouped 64): 4096 -> 4096 rank 16, four adapters 15.7 16.2 16.4
     // against 17.9 19.0 19.2; 688 -> 256 rank 64 16.4 16.9 17.3 against 18.7; 1024 -> 3000 rank 64
