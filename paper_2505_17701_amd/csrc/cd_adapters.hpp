@@ -623,10 +623,11 @@ __device__ __forceinline__ void ad_by_size(const AdArgs &a, int block, int *befo
 // and ranks past the last repeat another: they only reach sums of their own, which are not
 // stored. At rank 32 bound by reading x (16384 tokens of 4096 in 36 us, 34 without the
 // factor's loads; the last call's 134 MB of outputs are written back meanwhile), at rank 64
-// by the factor as well, which each tile reads again (8192 tokens of 4096 and 14336: 90 us, 70
-// without). Neither more blocks in flight nor more waves change that, and tiles of one adapter
-// on one XCD, whose L2 would hold the factor, cost more on the side of x (110 us): tiles that
-// run at the same time then lie far apart.
+// by the factor as well, which every XCD reads (8192 tokens of 4096 and 14336 in 8 equal adapters:
+// 83 us, 462 MB past L2 at 5.5 TB/s, of them x and dy 302). Neither more blocks in flight nor
+// more waves change that; 64 tokens a tile (104 us against 94) and half the ranks a workgroup (97)
+// do not pay; and tiles of one adapter on one XCD, whose L2 would hold the factor, cost more on
+// the side of x (110): tiles that run at the same time then lie far apart.
 template <int MT, int RT, int WAVES>
 __global__ __launch_bounds__(WAVES * cdk::kWave, MT + RT <= 4 ? 4 : 2) void k_ad_shrink(const AdArgs a, int kinds)
 {
@@ -802,6 +803,8 @@ struct AdTokens {
 // read as they lie. Bound by memory: 16384 tokens of 4096 bf16 outputs, 268 MB, in 58 us
 // (4.6 TB/s; a copy runs at 4.8). 32 tokens a wave read B half as often, but need the
 // registers of a second wave on the SIMD: 64 to 91 us.
+// The launch bounds leave KC 0 in fp32 a spill of 28 bytes: 63 us for 4096 tokens of 4096 outputs at rank
+// 128, with two waves a SIMD and no spill 67.
 template <int KC, bool F32>
 __global__ __launch_bounds__(kAdBlock, KC == 1 && !F32 ? 4 : 3) void k_ad_expand(const AdArgs a)
 {
@@ -956,12 +959,12 @@ __device__ __forceinline__ void ad_dx(const AdArgs &a, int part, int slice, int 
 // transposes them. A workgroup has 128 columns; its eight waves are WR parts of RT * 16 ranks
 // and the rest parts of the tokens, whose sums meet in LDS. Where that leaves CUs without a
 // workgroup, `parts` workgroups share the tokens as well, each with sums of its own in
-// a.part, and k_ad_sum adds them in order. 4096 tokens of 4096 and 4096 columns at rank 16:
-// 18 us (67 MB, 3.7 TB/s); 8192 tokens of 4096 and 14336 at rank 64, in equal adapters: 120
-// us, with 459 MB fetched past L2: the columns once (302) and the terms (6 MB, from
-// neighbouring columns over and over) where L2 has lost them. 64 ranks in a wave spill (200),
-// 16 ranks in each of four waves fetch the columns four times through L1 (170); two tiles of
-// columns a workgroup, 4 waves, or 64 tokens in flight change little (118 to 139).
+// a.part, and k_ad_sum adds them in order. 4096 tokens of 4096 and 4096 columns at rank 16, in
+// equal adapters: 14.4 us (67 MB, 4.7 TB/s); 8192 tokens of 4096 and 14336 at rank 64: 112 us,
+// with 363 MB fetched past L2: the columns once (302) and the terms (6 MB, from
+// neighbouring columns over and over) where an L2 has not had them. 64 ranks in a wave spill,
+// 16 ranks in each of four waves fetch the columns four times through L1; two tiles of
+// columns a workgroup, 4 waves, or 64 tokens in flight change little.
 template <int RT, int WR, bool DB>
 __device__ __forceinline__ void ad_outer(const AdArgs &a, const AdTile &grp, int block, int parts, f32x4_t *lds)
 {
