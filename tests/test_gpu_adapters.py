@@ -217,6 +217,26 @@ def test_backward(cd, shape, dx_type):
                                                           need=(False, False, True))[2], dB)
 
 
+@pytest.mark.parametrize("shape", [(16385, 64, 72, 40, 7, "runs"), (33001, 72, 64, 48, 70, "mixed"),
+                                   (40000, 64, 64, 32, 2, "one")])
+def test_more_tokens_than_a_batch_of_ids(cd, shape):
+    """More than 16 x 1024 tokens: a wave's run of ids is read in several batches, the last
+    in part."""
+    c = Case(6, *shape)
+    delta, mag = c.delta()
+    want = c.grads()
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=c.T, train=True) as pool:
+        y = cd.countdown_adapters_add(pool, d.x, d.ids, d.A, d.B, d.scale, base=d.base)
+        check(y, delta + c.base.double(), mag + c.base.double().abs(), c.di + c.r, "y")
+        dx, dA, dB = cd.countdown_adapters_backward(pool, d.x, d.dy, d.ids, d.A, d.B, d.scale,
+                                                    base=d.dbase)
+        v, m, n = want["dx"]
+        check(dx, v + c.dbase.double(), m + c.dbase.double().abs(), n, "dx")
+        check(dA, *want["dA"], "dA")
+        check(dB, *want["dB"], "dB")
+
+
 def test_gradients_against_differences(cd):
     """<dy, y> is linear in each of x, A, B: its central difference over a step in one
     element (from -4 to 4, both bf16) is the gradient, but for the rounding of y and of it."""
