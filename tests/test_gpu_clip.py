@@ -116,6 +116,42 @@ def test_offsets_and_alignment(cd):
             assert bool((dst[left] == 5.0).all())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("sizes", [[65536], [65535, 1], [65537], [4096] * 16, [4097] * 15, [2049] * 31,
+                                   [1] * 32, [4095, 4096, 4097, 1, 0, 9, 30000]])
+def test_one_workgroup_and_its_edges(cd, sizes, dtype):
+    """Up to 65536 elements, one or two chunks a wave: views at odd offsets, outputs at the
+    same alignment, at another and in place."""
+    total = sum(n + 3 for n in sizes)
+    flat = make(6, [total + 16], (dtype,))[0]
+    starts = [1 + sum(m + 3 for m in sizes[:i]) for i in range(len(sizes))]
+    views = lambda buf, shift: [buf[s + shift:s + shift + n]  # noqa: E731
+                                for s, n in zip(starts, sizes)]
+    grads = views(flat, 0)
+    inside = torch.zeros(total + 16, dtype=torch.bool, device="cuda")
+    with cd.GradClip(len(sizes)) as clip:
+        for top in (0.5, 1e30, math.inf):
+            for shift in (0, 1, 8):
+                dst = torch.full((total + 16,), 5.0, dtype=dtype, device="cuda")
+                norm = cd.countdown_clip_grads(clip, grads, top, out=views(dst, shift))
+                check_norm(norm, grads)
+                coef = min(1.0, top / float(norm))
+                for o, t in zip(views(dst, shift), grads):
+                    check_scaled(o, t, coef)
+                    assert coef < 1.0 or torch.equal(o, t)
+                inside.zero_()
+                for v in views(inside, shift):
+                    v.fill_(True)
+                assert bool((dst[~inside] == 5.0).all())
+        place = flat.clone()
+        norm = cd.countdown_clip_grads(clip, views(place, 0), 0.5)
+        want = torch.empty_like(flat).copy_(flat)
+        cd.countdown_clip_grads(clip, grads, 0.5, out=views(want, 0))
+        assert torch.equal(place, want)
+        for o, t in zip(views(place, 0), grads):
+            check_scaled(o, t, min(1.0, 0.5 / float(norm)))
+
+
 @pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_bad_numbers_leave_the_gradients(cd, bad, dtype):
