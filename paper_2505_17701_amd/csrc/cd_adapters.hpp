@@ -409,6 +409,7 @@ __global__ __launch_bounds__(kAdBlock) void k_ad_few_back(const AdArgs a, int nB
 // operand; the waves' sums meet in LDS, where the adapters' part is added. Rows past the
 // last and tokens past T repeat the last one: they only reach sums of their own.
 constexpr int kAdProjBlock = 512, kAdProjWaves = kAdProjBlock / cdk::kWave;
+constexpr int kAdOwnLatents = 32;
 
 // OWN: every workgroup forms the latents again, while its first columns of W are on their way.
 // NT: W past the caches.
@@ -416,7 +417,7 @@ template <bool OWN, bool NT>
 __global__ __launch_bounds__(kAdProjBlock) void k_ad_project(const AdArgs a)
 {
     __shared__ u32x4 lds[kAdProjWaves][kAdStage];
-    __shared__ float own[OWN ? kAdDecodeTokens * kAdMaxRank : 1];
+    __shared__ float own[OWN ? kAdOwnLatents : 1];
     const int lane = threadIdx.x % cdk::kWave, wave = ad_wave();
     const int m = lane % 16, g = lane / 16;
     const int o0 = blockIdx.x * 16;
@@ -1462,9 +1463,14 @@ cd_status countdown_adapters_project(cd_adapters *p, const uint16_t *x, size_t l
     if (T == 0)
         return CD_OK;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    // Few latents every workgroup forms for itself: 4096 x 4096 at one token, rank 16 (2^16 products)
-    // 11.0 us a call against 12.6 with a launch of their own.
-    const bool own = (int64_t)T * a.rank * a.d_in <= 1 << 17;
+    // Few latents every workgroup forms for itself, one after another, before its sums are whole;
+    // with more workgroups than the CUs hold at once (512) that comes twice. Captured / eager us a call
+    // against a launch of their own:
+    //   16 latents, 4096 -> 4096  8.4 /  8.2 against  9.0 /  9.2   4096 -> 14336 28.5 / 28.8 against 22.6 / 23.0
+    //   32 latents, 1000 -> 4096  5.4 /  7.3 against  5.2 / 10.2   4096 ->  4096 10.7 / 10.6 against  9.1 /  9.9
+    //   64 latents, 1000 -> 4096  7.8 /  7.7 against  5.3 /  9.7
+    const int latents = T * a.rank;
+    const bool own = latents <= kAdOwnLatents && latents * a.d_in <= 1 << 16 && a.d_out <= 512 * 16;
     // A W that would sweep most of the last-level cache goes past it: 117 MB (4096 x 14336, 8
     // tokens) 24.7 us against 27.1; 48 MB that was still there from the last call, 14.9 against 11.9.
     const bool nt = (size_t)a.d_in * a.d_out * sizeof(uint16_t) > ((size_t)64 << 20);

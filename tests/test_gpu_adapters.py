@@ -166,6 +166,22 @@ def test_project(cd, shape, y_type):
             assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("shape", [
+    (1, 8192, 4104, 8, 2, "one"), (3, 4096, 8208, 16, 4, "mixed"),  # W past the caches
+    (2, 2048, 8192, 16, 3, "one"), (2, 2048, 8200, 16, 3, "one"),  # one launch, two by d_out,
+    (4, 2056, 264, 8, 3, "mixed"), (3, 264, 264, 16, 3, "mixed"),  # by the work, by the latents
+])
+def test_project_by_its_paths(cd, shape):
+    c = Case(7, *shape)
+    ref, mag = c.delta()
+    ref = ref + c.x.double() @ c.W.double().t()
+    mag = mag + c.x.double().abs() @ c.W.double().abs().t()
+    d = c.dev()
+    with cd.Adapters(c.di, c.do, c.r, c.n, max_tokens=16) as pool:
+        y = cd.countdown_adapters_project(pool, d.x, d.W, d.ids, d.A, d.B, d.scale)
+        check(y, ref, mag, c.di + c.r, "y")
+
+
 @pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("shape", SHAPES + LONG + BIG)
 def test_add(cd, shape, y_type):
