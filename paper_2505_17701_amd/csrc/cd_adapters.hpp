@@ -270,8 +270,7 @@ __global__ __launch_bounds__(kAdTokenBlock) void k_ad_token(const AdArgs a)
 
 // The backward call on few tokens, without grouping: a workgroup per token forms lat
 // (blockIdx.y + kind 0) and glat (1), the next launch everything else.
-constexpr int kAdFewTokens = 16;
-constexpr int kAdFewRanks = 32;  // of glat, summed at a time
+constexpr int kAdFewTokens = 16, kAdFewRanks = 32;
 
 __global__ __launch_bounds__(kAdTokenBlock) void k_ad_few_latents(const AdArgs a, int kind)
 {
@@ -288,38 +287,35 @@ __global__ __launch_bounds__(kAdTokenBlock) void k_ad_few_latents(const AdArgs a
         return;
     }
     const uint16_t *B = a.B + (size_t)id * a.d_out * a.rank, *dy = a.dy + (size_t)t * a.lddy;
-    for (int r0 = 0; r0 < a.rank; r0 += kAdFewRanks) {
-        float acc[kAdFewRanks];
+    float acc[kAdFewRanks];
 #pragma unroll
-        for (int k = 0; k < kAdFewRanks; ++k)
-            acc[k] = 0.0f;
+    for (int k = 0; k < kAdFewRanks; ++k)
+        acc[k] = 0.0f;
 #pragma unroll 2
-        for (int o = threadIdx.x; o < a.d_out; o += kAdTokenBlock) {
-            const float d = cdk::bf16_lo(dy[o]);
+    for (int o = threadIdx.x; o < a.d_out; o += kAdTokenBlock) {
+        const float d = cdk::bf16_lo(dy[o]);
 #pragma unroll
-            for (int c = 0; c < kAdFewRanks / 8; ++c) {
-                const u32x4 b = load16(or_zero(r0 + 8 * c < a.rank, B + (size_t)o * a.rank + r0 + 8 * c));
+        for (int c = 0; c < kAdFewRanks / 8; ++c) {
+            const u32x4 b = load16(or_zero(8 * c < a.rank, B + (size_t)o * a.rank + 8 * c));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc[8 * c + 2 * e] += d * cdk::bf16_lo(b[e]);
-                    acc[8 * c + 2 * e + 1] += d * cdk::bf16_hi(b[e]);
-                }
+            for (int e = 0; e < 4; ++e) {
+                acc[8 * c + 2 * e] += d * cdk::bf16_lo(b[e]);
+                acc[8 * c + 2 * e + 1] += d * cdk::bf16_hi(b[e]);
             }
         }
-        __syncthreads();  // (the last ranks' sums are read)
+    }
 #pragma unroll
-        for (int k = 0; k < kAdFewRanks; ++k) {
-            const float s = cdk::wave_sum(acc[k]);
-            if (lane == 0)
-                sums[wave][k] = s;
-        }
-        __syncthreads();
-        if (threadIdx.x < kAdFewRanks && r0 + (int)threadIdx.x < a.rank) {
-            float s = 0.0f;
-            for (int w = 0; w < kAdTokenBlock / cdk::kWave; ++w)
-                s += sums[w][threadIdx.x];
-            a.glat[t * a.rank + r0 + threadIdx.x] = s * ad_scale(a, id);
-        }
+    for (int k = 0; k < kAdFewRanks; ++k) {
+        const float s = cdk::wave_sum(acc[k]);
+        if (lane == 0)
+            sums[wave][k] = s;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < a.rank) {
+        float s = 0.0f;
+        for (int w = 0; w < kAdTokenBlock / cdk::kWave; ++w)
+            s += sums[w][threadIdx.x];
+        a.glat[t * a.rank + threadIdx.x] = s * ad_scale(a, id);
     }
 }
 
@@ -1561,12 +1557,17 @@ cd_status countdown_adapters_backward(cd_adapters *p, const uint16_t *x, size_t 
     a.glatT = dA ? p->glatT : nullptr;
     a.part = p->part;
     a.by_size = dA || dB ? p->by_size : nullptr;
-    // Two launches instead of three while a workgroup reads a token's factors in a moment (us a
-    // call, tokens 1 / 8 / 16, grouped 64): 4096 -> 4096 rank 16, four adapters 15.7 16.2 16.4
-    // against 17.9 19.0 19.2; 688 -> 256 rank 64 16.4 16.9 17.3 against 18.7; 1024 -> 3000 rank 64
-    // 26.0 27.0 28.6 against 20.6 21.7 21.3. With more tokens of one adapter its row's sum is a
-    // long chain: 4096 -> 4096 rank 8, one adapter, 32 tokens 21.4 against 18.5.
-    if (T <= kAdFewTokens && (int64_t)a.rank * std::max(a.d_in, a.d_out) <= 1 << 17) {
+    // Two launches instead of three while a workgroup reads a token's factors in a moment, and the
+    // tokens of one adapter, one after another in its rows' sums, are few. Captured / eager us a call
+    // against the three:
+    //    1 token,  4096 -> 4096 rank 16, one adapter  10.1 / 10.8 against 13.1 / 13.7
+    //    8 tokens, 4096 -> 4096 rank 16, one adapter  12.6 / 13.0 against 13.0 / 13.9 (16: 16.1 against 13.4)
+    //   16 tokens, 4096 -> 4096 rank 16, four         11.1 / 11.5 against 16.4 / 17.2
+    //    1 token,  2048 -> 14336, one: rank 24        15.5 / 15.8 against 20.9 / 21.5, rank 32 22.3 / 22.6 against 21.1 / 21.6
+    //    8 tokens, 4096 -> 4096 rank 32, one adapter  14.8 / 15.1 against 14.8 / 15.4
+    //    8 tokens, 4096 -> 4096 rank 40, one adapter  19.9 / 20.2 against 14.4 / 15.1 (256 -> 688 15.8 against 12.1)
+    if (T <= std::min(kAdFewTokens, 8 * a.n) && a.rank <= kAdFewRanks &&
+        a.rank * std::max(a.d_in, a.d_out) <= 3 << 17) {
         k_ad_few_latents<<<dim3(T, back && dB ? 2 : 1), kAdTokenBlock, 0, s>>>(a, dB ? 0 : 1);
         const int nB = dB ? a.n * ad_ceil(a.d_out * (a.rank / 8), kAdBlock) : 0;
         const int nA = dA ? a.n * ad_ceil(a.rank * (a.d_in / 8), kAdBlock) : 0;

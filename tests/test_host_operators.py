@@ -102,12 +102,17 @@ def test_launches_by_the_work(host):
                            ((8, 8, 8, 1), 200000, ["k_ad_token"])]:
         assert kernels(add, (*sizes, T), T=T, ldb=sizes[1], ldy=sizes[1]) == want, (sizes, T)
     for sizes, T, want in [((4096, 4096, 16, 8), 1, ["k_ad_project"]),
-                           ((4096, 4096, 16, 8), 8, ["k_ad_lat", "k_ad_project"])]:
+                           ((4096, 4096, 16, 8), 8, ["k_ad_lat", "k_ad_project"]),
+                           ((1000, 8192, 16, 8), 2, ["k_ad_project"]),
+                           ((1000, 8200, 16, 8), 2, ["k_ad_lat", "k_ad_project"]),
+                           ((1000, 1024, 40, 8), 1, ["k_ad_lat", "k_ad_project"])]:
         assert kernels(project, (*sizes, T), T=T, ldy=sizes[1]) == want
     back = ["k_ad_group", "k_ad_shrink", "k_ad_back"]
     for sizes, T, want in [((256, 688, 8, 3), 37, back), ((4096, 4096, 16, 4), 4096, back),
                            ((520, 1080, 40, 1), 4877, back + ["k_ad_sum"]),
                            ((4096, 4096, 16, 4), 16, ["k_ad_few_latents", "k_ad_few_back"]),
+                           ((4096, 4096, 16, 1), 8, ["k_ad_few_latents", "k_ad_few_back"]),
+                           ((4096, 4096, 16, 1), 9, back), ((256, 688, 40, 4), 1, back),
                            ((4096, 4096, 16, 4), 17, back), ((1024, 3000, 64, 4), 8, back)]:
         kw = dict(T=T, lddy=sizes[1], ldb=sizes[0], lddx=sizes[0])
         assert kernels(backward, (*sizes, T), **kw) == want
