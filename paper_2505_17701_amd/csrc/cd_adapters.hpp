@@ -1497,18 +1497,22 @@ cd_status countdown_adapters_add(cd_adapters *p, const uint16_t *x, size_t ldx, 
     if (st != CD_OK || T == 0)
         return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    // How the tokens are taken (us a call, fp32 y, tokens 8 / 64 / 256 / 1024):
+    // How the tokens are taken (us an eager call, fp32 y, tokens 8 / 64 / 256 / 1024):
     //                          one launch            two launches          grouped
     //   4096 -> 4096, rank 16   8.4  8.3 12.5  41.6  11.2 11.5 11.0  28.0  14.8 15.4 15.7 21.5
     //   1024 -> 4096, rank 64   8.3  9.2 27.0 101.3  10.8 10.7 22.1  77.7  16.1 17.2 17.8 23.7
     //   4096 -> 4096, rank 64  13.0 19.0 49.2 179.9   9.8 10.9 31.8  97.3  21.0 21.7 22.9 33.2
     // By token, every one reads its adapter again: once, or A again for each 1024 outputs, 16
-    // ranks at a time. The bounds below are where the columns cross.
+    // ranks at a time. The bounds below are where the columns cross. (Captured, where a second
+    // launch costs 1.6 us and not 2.9, rank 32 and more would rather take two: 5.2 against 7.2 for
+    // 4096 -> 4096, 16 tokens.) Two launches and grouped, captured: T r (d_in + d_out) of 40 M 11.0
+    // against 19.8 (4096 -> 1024, rank 128, 64 tokens) to 22.7 against 18.3 (1024 -> 4096); of 59 to 67 M
+    // 27.0 against 15.7 (256 -> 688, rank 64, 1024 tokens) to 16.5 against 14.6 (4096 -> 4096, rank 32, 256).
     const int64_t down = (int64_t)a.rank * a.d_in, up = (int64_t)a.rank * a.d_out;
     const int slices = ad_ceil(a.d_out, kAdTokenBlock);
     if (a.rank <= 64 && down <= 3 << 16 && T * (slices * down + up) < 3 << 24) {
         k_ad_token<<<dim3(T, slices), kAdTokenBlock, 0, s>>>(a);
-    } else if (T * (down + up) <= 1 << 26) {
+    } else if (T * (down + up) < 3 << 24) {
         k_ad_lat<<<ad_ceil(T * a.rank, kAdWaves), kAdBlock, 0, s>>>(a);
         k_ad_up<<<dim3(T, ad_ceil(a.d_out, kAdBlock)), kAdBlock, 0, s>>>(a);
     } else {

@@ -94,7 +94,8 @@ def test_launches_by_the_work(host):
     by_token, grouped = ["k_ad_lat", "k_ad_up"], ["k_ad_group", "k_ad_shrink", "k_ad_expand"]
     for sizes, T, want in [((4096, 4096, 16, 16), 8, ["k_ad_token"]),
                            ((4096, 4096, 16, 16), 128, ["k_ad_token"]),
-                           ((4096, 4096, 16, 16), 400, by_token),
+                           ((4096, 4096, 16, 16), 383, by_token),
+                           ((4096, 4096, 16, 16), 384, grouped),
                            ((4096, 4096, 16, 16), 1024, grouped),
                            ((4096, 4096, 64, 16), 1, by_token),
                            ((512, 1024, 128, 4), 1, by_token),
