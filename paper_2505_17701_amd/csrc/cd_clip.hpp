@@ -332,7 +332,7 @@ size_t clip_size(int type) { return type == CD_TYPE_F32 ? sizeof(float) : sizeof
 
 struct ClipSpan {
     uintptr_t lo, hi;
-    const void *grad;  // the tensor's own gradient
+    int tensor;  // (-1: the norm)
     bool operator<(const ClipSpan &o) const { return lo < o.lo; }
 };
 
@@ -344,11 +344,11 @@ bool clip_disjoint(const cd_grad *g, int n, bool scaled, const double *norm)
     for (int i = 0; i < n; ++i)
         if (g[i].count && g[i].out && (scaled || g[i].out != g[i].grad)) {
             const uintptr_t lo = reinterpret_cast<uintptr_t>(g[i].out);
-            outs.push_back({lo, lo + g[i].count * clip_size(g[i].type), g[i].grad});
+            outs.push_back({lo, lo + g[i].count * clip_size(g[i].type), i});
         }
     if (norm) {
         const uintptr_t lo = reinterpret_cast<uintptr_t>(norm);
-        outs.push_back({lo, lo + sizeof(double), nullptr});
+        outs.push_back({lo, lo + sizeof(double), -1});
     }
     std::sort(outs.begin(), outs.end());
     for (size_t i = 1; i < outs.size(); ++i)
@@ -360,11 +360,11 @@ bool clip_disjoint(const cd_grad *g, int n, bool scaled, const double *norm)
         const uintptr_t lo = reinterpret_cast<uintptr_t>(g[i].grad);
         const uintptr_t hi = lo + g[i].count * clip_size(g[i].type);
         // the outputs are disjoint: those that end after lo and start before hi
-        auto o = std::upper_bound(outs.begin(), outs.end(), ClipSpan{lo, 0, nullptr});
+        auto o = std::upper_bound(outs.begin(), outs.end(), ClipSpan{lo, 0, -1});
         if (o != outs.begin() && (o - 1)->hi > lo)
             --o;
         for (; o != outs.end() && o->lo < hi; ++o)
-            if (o->lo != lo || o->hi != hi || o->grad != g[i].grad)
+            if (o->lo != lo || o->tensor != i)
                 return false;
     }
     return true;
