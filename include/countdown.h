@@ -422,7 +422,9 @@ cd_status countdown_adapters_backward(cd_adapters *ad, const uint16_t *x, size_t
 /* ------------------------------------------------------------------------
  * The global gradient norm over many tensors, and clipping:
  *   norm = sqrt(sum over all tensors and elements of g^2)   (fp64),
- *   out  = g * fp32(max_norm / norm) if norm > max_norm, else g.
+ *   out  = g * (max_norm / norm) if norm > max_norm, else g.
+ * The quotient is rounded to 24 significant bits, also where it lies below fp32's normal
+ * numbers, the product to fp32 and then to the tensor's type.
  * A norm that is not finite (an infinity or NaN among the gradients) leaves
  * out = g; the caller sees it in *norm and can skip its step.
  */

@@ -168,10 +168,28 @@ __global__ __launch_bounds__(kClipBlock) void k_clip_total(const double *part, u
         *norm_out = norm;
 }
 
-// a norm that is not finite scales nothing
-__device__ __forceinline__ float clip_coef(double norm, double max_norm)
+// The scale max_norm / norm as an fp32 factor and a power of two: below fp32's normal numbers
+// (gradients of 3e38 clipped to 1) the quotient alone would lose its bits, or all of it
+struct ClipCoef {
+    float f;
+    int e;  // 0 for the usual quotient, and out = grad * f
+};
+
+// a norm that is not finite scales nothing (norm is uniform)
+__device__ __forceinline__ ClipCoef clip_coef(double norm, double max_norm)
 {
-    return norm > max_norm && norm < (double)INFINITY ? (float)(max_norm / norm) : 1.0f;
+    const double c = norm > max_norm && norm < (double)INFINITY ? max_norm / norm : 1.0;
+    const bool low = c < (double)__FLT_MIN__;
+    const float f = (float)(low ? __builtin_amdgcn_frexp_mant(c) : c);
+    return {__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f))),
+            __builtin_amdgcn_readfirstlane(low ? __builtin_amdgcn_frexp_exp(c) : 0)};
+}
+
+__device__ __forceinline__ bool clip_same(const ClipCoef &c) { return c.f == 1.0f && c.e == 0; }
+
+__device__ __forceinline__ float clip_mul(float v, const ClipCoef &c)
+{
+    return __builtin_amdgcn_ldexpf(v * c.f, c.e);
 }
 
 __device__ __forceinline__ uint32_t bf16_bits(float v)
@@ -182,50 +200,50 @@ __device__ __forceinline__ float clip_round(float v, float) { return v; }
 __device__ __forceinline__ uint16_t clip_round(float v, uint16_t) { return (uint16_t)bf16_bits(v); }
 
 template <class T>
-__device__ __forceinline__ cdk::u32x4 scale16(cdk::u32x4 v, float coef)
+__device__ __forceinline__ cdk::u32x4 scale16(cdk::u32x4 v, const ClipCoef &coef)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        v[i] = sizeof(T) == 4 ? __float_as_uint(__uint_as_float(v[i]) * coef)
-                              : bf16_bits(cdk::bf16_lo(v[i]) * coef) |
-                                    bf16_bits(cdk::bf16_hi(v[i]) * coef) << 16;
+        v[i] = sizeof(T) == 4 ? __float_as_uint(clip_mul(__uint_as_float(v[i]), coef))
+                              : bf16_bits(clip_mul(cdk::bf16_lo(v[i]), coef)) |
+                                    bf16_bits(clip_mul(cdk::bf16_hi(v[i]), coef)) << 16;
     return v;
 }
 
 // coef 1 copies the bits (a NaN's among them)
 template <int BLOCK, class T>
-__device__ __forceinline__ void clip_scale(const T *p, T *o, unsigned n, float coef, unsigned at)
+__device__ __forceinline__ void clip_scale(const T *p, T *o, unsigned n, const ClipCoef &coef, unsigned at)
 {
     constexpr unsigned kVec = 16 / sizeof(T);
-    const bool same = coef == 1.0f;
+    const bool same = clip_same(coef);
     if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
         for (unsigned i = at; i < n; i += BLOCK)
-            o[i] = same ? p[i] : clip_round(clip_value(p[i]) * coef, T{});
+            o[i] = same ? p[i] : clip_round(clip_mul(clip_value(p[i]), coef), T{});
         return;
     }
     const unsigned lead = clip_lead(p, n), vecs = (n - lead) / kVec, done = lead + vecs * kVec;
     const cdk::u32x4 *v = reinterpret_cast<const cdk::u32x4 *>(p + lead);
     cdk::u32x4 *w = reinterpret_cast<cdk::u32x4 *>(o + lead);
     if (at < lead)
-        o[at] = same ? p[at] : clip_round(clip_value(p[at]) * coef, T{});
+        o[at] = same ? p[at] : clip_round(clip_mul(clip_value(p[at]), coef), T{});
 #pragma unroll 8
     for (unsigned i = at; i < vecs; i += BLOCK)
         w[i] = same ? v[i] : scale16<T>(v[i], coef);
     if (at < n - done)
         o[done + at] =
-            same ? p[done + at] : clip_round(clip_value(p[done + at]) * coef, T{});
+            same ? p[done + at] : clip_round(clip_mul(clip_value(p[done + at]), coef), T{});
 }
 
 // (BACK: the last chunks first. The norm read them last, they may still be in the last cache)
 template <int BLOCK, bool BACK>
-__device__ __forceinline__ void clip_scale_all(const ClipTable &a, float coef, unsigned first,
+__device__ __forceinline__ void clip_scale_all(const ClipTable &a, const ClipCoef &coef, unsigned first,
                                                unsigned step, unsigned at)
 {
     for (unsigned c = first; c < a.chunks; c += step) {
         const ClipChunk k = clip_chunk(a, BACK ? (unsigned)a.chunks - 1 - c : c);
         const void *grad = a.entry[k.t].grad;
         void *out = a.entry[k.t].out;
-        if (!out || (coef == 1.0f && out == grad))
+        if (!out || (clip_same(coef) && out == grad))
             continue;
         if (a.entry[k.t].type == CD_TYPE_F32)
             clip_scale<BLOCK>(static_cast<const float *>(grad) + k.first,
@@ -278,11 +296,11 @@ __device__ __forceinline__ double clip_hold(const T *p, unsigned n, unsigned lan
 
 // clip_scale from the kept vectors
 template <class T>
-__device__ __forceinline__ void clip_scale_held(const T *p, T *o, unsigned n, float coef, unsigned lane,
+__device__ __forceinline__ void clip_scale_held(const T *p, T *o, unsigned n, const ClipCoef &coef, unsigned lane,
                                                 const cdk::u32x4 (&v)[kClipHeld])
 {
     constexpr unsigned kVec = 16 / sizeof(T);
-    const bool same = coef == 1.0f;
+    const bool same = clip_same(coef);
     if (!o || (same && o == p))
         return;
     if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
@@ -292,13 +310,13 @@ __device__ __forceinline__ void clip_scale_held(const T *p, T *o, unsigned n, fl
     const unsigned lead = clip_lead(p, n), vecs = (n - lead) / kVec, done = lead + vecs * kVec;
     cdk::u32x4 *w = reinterpret_cast<cdk::u32x4 *>(o + lead);
     if (lane < lead)
-        o[lane] = same ? p[lane] : clip_round(clip_value(p[lane]) * coef, T{});
+        o[lane] = same ? p[lane] : clip_round(clip_mul(clip_value(p[lane]), coef), T{});
 #pragma unroll
     for (int u = 0; u < kClipHeld * (int)sizeof(T) / 4; ++u)
         if (lane + u * cdk::kWave < vecs)
             w[lane + u * cdk::kWave] = same ? v[u] : scale16<T>(v[u], coef);
     if (lane < n - done)
-        o[done + lane] = same ? p[done + lane] : clip_round(clip_value(p[done + lane]) * coef, T{});
+        o[done + lane] = same ? p[done + lane] : clip_round(clip_mul(clip_value(p[done + lane]), coef), T{});
 }
 
 __global__ __launch_bounds__(kClipOneBlock) void k_clip_one(const ClipTable a, double max_norm,
@@ -320,7 +338,7 @@ __global__ __launch_bounds__(kClipOneBlock) void k_clip_one(const ClipTable a, d
     const double norm = sqrt(clip_block_sum<kClipOneBlock>(s));
     if (norm_out && threadIdx.x == 0)
         *norm_out = norm;
-    const float coef = clip_coef(norm, max_norm);
+    const ClipCoef coef = clip_coef(norm, max_norm);
     if (mine && f32)
         clip_scale_held(p32, out ? static_cast<float *>(out) + k.first : nullptr, k.n, coef, lane, v);
     else if (mine)
