@@ -149,23 +149,24 @@ __global__ __launch_bounds__(kClipBlock) void k_clip_norm(const ClipTable a, dou
         part[blockIdx.x] = s;
 }
 
-// The norm from the workgroups' sums, in every thread. Each workgroup that needs it adds
-// them for itself (at most 16 KB a launch, from L2): a counter that tells one workgroup it is the last
-// makes every other flush its L2 first (2032 of them: 70 us for 67 MB of gradients).
+// The sum of the workgroups' sums, in every thread. Each workgroup of the launch that needs it
+// adds them for itself (16 KB from L2 for the 96 tensors of one launch): a counter that tells one workgroup
+// it is the last makes every other flush its L2 first (2032 of them: 70 us for 67 MB of gradients).
 __device__ __forceinline__ double clip_total(const double *part, unsigned parts)
 {
     double s = 0.0;
+#pragma unroll 4
     for (unsigned i = threadIdx.x; i < parts; i += kClipBlock)
         s += part[i];
-    return sqrt(clip_block_sum<kClipBlock>(s));
+    return clip_block_sum<kClipBlock>(s);
 }
 
 __global__ __launch_bounds__(kClipBlock) void k_clip_total(const double *part, unsigned parts,
                                                            double *norm_out)
 {
-    const double norm = clip_total(part, parts);
+    const double s = clip_total(part, parts);
     if (threadIdx.x == 0)
-        *norm_out = norm;
+        *norm_out = sqrt(s);
 }
 
 // The scale max_norm / norm as an fp32 factor and a power of two: below fp32's normal numbers
@@ -254,13 +255,18 @@ __device__ __forceinline__ void clip_scale_all(const ClipTable &a, const ClipCoe
     }
 }
 
+// (total: where the sum is kept for the launches that follow, as their only part; else null)
 __global__ __launch_bounds__(kClipBlock) void k_clip_scale(const ClipTable a, const double *part,
                                                            unsigned parts, double max_norm,
-                                                           double *norm_out)
+                                                           double *norm_out, double *total)
 {
-    const double norm = clip_total(part, parts);
-    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0)
-        *norm_out = norm;
+    const double sum = clip_total(part, parts), norm = sqrt(sum);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (norm_out)
+            *norm_out = norm;
+        if (total)
+            *total = sum;
+    }
     clip_scale_all<kClipBlock, true>(a, clip_coef(norm, max_norm), blockIdx.x, gridDim.x, threadIdx.x);
 }
 
@@ -392,6 +398,7 @@ bool clip_disjoint(const cd_grad *g, int n, bool scaled, const double *norm)
 
 struct cd_clip {
     int device, max_tensors;
+    double *total; // the sum of all squares
     double *part;  // workgroups' sums of every launch
 };
 
@@ -413,11 +420,12 @@ cd_status countdown_clip_create(int max_tensors, cd_clip **out)
     p->max_tensors = max_tensors;
     const size_t launches = (max_tensors + kClipTensors - 1) / kClipTensors;
     void *ws = nullptr;
-    if (hip_status(hipMalloc(&ws, launches * kClipGroups * sizeof(double))) != CD_OK) {
+    if (hip_status(hipMalloc(&ws, (1 + launches * kClipGroups) * sizeof(double))) != CD_OK) {
         delete p;
         return CD_ENOMEM;
     }
-    p->part = static_cast<double *>(ws);
+    p->total = static_cast<double *>(ws);
+    p->part = p->total + 1;
     *out = p;
     return CD_OK;
 }
@@ -432,7 +440,7 @@ cd_status countdown_clip_destroy(cd_clip *p)
         st = hip_status(hipSetDevice(p->device));
     if (st == CD_OK)
         st = hip_status(hipDeviceSynchronize());
-    if (hip_status(hipFree(p->part)) != CD_OK)
+    if (hip_status(hipFree(p->total)) != CD_OK)
         st = CD_EHIP;
     if (dev >= 0)
         (void)hip_status(hipSetDevice(dev));
@@ -505,6 +513,7 @@ cd_status countdown_clip_grads(cd_clip *p, const cd_grad *grads, int n, double m
     }
     // the norm of every launch's tensors, then the scaling
     unsigned parts = 0;
+    const double *part = p->part;
     for (int pass = 0; pass < (writes ? 2 : 1); ++pass) {
         int i = 0;
         do {
@@ -516,8 +525,12 @@ cd_status countdown_clip_grads(cd_clip *p, const cd_grad *grads, int n, double m
                 k_clip_norm<<<grid, kClipBlock, 0, s>>>(a, p->part + parts);
                 parts += grid;
             } else {
-                k_clip_scale<<<grid, kClipBlock, 0, s>>>(a, p->part, parts, max_norm, norm);
+                // with many tensors the sums are added up by the first launch alone
+                double *total = part == p->part && i < n ? p->total : nullptr;
+                k_clip_scale<<<grid, kClipBlock, 0, s>>>(a, part, parts, max_norm, norm, total);
                 norm = nullptr;  // written by the first
+                part = p->total;
+                parts = 1;
             }
             if (launched(hipGetLastError()) != CD_OK)
                 return CD_EHIP;

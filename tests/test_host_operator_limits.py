@@ -2,6 +2,7 @@
 library's own host code on a machine without a GPU (see host_hip.py)."""
 import ctypes as C
 import math
+import os
 
 import pytest
 
@@ -47,3 +48,54 @@ def test_one_gradient_into_two_outputs(host, clip):
         assert clip_call(host, clip, [(G, O, 10, F32), (G, O + 64, 10, F32)], top) == 0
     # with no limit the gradient in place is not written
     assert clip_call(host, clip, [(G, G, 10, F32), (G, O, 10, F32)], math.inf) == 0
+
+
+# host_hip.cpp with the number of sums that each scaling launch adds up (k_clip_scale's third
+# argument) behind its launch
+STUB = """
+#define hipLaunchKernel record_launch
+#include "%s"
+#undef hipLaunchKernel
+namespace { std::string parts; }
+extern "C" const char *host_hip_parts(void) { return parts.c_str(); }
+extern "C" hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3 block, void **args, size_t lds,
+                                      hipStream_t s)
+{
+    if (names()[f] == "k_clip_scale")
+        parts += std::to_string(grid.x) + " " + std::to_string(*(unsigned *)args[2]) + "\\n";
+    return record_launch(f, grid, block, args, lds, s);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def counting(tmp_path_factory):
+    root = tmp_path_factory.mktemp("counting")
+    (root / "tests").mkdir()
+    (root / "include").symlink_to(os.path.join(host_hip.ROOT, "include"))
+    (root / "tests" / "host_hip.cpp").write_text(
+        STUB % os.path.join(host_hip.ROOT, "tests", "host_hip.cpp"))
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(host_hip, "ROOT", str(root))
+        lib = host_hip.build(str(root))
+    h = host_hip.Host(lib)
+    h.lib.host_hip_parts.restype = C.c_char_p
+    return h
+
+
+@pytest.mark.parametrize("n", [1, 96, 97, 1000, 20000])
+def test_scaling_many_tensors_takes_work_in_proportion(counting, n):
+    """n tensors of one chunk each. The first launch's workgroups, at most 96, add the n sums; the
+    others must not do so again (n^2 sums in all)."""
+    c = C.c_void_p()
+    assert counting.lib.countdown_clip_create(n, C.byref(c)) == 0
+    before = len(counting.lib.host_hip_parts())
+    grads = [(G + 65536 * i, G + 65536 * i, 8191 if n > 1 else 1 << 20, F32) for i in range(n)]
+    assert clip_call(counting, c, grads, 1.0) == 0
+    rows = [tuple(map(int, line.split()))
+            for line in counting.lib.host_hip_parts()[before:].decode().splitlines()]
+    assert len(rows) == -(-n // 96)
+    sums = n if n > 1 else (1 << 20) // 8192
+    assert rows[0][1] == sums
+    assert sum(grid * parts for grid, parts in rows) <= rows[0][0] * sums + n
+    assert counting.lib.countdown_clip_destroy(c) == 0
