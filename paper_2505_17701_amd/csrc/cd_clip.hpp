@@ -155,7 +155,6 @@ __global__ __launch_bounds__(kClipBlock) void k_clip_norm(const ClipTable a, dou
 __device__ __forceinline__ double clip_total(const double *part, unsigned parts)
 {
     double s = 0.0;
-#pragma unroll 4
     for (unsigned i = threadIdx.x; i < parts; i += kClipBlock)
         s += part[i];
     return clip_block_sum<kClipBlock>(s);
@@ -176,22 +175,18 @@ struct ClipCoef {
     int e;  // 0 for the usual quotient, and out = grad * f
 };
 
-// a norm that is not finite scales nothing (norm is uniform)
+// a norm that is not finite scales nothing
 __device__ __forceinline__ ClipCoef clip_coef(double norm, double max_norm)
 {
-    const double c = norm > max_norm && norm < (double)INFINITY ? max_norm / norm : 1.0;
-    const bool low = c < (double)__FLT_MIN__;
-    const float f = (float)(low ? __builtin_amdgcn_frexp_mant(c) : c);
-    return {__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f))),
-            __builtin_amdgcn_readfirstlane(low ? __builtin_amdgcn_frexp_exp(c) : 0)};
+    if (!(norm > max_norm && norm < (double)INFINITY))
+        return {1.0f, 0};
+    const double c = max_norm / norm;
+    if (c >= (double)__FLT_MIN__)
+        return {(float)c, 0};
+    return {(float)__builtin_amdgcn_frexp_mant(c), __builtin_amdgcn_frexp_exp(c)};
 }
 
 __device__ __forceinline__ bool clip_same(const ClipCoef &c) { return c.f == 1.0f && c.e == 0; }
-
-__device__ __forceinline__ float clip_mul(float v, const ClipCoef &c)
-{
-    return __builtin_amdgcn_ldexpf(v * c.f, c.e);
-}
 
 __device__ __forceinline__ uint32_t bf16_bits(float v)
 {
@@ -201,13 +196,13 @@ __device__ __forceinline__ float clip_round(float v, float) { return v; }
 __device__ __forceinline__ uint16_t clip_round(float v, uint16_t) { return (uint16_t)bf16_bits(v); }
 
 template <class T>
-__device__ __forceinline__ cdk::u32x4 scale16(cdk::u32x4 v, const ClipCoef &coef)
+__device__ __forceinline__ cdk::u32x4 scale16(cdk::u32x4 v, float coef)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        v[i] = sizeof(T) == 4 ? __float_as_uint(clip_mul(__uint_as_float(v[i]), coef))
-                              : bf16_bits(clip_mul(cdk::bf16_lo(v[i]), coef)) |
-                                    bf16_bits(clip_mul(cdk::bf16_hi(v[i]), coef)) << 16;
+        v[i] = sizeof(T) == 4 ? __float_as_uint(__uint_as_float(v[i]) * coef)
+                              : bf16_bits(cdk::bf16_lo(v[i]) * coef) |
+                                    bf16_bits(cdk::bf16_hi(v[i]) * coef) << 16;
     return v;
 }
 
@@ -217,22 +212,22 @@ __device__ __forceinline__ void clip_scale(const T *p, T *o, unsigned n, const C
 {
     constexpr unsigned kVec = 16 / sizeof(T);
     const bool same = clip_same(coef);
-    if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
+    if (coef.e || ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
         for (unsigned i = at; i < n; i += BLOCK)
-            o[i] = same ? p[i] : clip_round(clip_mul(clip_value(p[i]), coef), T{});
+            o[i] = same ? p[i] : clip_round(__builtin_amdgcn_ldexpf(clip_value(p[i]) * coef.f, coef.e), T{});
         return;
     }
     const unsigned lead = clip_lead(p, n), vecs = (n - lead) / kVec, done = lead + vecs * kVec;
     const cdk::u32x4 *v = reinterpret_cast<const cdk::u32x4 *>(p + lead);
     cdk::u32x4 *w = reinterpret_cast<cdk::u32x4 *>(o + lead);
     if (at < lead)
-        o[at] = same ? p[at] : clip_round(clip_mul(clip_value(p[at]), coef), T{});
+        o[at] = same ? p[at] : clip_round(clip_value(p[at]) * coef.f, T{});
 #pragma unroll 8
     for (unsigned i = at; i < vecs; i += BLOCK)
-        w[i] = same ? v[i] : scale16<T>(v[i], coef);
+        w[i] = same ? v[i] : scale16<T>(v[i], coef.f);
     if (at < n - done)
         o[done + at] =
-            same ? p[done + at] : clip_round(clip_mul(clip_value(p[done + at]), coef), T{});
+            same ? p[done + at] : clip_round(clip_value(p[done + at]) * coef.f, T{});
 }
 
 // (BACK: the last chunks first. The norm read them last, they may still be in the last cache)
@@ -309,20 +304,20 @@ __device__ __forceinline__ void clip_scale_held(const T *p, T *o, unsigned n, co
     const bool same = clip_same(coef);
     if (!o || (same && o == p))
         return;
-    if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
+    if (coef.e || ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15u) != 0) {
         clip_scale<cdk::kWave>(p, o, n, coef, lane);
         return;
     }
     const unsigned lead = clip_lead(p, n), vecs = (n - lead) / kVec, done = lead + vecs * kVec;
     cdk::u32x4 *w = reinterpret_cast<cdk::u32x4 *>(o + lead);
     if (lane < lead)
-        o[lane] = same ? p[lane] : clip_round(clip_mul(clip_value(p[lane]), coef), T{});
+        o[lane] = same ? p[lane] : clip_round(clip_value(p[lane]) * coef.f, T{});
 #pragma unroll
     for (int u = 0; u < kClipHeld * (int)sizeof(T) / 4; ++u)
         if (lane + u * cdk::kWave < vecs)
-            w[lane + u * cdk::kWave] = same ? v[u] : scale16<T>(v[u], coef);
+            w[lane + u * cdk::kWave] = same ? v[u] : scale16<T>(v[u], coef.f);
     if (lane < n - done)
-        o[done + lane] = same ? p[done + lane] : clip_round(clip_mul(clip_value(p[done + lane]), coef), T{});
+        o[done + lane] = same ? p[done + lane] : clip_round(clip_value(p[done + lane]) * coef.f, T{});
 }
 
 __global__ __launch_bounds__(kClipOneBlock) void k_clip_one(const ClipTable a, double max_norm,
