@@ -1221,7 +1221,7 @@ cd_status ad_check(const cd_adapters *p, const AdArgs &a, int out_dim)
     const AdRows in[] = {{a.x, (size_t)p->d_in * 2, a.ldx * 2, a.T},
                          {a.dy, (size_t)p->d_out * 2, a.lddy * 2, a.T},
                          ad_flat(a.W, (size_t)p->d_out * p->d_in * 2),
-                         ad_flat(a.ids, (size_t)a.T * 4),
+                         {a.ids, 4, 4, a.T},
                          ad_flat(a.A, n * r * p->d_in * 2),
                          ad_flat(a.B, n * r * p->d_out * 2),
                          ad_flat(a.scale, n * 4),

@@ -99,3 +99,23 @@ def test_scaling_many_tensors_takes_work_in_proportion(counting, n):
     assert rows[0][1] == sums
     assert sum(grid * parts for grid, parts in rows) <= rows[0][0] * sums + n
     assert counting.lib.countdown_clip_destroy(c) == 0
+
+
+# ------------------------------------------------------------------ adapters
+
+PTR = {n: 0x100000000 * (i + 4) for i, n in enumerate(("x", "dy", "ids", "A", "B", "dx", "dA", "dB"))}
+
+
+@pytest.mark.parametrize("out", ["dA", "dB"])
+def test_an_empty_call_has_no_ids(host, out):
+    """With T = 0 ids stands for no element, wherever it points."""
+    h = C.c_void_p()
+    assert host.lib.countdown_adapters_create(264, 520, 24, 3, 64, 1, C.byref(h)) == 0
+
+    def call(T):
+        return host.lib.countdown_adapters_backward(
+            h, PTR["x"], 264, PTR["dy"], 520, T, PTR[out] + 64, PTR["A"], PTR["B"], None, 1, None, 0,
+            PTR["dx"], 264, PTR["dA"], PTR["dB"], None)
+
+    assert call(0) == 0 and call(1) == host.cd.CD_EINVAL
+    assert host.lib.countdown_adapters_destroy(h) == 0
