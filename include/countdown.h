@@ -373,8 +373,10 @@ typedef struct cd_adapters cd_adapters;
  * 1 <= n_adapters <= 1024; 1 <= max_tokens <= 2^20. CD_EINVAL for malformed
  * sizes and unknown flags, CD_EUNSUPPORTED beyond those limits (both before any
  * HIP call), CD_ENOMEM / CD_EHIP when allocation fails. *out is set only on
- * success. The workspace takes about 4 rank + 5 bytes per token; with
- * CD_ADAPTERS_TRAIN 20 rank + 5, as many bytes as B, and 16 MiB.
+ * success. Tokens are grouped by adapter in P positions: max_tokens rounded up to
+ * 32, and 32 for each adapter and for none. The workspace takes 4 rank + 4 bytes a
+ * position; with CD_ADAPTERS_TRAIN 8 rank + 12 R + 4 (R: rank rounded up to 16), as
+ * many bytes as B, and 16 MiB. Besides, up to 1 byte a token, 40 an adapter and 3 KB.
  */
 cd_status countdown_adapters_create(int d_in, int d_out, int rank, int n_adapters, int max_tokens,
                                     unsigned flags, cd_adapters **out);

@@ -119,3 +119,25 @@ def test_an_empty_call_has_no_ids(host, out):
 
     assert call(0) == 0 and call(1) == host.cd.CD_EINVAL
     assert host.lib.countdown_adapters_destroy(h) == 0
+
+
+@pytest.mark.parametrize("sizes", [  # d_in, d_out, rank, adapters, tokens
+    (4096, 4096, 16, 64, 8), (256, 688, 8, 3, 37), (264, 520, 24, 1024, 16), (64, 64, 256, 5, 1),
+    (512, 256, 40, 7, 100000),
+])
+@pytest.mark.parametrize("train", [0, 1])
+def test_the_workspace_takes_what_the_header_says(host, sizes, train):
+    _, d_out, rank, n, tokens = sizes
+    places = -(-tokens // 32) * 32 + 32 * (n + 1)
+    size = places * (4 * rank + 4)
+    if train:
+        size = places * (8 * rank + 12 * (-(-rank // 16) * 16) + 4) + 2 * n * rank * d_out + (16 << 20)
+    h = C.c_void_p()
+    try:
+        host.limit(size + tokens + 40 * n + 3072)
+        assert host.lib.countdown_adapters_create(*sizes, train, C.byref(h)) == 0
+        assert host.lib.countdown_adapters_destroy(h) == 0
+        host.limit(size)
+        assert host.lib.countdown_adapters_create(*sizes, train, C.byref(h)) == host.cd.CD_ENOMEM
+    finally:
+        host.limit()
