@@ -624,7 +624,7 @@ __device__ __forceinline__ void ad_by_size(const AdArgs &a, int block, int *befo
     a.by_size[place] = AdTile{i, mine.first, mine.count, 0};
 }
 
-// The low-rank latents of a tile of MT * 16 tokens and RT * 16 ranks (blockIdx.y the ranks;
+// The low-rank latents of a tile (MT * 16 tokens) and RT * 16 ranks (blockIdx.y the ranks;
 // blockIdx.z: with both, 0 is glat). The waves split the contraction in blocks of 128
 // columns, and their sums meet in LDS. The scale is applied here. Tokens past the tile's last
 // and ranks past the last repeat another: they only reach sums of their own, which are not
@@ -642,15 +642,14 @@ __global__ __launch_bounds__(WAVES * cdk::kWave, MT + RT <= 4 ? 4 : 2) void k_ad
     constexpr int kSums = MT * RT * cdk::kWave;
     constexpr int kDepth = MT + RT <= 2 ? 2 : 1;  // blocks in flight
     __shared__ u32x4 lds[WAVES * (kSums > kAdStage ? kSums : kAdStage)];
-    const int sub = a.tile / (MT * 16);  // a tile is taken in so many parts
-    const int spare = blockIdx.x - (a.T / a.tile + a.n + 1) * sub;  // workgroups past the tiles: a.by_size
+    const int spare = blockIdx.x - (a.T / a.tile + a.n + 1);  // workgroups past the tiles: a.by_size
     if (spare >= 0) {
         if (blockIdx.y == 0 && blockIdx.z == 0)
             ad_by_size<WAVES>(a, spare, reinterpret_cast<int *>(lds));
         return;
     }
-    const AdTile tile = a.tiles[blockIdx.x / sub];
-    const int off = blockIdx.x % sub * MT * 16, count = tile.count - off;
+    const AdTile tile = a.tiles[blockIdx.x];
+    const int count = tile.count;
     if (count <= 0 || tile.group == a.n)
         return;
     const bool back = kinds == 3 ? blockIdx.z == 0 : kinds == 2;  // glat
@@ -666,7 +665,7 @@ __global__ __launch_bounds__(WAVES * cdk::kWave, MT + RT <= 4 ? 4 : 2) void k_ad
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            xr[i][q] = a.order[tile.first + off + min(i * 16 + 4 * q + g, count - 1)];
+            xr[i][q] = a.order[tile.first + min(i * 16 + 4 * q + g, count - 1)];
 #pragma unroll
     for (int j = 0; j < RT; ++j)
 #pragma unroll
@@ -743,7 +742,7 @@ __global__ __launch_bounds__(WAVES * cdk::kWave, MT + RT <= 4 ? 4 : 2) void k_ad
     const int r = r0 + wave % RT * 16 + g * 4;
     if (at >= count || r >= a.rank)
         return;
-    const size_t p = tile.first + off + at;
+    const size_t p = tile.first + at;
     *reinterpret_cast<f32x4_t *>((back ? a.glat : a.lat) + p * a.rank + r) = v;
     uint16_t *terms = back ? a.glatT : a.latT;
     if (!terms)
@@ -1293,10 +1292,9 @@ void ad_shrink(const AdArgs &a, int kinds, hipStream_t s)
     // gradient's sums are the same alone and together.)
     const bool few = slots * (a.dy ? 2 : 1) * ad_ceil(a.rank, 16) <= 256;
     const int rt = a.rank <= 16 || few ? 1 : a.rank <= 32 ? 2 : 4;
-    const int m = std::min(mt, 2);  // sums of a workgroup: at most one per thread
-    const dim3 grid(slots * (mt / m) + (a.by_size ? ad_ceil(a.n, cdk::kWave) : 0), ad_ceil(a.rank, rt * 16), both);
+    const dim3 grid(slots + (a.by_size ? ad_ceil(a.n, cdk::kWave) : 0), ad_ceil(a.rank, rt * 16), both);
 #define AD_SHRINK(M, R, W) \
-    if (m == M && rt == R && few == (W == 16)) \
+    if (mt == M && rt == R && few == (W == 16)) \
         k_ad_shrink<M, R, W><<<grid, W * cdk::kWave, 0, s>>>(a, kinds)
     AD_SHRINK(1, 1, 16);
     AD_SHRINK(1, 1, 8);

@@ -84,7 +84,7 @@ __device__ __forceinline__ void square16(const cdk::u32x4 &v, double (&s)[4])
     for (int i = 0; i < 4; ++i)
         if constexpr (sizeof(T) == 4) {
             s[i] += square(__uint_as_float(v[i]));
-        } else {  //
+        } else {
             s[i] += square(cdk::bf16_lo(v[i]));
             s[i] += square(cdk::bf16_hi(v[i]));
         }
