@@ -1506,6 +1506,11 @@ cd_status countdown_adapters_add(cd_adapters *p, const uint16_t *x, size_t ldx, 
     // 4096 -> 4096, 16 tokens.) Two launches and grouped, captured: T r (d_in + d_out) of 40 M 11.0
     // against 19.8 (4096 -> 1024, rank 128, 64 tokens) to 22.7 against 18.3 (1024 -> 4096); of 59 to 67 M
     // 27.0 against 15.7 (256 -> 688, rank 64, 1024 tokens) to 16.5 against 14.6 (4096 -> 4096, rank 32, 256).
+    // They count products, not the workgroup and the round trips that every token costs, and so come
+    // late for narrow layers and thousands of tokens. One launch, two and grouped, captured:
+    //   256 -> 256 rank 8, 2048 tokens  8.2  7.9 11.5   4096 13.5 11.6 12.2    8192 24.5 19.1 14.3
+    //    64 ->  64 rank 16, 2048 tokens 9.0  9.9 11.4   4096 15.2 15.2 11.5   16384 51.3 47.5 14.8
+    // From 1024 -> 1024, rank 16 on they hold there too: 2048 tokens 14.1 15.6 15.4.
     const int64_t down = (int64_t)a.rank * a.d_in, up = (int64_t)a.rank * a.d_out;
     const int slices = ad_ceil(a.d_out, kAdTokenBlock);
     if (a.rank <= 64 && down <= 3 << 16 && T * (slices * down + up) < 3 << 24) {
