@@ -94,3 +94,48 @@ def test_the_norm_after_clipping(cd):
             cd.countdown_clip_grads(clip, [t], 1.0)
             after = float(cd.countdown_clip_grads(clip, [t], math.inf))
         assert abs(after - 1.0) <= 2.0 ** -23 + 2.0 ** -52 * n
+
+
+@pytest.mark.parametrize("dtype,value", [(F32, 1e-42), (F32, 3 * 2.0 ** -149), (BF16, 5 * 2.0 ** -133)])
+def test_subnormal_gradients(cd, dtype, value):
+    """Squares below fp32's range, results that are subnormal themselves."""
+    for n in (1000, 100001):
+        t = torch.full((n,), value, dtype=dtype, device="cuda")
+        with cd.GradClip(1) as clip:
+            norm = float(cd.countdown_clip_grads(clip, [t], math.inf))
+            want = math.sqrt(n) * float(t[0].double())
+            assert abs(norm - want) <= 2.0 ** -52 * (n / 2 + 3) * want
+            out = torch.empty_like(t)
+            cd.countdown_clip_grads(clip, [t], norm * 0.6, out=[out])
+            check(out, t, 0.6)
+
+
+def test_many_tensors(cd):
+    """Eleven launches of 96 tensors, the sum of the first one used by the others: eager, in
+    place, and replayed with other values."""
+    g = torch.Generator().manual_seed(9)
+    sizes = [int(v) for v in torch.randint(1, 9000, (1000,), generator=g)]
+    flat = torch.randn(sum(sizes), generator=g).cuda()
+    grads = [t.to(BF16) if i % 3 == 0 else t for i, t in enumerate(flat.split(sizes))]
+    clip, other = cd.GradClip(1000), cd.GradClip(1000)
+    out = [torch.empty_like(t) for t in grads]
+    norm = torch.empty((), dtype=torch.float64, device="cuda")
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        cd.countdown_clip_grads(clip, grads, 2.0, out=out, norm=norm)
+    for k in range(3):
+        for t in grads:
+            t.mul_(1.0 + k)
+        want = math.sqrt(math.fsum(float((t.double() ** 2).sum()) for t in grads))
+        place = [t.clone() for t in grads]
+        eager = cd.countdown_clip_grads(other, place, 2.0)
+        assert abs(float(eager) - want) <= 2.0 ** -52 * (sum(sizes) / 2 + 2) * want
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(norm, eager)
+        for o, p, t in zip(out, place, grads):
+            assert torch.equal(o, p)
+            check(o, t, 2.0 / float(norm))
+    clip.close()
+    other.close()
