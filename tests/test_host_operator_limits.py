@@ -134,7 +134,7 @@ def test_the_workspace_takes_what_the_header_says(host, sizes, train):
         size = places * (8 * rank + 12 * (-(-rank // 16) * 16) + 4) + 2 * n * rank * d_out + (16 << 20)
     h = C.c_void_p()
     try:
-        host.limit(size + tokens + 40 * n + 3072)
+        host.limit(size + tokens + 40 * n + 3 * 1024)
         assert host.lib.countdown_adapters_create(*sizes, train, C.byref(h)) == 0
         assert host.lib.countdown_adapters_destroy(h) == 0
         host.limit(size)
