@@ -458,6 +458,116 @@ cd_status countdown_clip_destroy(cd_clip *clip);
 cd_status countdown_clip_grads(cd_clip *clip, const cd_grad *grads, int n, double max_norm,
                                double *norm, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The gated block of many tokens (prompts, training batches; also decode steps):
+ *   g = x W_gate^T, u = x W_up^T, h = SiLU(g) * u,
+ * and its gradients. W_gate and W_up are [d_ff][d_model] bf16, as in the FFN calls, and
+ * stay with the caller. Products and sums are fp32; h is rounded to its type once. Numbers that are
+ * not finite reach what is computed from them, as infinity or NaN.
+ *
+ * Conventions beyond those at the top of this file:
+ *  - x, h, dh and dx are row-major with a row stride (ld*, in elements, a multiple of 8, at
+ *    least the row's width; ldx and lddh at most 2^20, else CD_EUNSUPPORTED), so they may be
+ *    column slices of wider tensors; what lies between their rows is left as it was.
+ *  - `type` (CD_TYPE_*) is the type of h, or of the three gradients.
+ *  - An output must share no element with an input or with another output (CD_EINVAL;
+ *    tensors of different row strides whose ranges touch count as sharing).
+ *  - T = 0 is a valid empty call (the backward call then writes zeros to dW_gate and dW_up).
+ *    T > max_tokens is CD_EINVAL.
+ *  - The same call on the same inputs gives the same bits.
+ *  - A handle belongs to the device current at its creation. The forward call uses no
+ *    workspace; backward calls on one handle must not overlap (two streams, two graphs
+ *    replayed at once).
+ */
+typedef struct cd_gated cd_gated;
+
+/* Flags of countdown_gated_create. */
+#define CD_GATED_TRAIN 1u       /* also allocate the workspace of the backward call */
+#define CD_GATED_FP32_GRADS 2u  /* (with CD_GATED_TRAIN) enough of it for fp32 gradients */
+
+/*
+ * Create a handle for one layer's sizes on the current device. d_model and d_ff: positive
+ * multiples of 8 up to 65536; 1 <= max_tokens <= 2^20. CD_EINVAL for malformed sizes and flags,
+ * CD_EUNSUPPORTED beyond those limits (both before any HIP call), CD_ENOMEM / CD_EHIP when
+ * allocation fails. *out is set only on success. CD_GATED_TRAIN takes 4 max_tokens d_ff
+ * bytes (dg and du) and 16 MiB, with CD_GATED_FP32_GRADS 12 max_tokens d_ff and 16 MiB.
+ */
+cd_status countdown_gated_create(int d_model, int d_ff, int max_tokens, unsigned flags,
+                                 cd_gated **out);
+
+/* Release a handle and its workspace (synchronises the device first). NULL is a no-op. */
+cd_status countdown_gated_destroy(cd_gated *gated);
+
+/* h_t = SiLU(W_gate x_t) * (W_up x_t), [T][d_ff] of `type`. */
+cd_status countdown_gated_forward(cd_gated *gated, const uint16_t *x, size_t ldx, int T,
+                                  const uint16_t *W_gate, const uint16_t *W_up, int type, void *h,
+                                  size_t ldh, void *stream);
+
+/*
+ * Gradients of sum_t <dh_t, h_t> (a CD_GATED_TRAIN handle, else CD_EINVAL). Nothing is kept from
+ * the forward call: g and u are formed again. With s = 1 / (1 + exp(-g)):
+ *   dg = dh u s (1 + g (1 - s)),   du = dh g s,
+ *   dx = dg W_gate + du W_up,   dW_gate = dg^T x,   dW_up = du^T x.
+ * dh [T][d_ff] bf16. dx [T][d_model], dW_gate and dW_up [d_ff][d_model] of `type`, overwritten
+ * whole; each may be NULL: that gradient is not computed. With CD_TYPE_BF16 dg and du are
+ * rounded to bf16, the operands of bf16 products; with CD_TYPE_F32 (a handle with
+ * CD_GATED_FP32_GRADS, else CD_EINVAL) they keep fp32 and enter as three exact bf16 terms, at
+ * three times the products of the last line.
+ */
+cd_status countdown_gated_backward(cd_gated *gated, const uint16_t *x, size_t ldx,
+                                   const uint16_t *dh, size_t lddh, int T, const uint16_t *W_gate,
+                                   const uint16_t *W_up, int type, void *dx, size_t lddx,
+                                   void *dW_gate, void *dW_up, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Decode products with 4-bit weights and group scales. A matrix W [rows][cols] holds
+ *   w[r][c] = scale[r][c / group] code[r][c],   code in -8..7, scale bf16,
+ * group 32, 64 or 128 (the last group of a row may be shorter), rows and cols positive multiples
+ * of 8 up to 65536. It is kept in a packed DEVICE buffer of countdown_q4_bytes bytes, owned by the
+ * caller, 16-byte aligned, written whole by countdown_q4_quantize or countdown_q4_pack: blocks of
+ * 16 rows x 128 columns, a row tile's blocks one after another; a block holds 1024
+ * bytes of codes, then 16 scales for each of its 128 / group groups. Bytes 16 l..16 l + 15 of the
+ * codes (l = 16 j + i) are row i; the 32-bit word k of them has columns 32 k + 8 j + e, the code of
+ * e = 2 p plus 8 at bits 4 p, that of e = 2 p + 1 at bits 16 + 4 p. Padding has code 0, scale 0.
+ *
+ * Products and sums are fp32: a code enters as 24 + code and 24 times the group's sum of x leaves
+ * again, so |x| must stay below 2^100, and an infinity in x or a scale reaches its results as
+ * infinity or NaN. x, base, y, h and W have row strides, base may be y itself, and outputs must
+ * not share memory with inputs, as for the adapters' calls. Up to 16 tokens (CD_EUNSUPPORTED
+ * beyond: unpack the weights and use a matrix product, e.g. countdown_gated_forward); T = 0 is a
+ * valid empty call. No workspace: calls may overlap. The same call on the same inputs gives the
+ * same bits.
+ */
+/* Bytes of a packed matrix; 0 for sizes that the calls refuse. Host only. */
+size_t countdown_q4_bytes(int rows, int cols, int group);
+
+/*
+ * Quantise W (bf16, row stride ldw): scale = bf16(max |w| / 7) over the group, code = w / scale
+ * (fp32) rounded to nearest even, kept within -8..7 (0 where the scale is 0). A group that holds
+ * an infinity or NaN gets the scale NaN.
+ */
+cd_status countdown_q4_quantize(const uint16_t *W, size_t ldw, int rows, int cols, int group,
+                                void *packed, void *stream);
+
+/* Pack given codes [rows][cols] (int8; the low four bits are kept) and scales
+ * [rows][ceil(cols / group)] (bf16), both contiguous. */
+cd_status countdown_q4_pack(const int8_t *codes, const uint16_t *scale, int rows, int cols,
+                            int group, void *packed, void *stream);
+
+/* W = scale code, rounded to bf16 (row stride ldw). */
+cd_status countdown_q4_unpack(const void *packed, int rows, int cols, int group, uint16_t *W,
+                              size_t ldw, void *stream);
+
+/* y_t = base_t + W x_t (base NULL: y_t = W x_t), W [d_out][d_in] packed; `type` of y and base. */
+cd_status countdown_q4_project(const uint16_t *x, size_t ldx, int T, const void *W, int d_in,
+                               int d_out, int group, int type, const void *base, size_t ldb,
+                               void *y, size_t ldy, void *stream);
+
+/* h_t = SiLU(W_gate x_t) * (W_up x_t), both [d_ff][d_model] packed with the same group. */
+cd_status countdown_q4_gated(const uint16_t *x, size_t ldx, int T, const void *W_gate,
+                             const void *W_up, int d_model, int d_ff, int group, int type, void *h,
+                             size_t ldh, void *stream);
+
 /*
  * Host-only validation of an FFN call's arguments against a shape, exactly
  * as the entry points perform it before launching: pointers non-NULL and

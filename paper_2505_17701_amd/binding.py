@@ -24,6 +24,7 @@ CD_PLAN_KEEP_COEF, CD_PLAN_DETERMINISTIC = 1, 2
 CD_PHASE_COEF, CD_PHASE_DOWN, CD_PHASE_ALL = 1, 2, 3
 CD_TYPE_F32, CD_TYPE_BF16 = 0, 1
 CD_ADAPTERS_TRAIN = 1
+CD_GATED_TRAIN, CD_GATED_FP32_GRADS = 1, 2
 
 # every symbol include/countdown.h declares
 EXPORTS = (
@@ -38,6 +39,10 @@ EXPORTS = (
     "countdown_adapters_create", "countdown_adapters_destroy", "countdown_adapters_project",
     "countdown_adapters_add", "countdown_adapters_backward",
     "countdown_clip_create", "countdown_clip_destroy", "countdown_clip_grads",
+    "countdown_gated_create", "countdown_gated_destroy", "countdown_gated_forward",
+    "countdown_gated_backward",
+    "countdown_q4_bytes", "countdown_q4_quantize", "countdown_q4_pack", "countdown_q4_unpack",
+    "countdown_q4_project", "countdown_q4_gated",
 )
 
 _lib = None
@@ -93,6 +98,16 @@ def load_library(path: str = LIB_PATH):
         "countdown_clip_create": (i, [i, C.POINTER(vp)]),
         "countdown_clip_destroy": (i, [vp]),
         "countdown_clip_grads": (i, [vp, vp, i, d, vp, vp]),
+        "countdown_gated_create": (i, [i, i, i, u, C.POINTER(vp)]),
+        "countdown_gated_destroy": (i, [vp]),
+        "countdown_gated_forward": (i, [vp, vp, z, i, vp, vp, i, vp, z, vp]),
+        "countdown_gated_backward": (i, [vp, vp, z, vp, z, i, vp, vp, i, vp, z, vp, vp, vp]),
+        "countdown_q4_bytes": (z, [i, i, i]),
+        "countdown_q4_quantize": (i, [vp, z, i, i, i, vp, vp]),
+        "countdown_q4_pack": (i, [vp, vp, i, i, i, vp, vp]),
+        "countdown_q4_unpack": (i, [vp, i, i, i, vp, z, vp]),
+        "countdown_q4_project": (i, [vp, z, i, vp, i, i, i, i, vp, z, vp, z, vp]),
+        "countdown_q4_gated": (i, [vp, z, i, vp, vp, i, i, i, i, vp, z, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -725,6 +740,230 @@ def _out_ptr(g, o, device) -> int:
     if o.get_device() != device or not o.is_contiguous():
         raise ValueError(f"outputs must be contiguous tensors on GPU {device}")
     return o.data_ptr()
+
+
+class Gated:
+    """Owns a ``cd_gated``: the gated block of one layer's sizes for up to ``max_tokens`` tokens a
+    call (``train``: the workspace of the backward call too, ``fp32_grads``: also for fp32
+    gradients). The weights stay with the caller: W_gate and W_up [d_ff, d_model], bf16."""
+
+    def __init__(self, d_model: int, d_ff: int, max_tokens: int, train: bool = False,
+                 fp32_grads: bool = False):
+        self.d_model, self.d_ff, self.max_tokens = d_model, d_ff, max_tokens
+        self.train, self.fp32_grads = train, train and fp32_grads
+        self._w_shape = (d_ff, d_model)
+        flags = (CD_GATED_TRAIN if train else 0) | (CD_GATED_FP32_GRADS if self.fp32_grads else 0)
+        h = C.c_void_p()
+        _check(load_library().countdown_gated_create(d_model, d_ff, max_tokens, flags,
+                                                     C.byref(h)), "countdown_gated_create")
+        self.handle = h.value
+        self.device = (_torch or _use_torch()).cuda.current_device()
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _check(load_library().countdown_gated_destroy(self.handle), "countdown_gated_destroy")
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+def countdown_gated_create(d_model, d_ff, max_tokens, train=False, fp32_grads=False):
+    return Gated(d_model, d_ff, max_tokens, train, fp32_grads)
+
+
+def countdown_gated_destroy(gated: Gated) -> None:
+    gated.close()
+
+
+def _gated_args(gated: Gated, x, W_gate, W_up):
+    if gated.handle is None:
+        raise ValueError("the handle is closed")
+    if x.dim() != 2 or x.dtype is not _BF16:
+        raise TypeError(f"x must be a bfloat16 [T, {gated.d_model}] tensor")
+    T, dev = x.shape[0], gated.device
+    xp, ldx = _rows(x, T, gated.d_model, "x", dev)
+    return (T, xp, ldx, _whole(W_gate, gated._w_shape, _BF16, "W_gate", dev),
+            _whole(W_up, gated._w_shape, _BF16, "W_up", dev))
+
+
+def countdown_gated_forward(gated: Gated, x, W_gate, W_up, h=None, stream=None):
+    """h = SiLU(x W_gate^T) * (x W_up^T); returns h ``[T, d_ff]`` (bf16, or the type of the given
+    fp32 / bf16 ``h``)."""
+    T, xp, ldx, gp, up = _gated_args(gated, x, W_gate, W_up)
+    if h is None:
+        h = _torch.empty((T, gated.d_ff), dtype=_BF16, device=x.device)
+    hp, ldh = _rows(h, T, gated.d_ff, "h", gated.device)
+    _check(load_library().countdown_gated_forward(gated.handle, xp, ldx, T, gp, up,
+                                                  _row_type(h, "h"), hp, ldh, _stream(stream)),
+           "countdown_gated_forward")
+    return h
+
+
+def countdown_gated_backward(gated: Gated, x, dh, W_gate, W_up, dx=None, dW_gate=None, dW_up=None,
+                             dtype=None, need=(True, True, True), stream=None):
+    """The gradients ``(dx, dW_gate, dW_up)`` of the block for ``dh`` (bf16 [T, d_ff]); a handle with
+    ``train``. All have one type: that of the given tensors, else ``dtype``, else fp32 for a
+    handle with ``fp32_grads`` and bf16 without. ``need`` says which of the three are computed
+    (None is returned for the others); given tensors are overwritten, missing ones made."""
+    T, xp, ldx, gp, up = _gated_args(gated, x, W_gate, W_up)
+    dev = gated.device
+    if dh.dtype is not _BF16:
+        raise TypeError(f"dh: expected a bfloat16 tensor, got {dh.dtype}")
+    dhp, lddh = _rows(dh, T, gated.d_ff, "dh", dev)
+    for t in (dx, dW_gate, dW_up):
+        if dtype is None and t is not None:
+            dtype = t.dtype
+    if dtype is None:
+        dtype = _F32 if gated.fp32_grads else _BF16
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise TypeError(f"gradients must be float32 or bfloat16, got {dtype}")
+    dxp, lddx, dgp, dup = None, 0, None, None
+    if need[0]:
+        if dx is None:
+            dx = _torch.empty((T, gated.d_model), dtype=dtype, device=x.device)
+        elif dx.dtype is not dtype:
+            raise TypeError(f"dx: expected {dtype}, got {dx.dtype}")
+        dxp, lddx = _rows(dx, T, gated.d_model, "dx", dev)
+    if need[1]:
+        if dW_gate is None:
+            dW_gate = _torch.empty(gated._w_shape, dtype=dtype, device=x.device)
+        dgp = _whole(dW_gate, gated._w_shape, dtype, "dW_gate", dev)
+    if need[2]:
+        if dW_up is None:
+            dW_up = _torch.empty(gated._w_shape, dtype=dtype, device=x.device)
+        dup = _whole(dW_up, gated._w_shape, dtype, "dW_up", dev)
+    _check(load_library().countdown_gated_backward(
+        gated.handle, xp, ldx, dhp, lddh, T, gp, up, kind, dxp, lddx, dgp, dup, _stream(stream)),
+        "countdown_gated_backward")
+    return dx if need[0] else None, dW_gate if need[1] else None, dW_up if need[2] else None
+
+
+class Q4:
+    """A [rows, cols] matrix of 4-bit weights with a bf16 scale for each group of columns, packed
+    (``data``: uint8, ``countdown_q4_bytes`` long). Made by :func:`countdown_q4_quantize` and
+    :func:`countdown_q4_pack`."""
+
+    def __init__(self, rows: int, cols: int, group: int, data):
+        n = countdown_q4_bytes(rows, cols, group)
+        if n == 0:
+            raise CountdownError(CD_EINVAL, "countdown_q4_bytes")
+        if _torch is None:
+            _use_torch()
+        if data.dtype is not _torch.uint8 or data.shape != (n,) or not data.is_contiguous():
+            raise ValueError(f"data must be a contiguous uint8 tensor of {n} bytes")
+        if not data.is_cuda:
+            raise ValueError("countdown tensors must live on the GPU")
+        self.rows, self.cols, self.group, self.data = rows, cols, group, data
+        self.device = data.get_device()
+
+
+def countdown_q4_bytes(rows: int, cols: int, group: int) -> int:
+    """Bytes of a packed matrix (0: sizes that the calls refuse)."""
+    return load_library().countdown_q4_bytes(rows, cols, group)
+
+
+def _q4_device(t, name) -> int:
+    """The current device, on which t has to live."""
+    dev = (_torch or _use_torch()).cuda.current_device()
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must live on GPU {dev}, the current device")
+    return dev
+
+
+def _q4_new(rows, cols, group, device, what) -> Q4:
+    n = countdown_q4_bytes(rows, cols, group)
+    if n == 0:
+        raise CountdownError(CD_EINVAL, what)
+    return Q4(rows, cols, group, _torch.empty(n, dtype=_torch.uint8, device=f"cuda:{device}"))
+
+
+def countdown_q4_quantize(W, group: int = 128, stream=None) -> Q4:
+    """4-bit weights of W (bf16 [rows, cols]): the scale of a group is its largest magnitude / 7,
+    rounded to bf16, a code the nearest."""
+    dev = _q4_device(W, "W")
+    if W.dim() != 2 or W.dtype is not _BF16:
+        raise TypeError("W must be a bfloat16 [rows, cols] tensor")
+    rows, cols = W.shape
+    wp, ldw = _rows(W, rows, cols, "W", dev)
+    q = _q4_new(rows, cols, group, dev, "countdown_q4_quantize")
+    _check(load_library().countdown_q4_quantize(wp, ldw, rows, cols, group, q.data.data_ptr(),
+                                                _stream(stream)), "countdown_q4_quantize")
+    return q
+
+
+def countdown_q4_pack(codes, scale, group: int = 128, stream=None) -> Q4:
+    """Pack int8 ``codes`` [rows, cols] (-8..7) and bf16 ``scale`` [rows, ceil(cols / group)]."""
+    dev = _q4_device(codes, "codes")
+    if codes.dim() != 2:
+        raise ValueError(f"codes must be [rows, cols], got {tuple(codes.shape)}")
+    rows, cols = codes.shape
+    q = _q4_new(rows, cols, group, dev, "countdown_q4_pack")
+    _check(load_library().countdown_q4_pack(
+        _whole(codes, (rows, cols), _torch.int8, "codes", dev),
+        _whole(scale, (rows, -(-cols // group)), _BF16, "scale", dev), rows, cols, group,
+        q.data.data_ptr(), _stream(stream)), "countdown_q4_pack")
+    return q
+
+
+def countdown_q4_unpack(q: Q4, W=None, stream=None):
+    """scale * code as bf16 [rows, cols]: the weights of a prompt's matrix products."""
+    dev = _q4_device(q.data, "the packed weights")
+    if W is None:
+        W = _torch.empty((q.rows, q.cols), dtype=_BF16, device=f"cuda:{dev}")
+    if W.dtype is not _BF16:
+        raise TypeError(f"W: expected a bfloat16 tensor, got {W.dtype}")
+    wp, ldw = _rows(W, q.rows, q.cols, "W", dev)
+    _check(load_library().countdown_q4_unpack(q.data.data_ptr(), q.rows, q.cols, q.group, wp, ldw,
+                                              _stream(stream)), "countdown_q4_unpack")
+    return W
+
+
+def _q4_x(x, q: Q4):
+    dev = _q4_device(x, "x")
+    if q.device != dev:
+        raise ValueError(f"the packed weights must live on GPU {dev}, the current device")
+    if x.dim() != 2 or x.dtype is not _BF16:
+        raise TypeError(f"x must be a bfloat16 [T, {q.cols}] tensor")
+    return (x.shape[0], dev) + _rows(x, x.shape[0], q.cols, "x", dev)
+
+
+def countdown_q4_project(x, W: Q4, base=None, y=None, stream=None):
+    """y = base + x W^T for up to 16 tokens and 4-bit weights; returns y ``[T, rows]``. ``base`` (fp32
+    or bf16, None: zeros) may be ``y`` itself (in place); y has its type, is fp32 without a base
+    and a new tensor if None."""
+    T, dev, xp, ldx = _q4_x(x, W)
+    y, basep, ldb, yp, ldy = _base(base, y, T, W.rows, "y", _F32, dev)
+    _check(load_library().countdown_q4_project(
+        xp, ldx, T, W.data.data_ptr(), W.cols, W.rows, W.group, _row_type(y, "y"), basep, ldb, yp,
+        ldy, _stream(stream)), "countdown_q4_project")
+    return y
+
+
+def countdown_q4_gated(x, W_gate: Q4, W_up: Q4, h=None, stream=None):
+    """h = SiLU(x W_gate^T) * (x W_up^T) for up to 16 tokens and 4-bit weights of one shape and
+    group; returns h ``[T, rows]`` (bf16, or the type of the given fp32 / bf16 ``h``)."""
+    T, dev, xp, ldx = _q4_x(x, W_gate)
+    if (W_up.rows, W_up.cols, W_up.group, W_up.device) != (W_gate.rows, W_gate.cols, W_gate.group,
+                                                           dev):
+        raise ValueError("W_gate and W_up must have one shape, group and device")
+    if h is None:
+        h = _torch.empty((T, W_gate.rows), dtype=_BF16, device=x.device)
+    hp, ldh = _rows(h, T, W_gate.rows, "h", dev)
+    _check(load_library().countdown_q4_gated(
+        xp, ldx, T, W_gate.data.data_ptr(), W_up.data.data_ptr(), W_gate.cols, W_gate.rows,
+        W_gate.group, _row_type(h, "h"), hp, ldh, _stream(stream)), "countdown_q4_gated")
+    return h
 
 
 def countdown_check_args(variant, d_model, d_ff, max_batch, d_rank, x, B, W_gate, W_up, W_down,

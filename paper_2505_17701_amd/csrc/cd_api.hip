@@ -940,3 +940,6 @@ extern "C" cd_status countdown_ffn_mono_noalloc(const uint16_t *x, int B, const 
 // ------------------------------------------------- low-rank adapters, gradient clipping
 #include "cd_adapters.hpp"
 #include "cd_clip.hpp"
+// ------------------------------------------------- gated block, 4-bit weights
+#include "cd_gated.hpp"
+#include "cd_q4.hpp"

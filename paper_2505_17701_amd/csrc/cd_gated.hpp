@@ -1,0 +1,622 @@
+// The gated block for prompts and training: both projections, the activation and the product in
+// one kernel, and its backward pass. Part of cd_api.hip (its only includer, after cd_adapters.hpp).
+//
+//   g = x Wg^T, u = x Wu^T, s = 1 / (1 + exp(-g)), h = g s u
+//   dg = dh u s (1 + g (1 - s)), du = dh g s
+//   dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x
+//
+// All are products C[m][n] = sum_k M(m, k) N(n, k), n contiguous in C. N's rows are the first operand
+// of an MFMA, so that a lane holds four neighbouring n. An operand is stored with k contiguous (x and
+// the weights of the first two products, dg and du of dx) or with k across its rows (the weights of
+// dx, both operands of the weights' gradients). Either way a tile goes to LDS as it lies in memory,
+// 16 bytes a lane without passing registers; a k-contiguous tile is read 16 bytes a lane, the other
+// with the transposing LDS reads.
+#pragma once
+
+#include "cd_device.hpp"
+
+namespace {
+
+constexpr int kGtMaxDim = 65536, kGtMaxTokens = 1 << 20;
+constexpr size_t kGtMaxStride = (size_t)1 << 20;  // row strides: 256 rows stay below 2^30 bytes
+constexpr int kGtTerms = 3;                       // bf16 terms of an fp32 number
+constexpr int kGtOutside = 0x40000000;            // an offset past every resource: reads zeros
+constexpr size_t kGtPartFloats = (size_t)4 << 20; // place for dx's partial sums (16 MiB)
+
+enum GtKind { kGtForward, kGtBackward, kGtDx, kGtDw };
+
+struct GtArgs {
+    const uint16_t *x;  // [T][m], row stride ldx
+    size_t ldx;
+    const uint16_t *Wg, *Wu;  // [f][m]
+    const uint16_t *dh;       // [T][f], row stride lddh
+    size_t lddh;
+    int T, m, f;
+    int type;    // of out (and of both weight gradients)
+    void *out;   // h or dx; dW: the gradient of W_gate
+    void *out2;  // dW: the gradient of W_up
+    size_t ldo;
+    uint16_t *d;  // [terms][T][2 f]: dg and du of a token side by side
+    int terms;
+    float *part;     // dx split over k: [splits][T][m]
+    int mt, nt;      // tiles
+    int ktiles;      // of a workgroup (a split)
+};
+
+// a buffer resource over 2^30 bytes at p (uniform): what lies past them reads as zero
+__device__ __forceinline__ u32x4 gt_resource(const uint16_t *p)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)kGtOutside, 0x00027000u};
+}
+
+// 16 bytes a lane from the resource to LDS at `lds` + 16 lane. The builtin would do, but the compiler
+// then waits for every load in flight before each LDS read. Nothing is written but LDS; the waits and
+// barriers are gt_wait's.
+__device__ __forceinline__ void gt_load_lds(const u32x4 &r, int off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 ::"s"(lds), "v"(off), "s"(r) : "memory", "m0");
+}
+
+// All but the last N loads of this wave have come, and its LDS reads; then every wave's have.
+template <int N>
+__device__ __forceinline__ void gt_wait()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t gt_lds(const void *p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// A tile of R rows (of m or n) x BK columns of k.
+//
+// KC, k contiguous: rows of BK; 16-byte chunk c of row r sits at c ^ (r & 7), which spreads the 16
+// rows of an operand over the banks. Otherwise BK rows of R; the 32-byte slots of row k are permuted
+// by k & 3 and bit 3 of k, so that what the lanes of a transposing read take (rows 8 j + 0..3 of one
+// slot for 16 lanes, j = lane / 16) lies on different banks.
+template <int R, int BK, bool KC, int THREADS>
+struct GtTile {
+    static constexpr int kRowChunks = (KC ? BK : R) / 8;
+    static constexpr int kLoads = R * BK / 8 / THREADS;
+    static constexpr int kBytes = R * BK * 2;
+    static constexpr int kRowsALoad = THREADS / kRowChunks;
+    static_assert(R * BK / 8 % THREADS == 0 && THREADS % kRowChunks == 0, "whole loads");
+    static_assert(!KC || kRowsALoad % 8 == 0, "the row's swizzle is the same for every load");
+
+    int off[kLoads];  // byte offset from the tile's first element
+    int k[kLoads];    // k of this thread's chunks
+
+    static __device__ __forceinline__ int slot_key(int k) { return ((k & 3) | (k >> 1 & 4)) & (R / 16 - 1); }
+
+    // valid: rows (KC) or columns that the operand has from this tile on
+    __device__ __forceinline__ void init(size_t ld, int valid)
+    {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = threadIdx.x / kRowChunks + i * kRowsALoad, pos = threadIdx.x % kRowChunks;
+            if (KC) {
+                const int c = pos ^ (row & 7);
+                k[i] = c * 8;
+                off[i] = row < valid ? row * (int)ld * 2 + c * 16 : kGtOutside;
+            } else {
+                const int c = ((pos >> 1) ^ slot_key(row)) * 2 + (pos & 1);
+                k[i] = row;
+                off[i] = c * 8 < valid ? row * (int)ld * 2 + c * 16 : kGtOutside;
+            }
+        }
+    }
+
+    // the tile at base (uniform), of whose k `left` remain
+    __device__ __forceinline__ void load(const uint16_t *base, int left, uint32_t lds) const
+    {
+        const u32x4 r = gt_resource(base);
+        const uint32_t at = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave) * 1024;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            gt_load_lds(r, k[i] < left ? off[i] : kGtOutside, at + i * (THREADS * 16));
+    }
+
+    // operand of rows r0..r0 + 15 and k 32 kk..32 kk + 31 (lane: row lane % 16, k 8 (lane / 16)..)
+    static __device__ __forceinline__ u32x4 read(const char *lds, int r0, int kk)
+    {
+        const int lane = threadIdx.x % cdk::kWave, i = lane % 16, j = lane / 16;
+        if constexpr (KC) {
+            const int r = r0 + i;
+            return *reinterpret_cast<const u32x4 *>(lds + r * (BK * 2) + (((kk * 4 + j) ^ (r & 7)) << 4));
+        } else {
+            const int k = kk * 32 + 8 * j + (i >> 2);
+            const char *p = lds + k * (R * 2) + ((r0 / 16) ^ slot_key(k)) * 32 + (i & 3) * 8;
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * (R * 2)));
+            return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// The workgroup's tile. Neighbours in time on one XCD (blockIdx.x % 8) take `group` tiles of m by a
+// stretch of n, so that its L2 holds what they share. False: no tile.
+__device__ __forceinline__ bool gt_place(int mt, int nt, int &mi, int &ni)
+{
+    constexpr int group = 8;
+    const int total = mt * nt, per = (total + 7) / 8;
+    const int t = (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8;
+    if ((int)blockIdx.x / 8 >= per || t >= total)
+        return false;
+    const int width = group * nt, first = t / width * group, rows = min(group, mt - first);
+    mi = first + t % width % rows;
+    ni = t % width / rows;
+    return true;
+}
+
+__device__ __forceinline__ void gt_store4(void *out, int type, size_t i, const float (&v)[4])
+{
+    if (type == CD_TYPE_F32) {
+        f32x4_t w = {v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + i) = w;
+    } else {
+        const uint64_t w = ad_pack(v[0], v[1]) | (uint64_t)ad_pack(v[2], v[3]) << 32;
+        *reinterpret_cast<uint64_t *>(static_cast<uint16_t *>(out) + i) = w;
+    }
+}
+
+// h of four neurons
+__device__ __forceinline__ void gt_forward4(const GtArgs &a, size_t t, int n, const f32x4_t &g, const f32x4_t &u)
+{
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        v[r] = cdk::silu(g[r]) * u[r];
+    gt_store4(a.out, a.type, t * a.ldo + n, v);
+}
+
+// dg and du of four neurons, in a.terms bf16 terms: one is rounded to nearest even, the operand that
+// a bf16 product takes; two hold 16 bits, three all of an fp32 number.
+__device__ __forceinline__ void gt_backward4(const GtArgs &a, size_t t, int n, const f32x4_t &g, const f32x4_t &u)
+{
+    const uint64_t w = *reinterpret_cast<const uint64_t *>(a.dh + t * a.lddh + n);
+    float d[2][4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t p = (uint32_t)(w >> (r / 2 * 32));
+        const float dh = r % 2 ? cdk::bf16_hi(p) : cdk::bf16_lo(p);
+        const float s = 1.0f / (1.0f + expf(-g[r]));
+        d[0][r] = dh * u[r] * (s * (1.0f + g[r] * (1.0f - s)));
+        d[1][r] = dh * cdk::silu(g[r]);
+    }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        uint16_t *o = a.d + t * (2 * (size_t)a.f) + (size_t)q * a.f + n;
+        if (a.terms == 1) {
+            gt_store4(o, CD_TYPE_BF16, 0, d[q]);
+            continue;
+        }
+        uint64_t out[kGtTerms] = {0, 0, 0};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            uint32_t w3[3];
+            ad_split(d[q][r], w3);
+            if (a.terms == 2)  // the second rounded
+                w3[1] = ad_pack(__uint_as_float(w3[1]) + __uint_as_float(w3[2]), 0.0f) << 16;
+#pragma unroll
+            for (int k = 0; k < kGtTerms; ++k)
+                out[k] |= (uint64_t)(w3[k] >> 16) << (16 * r);
+        }
+#pragma unroll
+        for (int k = 0; k < kGtTerms; ++k)
+            if (k < a.terms)
+                *reinterpret_cast<uint64_t *>(o + (size_t)k * a.T * 2 * a.f) = out[k];
+    }
+}
+
+// One tile of BM x BN (twice BN for the two projections, of which a lane holds g and u of the same
+// elements). WM x WN waves share it, WK of them each a part of every BK columns of k. STAGES tiles
+// of k are in LDS, STAGES - 1 of them in flight. One barrier a tile.
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
+__global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtArgs a)
+{
+    constexpr int kThreads = WM * WN * WK * cdk::kWave;
+    constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
+    constexpr int NP = kTwo ? 2 : 1, FM = BM / WM / 16, FN = BN / WN / 16, KK = BK / 32 / WK;
+    using TM = GtTile<BM, BK, KIND != kGtDw, kThreads>;
+    using TN = GtTile<BN, BK, kTwo, kThreads>;
+    constexpr int kStage = TM::kBytes + NP * TN::kBytes;
+    constexpr int kFlight = (TM::kLoads + NP * TN::kLoads) * (STAGES - 2);
+    constexpr int kSums = WK > 1 ? (WK - 1) * WM * WN * NP * FM * FN * cdk::kWave * 16 : 0;
+    __shared__ __align__(1024) char lds[STAGES * kStage > kSums ? STAGES * kStage : kSums];
+
+    int mi, ni;
+    if (!gt_place(KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
+        return;
+    // dW: the tiles of W_gate's gradient, then those of W_up's
+    const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
+    if (KIND == kGtDw && mi >= a.mt)
+        mi -= a.mt;
+    const int m0 = mi * BM, n0 = ni * BN;
+    const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
+    const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
+    const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
+    const size_t plane = (size_t)a.T * 2 * a.f;
+
+    TM tm;
+    TN tn;
+    tm.init(ldm, M - m0);
+    tn.init(ldn, N - n0);
+    // The k tiles of this workgroup: of one product after another (dx: dg Wg and du Wu, each for
+    // every term; dW: every term).
+    const int per = (K + BK - 1) / BK;
+    const int products = kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms;
+    const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;
+    const int nk = KIND == kGtDx ? min(a.ktiles, products * per - first) : products * per;
+    int prod = KIND == kGtDx ? first / per : 0, kt = KIND == kGtDx ? first % per : 0;
+    const uint16_t *pm, *pn, *pn2 = nullptr;
+    const auto begin = [&]() {
+        if constexpr (kTwo) {
+            pm = a.x + m0 * a.ldx;
+            pn = a.Wg + (size_t)n0 * a.m;
+            pn2 = a.Wu + (size_t)n0 * a.m;
+        } else if constexpr (KIND == kGtDx) {
+            pm = a.d + (prod / 2) * plane + (size_t)(prod % 2) * a.f + m0 * ldm + (size_t)kt * BK;
+            pn = (prod % 2 ? a.Wu : a.Wg) + n0 + (size_t)kt * BK * a.m;
+        } else {
+            pm = a.d + prod * plane + (size_t)second * a.f + m0;
+            pn = a.x + n0;
+        }
+    };
+    begin();
+    const uint32_t base = gt_lds(lds);
+    int left = K - kt * BK;
+    const auto issue = [&](int stage) {  // the next tile of k (zeros behind the last)
+        const uint32_t at = base + stage * kStage;
+        tm.load(pm, left, at);
+        tn.load(pn, left, at + TM::kBytes);
+        if constexpr (kTwo)
+            tn.load(pn2, left, at + TM::kBytes + TN::kBytes);
+        pm += KIND == kGtDw ? (size_t)BK * ldm : BK;
+        pn += kTwo ? BK : (size_t)BK * ldn;
+        pn2 += BK;
+        left -= BK;
+        if (!kTwo && left <= 0 && prod + 1 < products) {
+            ++prod;
+            kt = 0;
+            left = K;
+            begin();
+        }
+    };
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave);
+    const int wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN;
+    f32x4_t acc[NP][FN][FM];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                acc[p][i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        issue(s);
+    int stage = 0;
+    for (int t = 0; t < nk; ++t) {
+        gt_wait<kFlight>();  // tile t is there, and every wave is done with tile t - 1
+        issue(stage == 0 ? STAGES - 1 : stage - 1);
+        const char *s = lds + stage * kStage;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            u32x4 vm[FM], vn[NP][FN];
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                vm[j] = TM::read(s, (wm * FM + j) * 16, wk * KK + kk);
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+                    vn[p][i] = TN::read(s + TM::kBytes + p * TN::kBytes, (wn * FN + i) * 16, wk * KK + kk);
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int j = 0; j < FM; ++j)
+                        acc[p][i][j] = mfma16(vn[p][i], vm[j], acc[p][i][j]);
+        }
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    gt_wait<0>();  // no load outlives the workgroup's LDS
+
+    const int lane = threadIdx.x % cdk::kWave;
+    if constexpr (WK > 1) {  // the waves' parts of k, added in their order
+        f32x4_t *sums = reinterpret_cast<f32x4_t *>(lds);
+        const auto at = [&](int w, int p, int i, int j) {
+            return ((((w * WM + wm) * WN + wn) * NP + p) * FN + i) * FM * cdk::kWave + j * cdk::kWave + lane;
+        };
+        if (wk > 0) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int j = 0; j < FM; ++j)
+                        sums[at(wk - 1, p, i, j)] = acc[p][i][j];
+        }
+        __syncthreads();
+        if (wk > 0)
+            return;
+#pragma unroll
+        for (int w = 0; w < WK - 1; ++w)
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int j = 0; j < FM; ++j)
+                        acc[p][i][j] += sums[at(w, p, i, j)];
+    }
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            const int m = m0 + (wm * FM + j) * 16 + lane % 16, n = n0 + (wn * FN + i) * 16 + lane / 16 * 4;
+            if (m >= M || n >= N)
+                continue;
+            if constexpr (KIND == kGtForward) {
+                gt_forward4(a, m, n, acc[0][i][j], acc[1][i][j]);
+            } else if constexpr (KIND == kGtBackward) {
+                gt_backward4(a, m, n, acc[0][i][j], acc[1][i][j]);
+            } else {
+                const float v[4] = {acc[0][i][j][0], acc[0][i][j][1], acc[0][i][j][2], acc[0][i][j][3]};
+                if (KIND == kGtDx && gridDim.y > 1)
+                    gt_store4(a.part + blockIdx.y * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, v);
+                else
+                    gt_store4(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, v);
+            }
+        }
+}
+
+// dx from its parts, in their order; four columns a thread
+__global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a, int splits)
+{
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (size_t)a.T * a.m;
+    if (i >= n)
+        return;
+    f32x4_t s = *reinterpret_cast<const f32x4_t *>(a.part + i);
+    for (int k = 1; k < splits; ++k)
+        s += *reinterpret_cast<const f32x4_t *>(a.part + k * n + i);
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    gt_store4(a.out, a.type, i / a.m * a.ldo + i % a.m, v);
+}
+
+__global__ __launch_bounds__(256) void k_gt_zero(uint32_t *p, size_t words)
+{
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256)
+        p[i] = 0u;
+}
+
+}  // namespace
+
+struct cd_gated {
+    int m, f, max_tokens, device;
+    unsigned flags;
+    void *ws;
+    uint16_t *d;
+    float *part;
+};
+
+namespace {
+
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
+void gt_product(GtArgs a, int M, int N, int splits, hipStream_t s)
+{
+    a.mt = ad_ceil(M, BM);
+    a.nt = ad_ceil(N, BN);
+    if (KIND == kGtDx) {
+        const int all = 2 * a.terms * ad_ceil(a.f, BK);
+        a.ktiles = ad_ceil(all, splits);
+        splits = ad_ceil(all, a.ktiles);
+    }
+    const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
+    k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES>
+        <<<dim3(ad_ceil(tiles, 8) * 8, splits), WM * WN * WK * cdk::kWave, 0, s>>>(a);
+    if (KIND == kGtDx && splits > 1)
+        k_gt_sum<<<(unsigned)(((size_t)a.T * a.m / 4 + 255) / 256), 256, 0, s>>>(a, splits);
+}
+
+// g and u over T tokens, and what KIND makes of them
+template <int KIND>
+void gt_projections(const GtArgs &a, hipStream_t s)
+{
+    if (a.T <= 16)
+        gt_product<KIND, 16, 16, 256, 1, 1, 4, 3>(a, a.T, a.f, 1, s);
+    else if (a.T <= 32)
+        gt_product<KIND, 32, 32, 128, 1, 2, 2, 3>(a, a.T, a.f, 1, s);
+    else if (a.T <= 256)
+        gt_product<KIND, 64, 32, 64, 2, 2, 1, 3>(a, a.T, a.f, 1, s);
+    else
+        gt_product<KIND, 128, 64, 64, 2, 2, 1, 2>(a, a.T, a.f, 1, s);
+}
+
+bool gt_ld_ok(size_t ld, int width) { return ad_ld_ok(ld, width) && ld <= kGtMaxStride; }
+
+// what the two calls share; in: the operands that are read, out: those that are written
+cd_status gt_check(const cd_gated *p, const AdRows *in, int nin, const AdRows *out, int nout)
+{
+    for (int i = 0; i < nout; ++i) {
+        for (int j = 0; j < nin; ++j)
+            if (ad_overlap(out[i], in[j]))
+                return CD_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (ad_overlap(out[i], out[j]))
+                return CD_EINVAL;
+    }
+    int dev = -1;
+    if (hip_status(hipGetDevice(&dev)) != CD_OK)
+        return CD_EHIP;
+    return dev == p->device ? CD_OK : CD_EINVAL;
+}
+
+}  // namespace
+
+extern "C" {
+
+cd_status countdown_gated_create(int d_model, int d_ff, int max_tokens, unsigned flags, cd_gated **out)
+{
+    if (!out || d_model < 8 || d_model % 8 || d_ff < 8 || d_ff % 8 || max_tokens < 1 ||
+        (flags & ~(CD_GATED_TRAIN | CD_GATED_FP32_GRADS)) ||
+        ((flags & CD_GATED_FP32_GRADS) && !(flags & CD_GATED_TRAIN)))
+        return CD_EINVAL;
+    if (d_model > kGtMaxDim || d_ff > kGtMaxDim || max_tokens > kGtMaxTokens)
+        return CD_EUNSUPPORTED;
+    int dev = -1;
+    if (hip_status(hipGetDevice(&dev)) != CD_OK)
+        return CD_EHIP;
+    cd_gated *p = new (std::nothrow) cd_gated{};
+    if (!p)
+        return CD_ENOMEM;
+    p->m = d_model;
+    p->f = d_ff;
+    p->max_tokens = max_tokens;
+    p->flags = flags;
+    p->device = dev;
+    if (flags & CD_GATED_TRAIN) {
+        const size_t terms = flags & CD_GATED_FP32_GRADS ? kGtTerms : 1;
+        const size_t planes = (terms * max_tokens * 2 * d_ff * sizeof(uint16_t) + 255) / 256 * 256;
+        if (hip_status(hipMalloc(&p->ws, planes + kGtPartFloats * sizeof(float))) != CD_OK) {
+            delete p;
+            return CD_ENOMEM;
+        }
+        p->d = static_cast<uint16_t *>(p->ws);
+        p->part = reinterpret_cast<float *>(static_cast<char *>(p->ws) + planes);
+    }
+    *out = p;
+    return CD_OK;
+}
+
+cd_status countdown_gated_destroy(cd_gated *p)
+{
+    if (!p)
+        return CD_OK;
+    int dev = -1;
+    cd_status st = hip_status(hipGetDevice(&dev));
+    if (st == CD_OK)
+        st = hip_status(hipSetDevice(p->device));
+    if (st == CD_OK)
+        st = hip_status(hipDeviceSynchronize());
+    if (p->ws && hip_status(hipFree(p->ws)) != CD_OK)
+        st = CD_EHIP;
+    if (dev >= 0)
+        (void)hip_status(hipSetDevice(dev));
+    delete p;
+    return st;
+}
+
+cd_status countdown_gated_forward(cd_gated *p, const uint16_t *x, size_t ldx, int T,
+                                  const uint16_t *W_gate, const uint16_t *W_up, int type, void *h,
+                                  size_t ldh, void *stream)
+{
+    if (!p || T < 0 || T > p->max_tokens || (type != CD_TYPE_F32 && type != CD_TYPE_BF16) ||
+        !W_gate || !aligned16(W_gate) || !W_up || !aligned16(W_up))
+        return CD_EINVAL;
+    if (T > 0 && (!x || !aligned16(x) || !ad_ld_ok(ldx, p->m) || !h || !aligned16(h) || !ad_ld_ok(ldh, p->f)))
+        return CD_EINVAL;
+    const size_t es = ad_size(type), w = (size_t)p->f * p->m * 2;
+    const AdRows in[] = {{x, (size_t)p->m * 2, ldx * 2, T}, ad_flat(W_gate, w), ad_flat(W_up, w)};
+    const AdRows out[] = {{h, p->f * es, ldh * es, T}};
+    const cd_status st = gt_check(p, in, 3, out, 1);
+    if (st != CD_OK)
+        return st;
+    if (T > 0 && ldx > kGtMaxStride)
+        return CD_EUNSUPPORTED;
+    if (T == 0)
+        return CD_OK;
+    GtArgs a{};
+    a.x = x;
+    a.ldx = ldx;
+    a.Wg = W_gate;
+    a.Wu = W_up;
+    a.T = T;
+    a.m = p->m;
+    a.f = p->f;
+    a.type = type;
+    a.out = h;
+    a.ldo = ldh;
+    gt_projections<kGtForward>(a, reinterpret_cast<hipStream_t>(stream));
+    return launched(hipGetLastError());
+}
+
+cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, const uint16_t *dh,
+                                   size_t lddh, int T, const uint16_t *W_gate, const uint16_t *W_up,
+                                   int type, void *dx, size_t lddx, void *dW_gate, void *dW_up,
+                                   void *stream)
+{
+    if (!p || !(p->flags & CD_GATED_TRAIN) || T < 0 || T > p->max_tokens ||
+        (type != CD_TYPE_F32 && type != CD_TYPE_BF16) ||
+        (type == CD_TYPE_F32 && !(p->flags & CD_GATED_FP32_GRADS)) ||
+        !W_gate || !aligned16(W_gate) || !W_up || !aligned16(W_up) || !aligned16(dW_gate) || !aligned16(dW_up))
+        return CD_EINVAL;
+    if (T > 0 && (!x || !aligned16(x) || !ad_ld_ok(ldx, p->m) || !dh || !aligned16(dh) || !ad_ld_ok(lddh, p->f) ||
+                  (dx && (!aligned16(dx) || !ad_ld_ok(lddx, p->m)))))
+        return CD_EINVAL;
+    const size_t es = ad_size(type), w = (size_t)p->f * p->m;
+    const AdRows in[] = {{x, (size_t)p->m * 2, ldx * 2, T}, {dh, (size_t)p->f * 2, lddh * 2, T},
+                         ad_flat(W_gate, w * 2), ad_flat(W_up, w * 2)};
+    const AdRows out[] = {{dx, p->m * es, lddx * es, T}, ad_flat(dW_gate, w * es), ad_flat(dW_up, w * es)};
+    const cd_status st = gt_check(p, in, 4, out, 3);
+    if (st != CD_OK)
+        return st;
+    if (T > 0 && (ldx > kGtMaxStride || lddh > kGtMaxStride))
+        return CD_EUNSUPPORTED;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (T == 0) {
+        for (void *g : {dW_gate, dW_up})
+            if (g)
+                k_gt_zero<<<1024, 256, 0, s>>>(static_cast<uint32_t *>(g), w * es / 4);
+        return launched(hipGetLastError());
+    }
+    if (!dx && !dW_gate && !dW_up)
+        return CD_OK;
+    GtArgs a{};
+    a.x = x;
+    a.ldx = ldx;
+    a.Wg = W_gate;
+    a.Wu = W_up;
+    a.dh = dh;
+    a.lddh = lddh;
+    a.T = T;
+    a.m = p->m;
+    a.f = p->f;
+    a.type = type;
+    a.d = p->d;
+    a.part = p->part;
+    a.terms = type == CD_TYPE_F32 ? kGtTerms : 1;
+    gt_projections<kGtBackward>(a, s);
+    if (dx) {
+        a.out = dx;
+        a.ldo = lddx;
+        const int tiles = ad_ceil(a.T, 64) * ad_ceil(a.m, 64);
+        const int most = (int)std::min<size_t>(64, kGtPartFloats / ((size_t)a.T * a.m));
+        const int splits = std::max(1, std::min(most, 512 / tiles));
+        if (tiles <= 512)
+            gt_product<kGtDx, 64, 64, 64, 2, 2, 1, 3>(a, a.T, a.m, splits, s);
+        else
+            gt_product<kGtDx, 128, 128, 64, 2, 2, 1, 2>(a, a.T, a.m, 1, s);
+    }
+    if (dW_gate || dW_up) {
+        a.out = dW_gate;
+        a.out2 = dW_up;
+        a.ldo = a.m;
+        if (ad_ceil(a.f, 128) * ad_ceil(a.m, 128) <= 128)
+            gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, 1, s);
+        else
+            gt_product<kGtDw, 128, 128, 64, 2, 2, 1, 2>(a, a.f, a.m, 1, s);
+    }
+    return launched(hipGetLastError());
+}
+
+}  // extern "C"
