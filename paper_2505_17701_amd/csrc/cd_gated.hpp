@@ -47,16 +47,17 @@ struct GtArgs {
 __device__ __forceinline__ u32x4 gt_resource(const uint16_t *p)
 {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
-    return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)kGtOutside, 0x00027000u};
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return u32x4{lo, hi, (uint32_t)kGtOutside, 0x00027000u};
 }
 
 // 16 bytes a lane from the resource to LDS at `lds` + 16 lane. The builtin would do, but the compiler
-// then waits for every load in flight before each LDS read. Nothing is written but LDS; the waits and
-// barriers are gt_wait's.
+// then waits for every load in flight before each LDS read. Nothing is written but LDS and m0 (which
+// compiled code sets where it uses it, and does not in these kernels); the waits and barriers are gt_wait's.
 __device__ __forceinline__ void gt_load_lds(const u32x4 &r, int off, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 ::"s"(lds), "v"(off), "s"(r) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 ::"s"(lds), "v"(off), "s"(r) : "memory");
 }
 
 // All but the last N loads of this wave have come, and its LDS reads; then every wave's have.
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
     tm.init(ldm, M - m0);
     tn.init(ldn, N - n0);
     // The k tiles of this workgroup: of one product after another (dx: dg Wg and du Wu, each for
-    // every term; dW: every term).
+    // every term; dW: every term), the smallest terms first.
     const int per = (K + BK - 1) / BK;
     const int products = kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms;
     const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;
@@ -261,10 +262,10 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
             pn = a.Wg + (size_t)n0 * a.m;
             pn2 = a.Wu + (size_t)n0 * a.m;
         } else if constexpr (KIND == kGtDx) {
-            pm = a.d + (prod / 2) * plane + (size_t)(prod % 2) * a.f + m0 * ldm + (size_t)kt * BK;
+            pm = a.d + (a.terms - 1 - prod / 2) * plane + (size_t)(prod % 2) * a.f + m0 * ldm + (size_t)kt * BK;
             pn = (prod % 2 ? a.Wu : a.Wg) + n0 + (size_t)kt * BK * a.m;
         } else {
-            pm = a.d + prod * plane + (size_t)second * a.f + m0;
+            pm = a.d + (a.terms - 1 - prod) * plane + (size_t)second * a.f + m0;
             pn = a.x + n0;
         }
     };
@@ -380,6 +381,179 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
         }
 }
 
+// Many tiles: 256 x 256 (256 x 128 of both projections), eight waves, each 64 rows of either half of
+// m and 32 of either half of n, so four quarters of 64 x 32 whose operands are read one half at a
+// time. A tile of 64 columns of k takes four phases: read a half's operands and start loading a half
+// tile of k two tiles ahead, then 16 MFMAs a wave. Waves 0-3 and 4-7 (one of each on a SIMD) are half a
+// phase apart: while one half multiplies, the other reads. A half tile read in phase p is overwritten
+// by loads of phase p + 2 or later, when both halves' reads have returned, and is read five
+// phases after its loads were issued, of which the last eight may be in flight.
+template <int KIND>
+__global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
+{
+    constexpr int BK = 64, FM = 4, FN = 2, KK = BK / 32, kFlight = 8;
+    constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
+    using TM = GtTile<128, BK, KIND != kGtDw, 512>;
+    using TN = GtTile<128, BK, kTwo, 512>;
+    constexpr int kHalf = TM::kBytes, kStage = 4 * kHalf;  // m 0, m 1, n 0, n 1
+    static_assert(TM::kBytes == TN::kBytes && TM::kLoads == 2 && TN::kLoads == 2, "loads of a phase");
+    __shared__ __align__(1024) char lds[2 * kStage];
+
+    int mi, ni;
+    if (!gt_place(KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
+        return;
+    const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
+    if (KIND == kGtDw && mi >= a.mt)
+        mi -= a.mt;
+    const int m0 = mi * 256, n0 = ni * (kTwo ? 128 : 256);
+    const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
+    const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
+    const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
+    const size_t plane = (size_t)a.T * 2 * a.f;
+    const int per = (K + BK - 1) / BK;
+    const int products = kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms;
+    const int nk = products * per;
+
+    TM tm[2];
+    TN tn[2];
+    tm[0].init(ldm, M - m0);
+    tm[1].init(ldm, M - m0 - 128);
+    tn[0].init(ldn, N - n0);
+    tn[1].init(ldn, N - n0 - (kTwo ? 0 : 128));
+    const size_t m1 = KIND == kGtDw ? 128 : 128 * ldm, n1 = 128;  // the second halves (k across rows: columns)
+
+    struct Cursor {  // a tile of k
+        const uint16_t *pm, *pn, *pn2;
+        int left;
+    };
+    Cursor c2, c1;  // the tiles whose first and whose second halves are loaded next
+    int prod = 0;
+    const auto begin = [&]() {
+        if constexpr (kTwo) {
+            c2 = {a.x + m0 * a.ldx, a.Wg + (size_t)n0 * a.m, a.Wu + (size_t)n0 * a.m, K};
+        } else if constexpr (KIND == kGtDx) {
+            const int term = a.terms - 1 - prod / 2;
+            const uint16_t *w = (prod % 2 ? a.Wu : a.Wg) + n0;
+            c2 = {a.d + term * plane + (size_t)(prod % 2) * a.f + m0 * ldm, w, w + n1, K};
+        } else {
+            const int term = a.terms - 1 - prod;
+            c2 = {a.d + term * plane + (size_t)second * a.f + m0, a.x + n0, a.x + n0 + n1, K};
+        }
+    };
+    const auto advance = [&]() {
+        c1 = c2;
+        c2.pm += KIND == kGtDw ? (size_t)BK * ldm : BK;
+        c2.pn += kTwo ? BK : (size_t)BK * ldn;
+        c2.pn2 += kTwo ? BK : (size_t)BK * ldn;
+        c2.left -= BK;
+        if (!kTwo && c2.left <= 0 && prod + 1 < products) {
+            ++prod;
+            begin();
+        }
+    };
+    const uint32_t base = gt_lds(lds);
+    begin();
+    tm[0].load(c2.pm, c2.left, base);
+    tn[0].load(c2.pn, c2.left, base + 2 * kHalf);
+    advance();
+    tn[1].load(c1.pn2, c1.left, base + 3 * kHalf);
+    tm[1].load(c1.pm + m1, c1.left, base + kHalf);
+    tm[0].load(c2.pm, c2.left, base + kStage);
+    tn[0].load(c2.pn, c2.left, base + kStage + 2 * kHalf);
+    advance();
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave), lane = threadIdx.x % cdk::kWave;
+    const int wn = wave % 4, wm = wave / 4;
+    f32x4_t acc[2][2][FN][FM];  // halves of n, of m
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                acc[p / 2][p % 2][i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    u32x4 vm[FM][KK], vn[2][FN][KK];
+    const auto read_m = [&](const char *s) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                vm[j][kk] = TM::read(s, (wm * FM + j) * 16, kk);
+    };
+    const auto read_n = [&](u32x4 (&v)[FN][KK], const char *s) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+                v[i][kk] = TN::read(s, (wn * FN + i) * 16, kk);
+    };
+    const auto multiply = [&](int hn, int hm) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j)
+                    acc[hn][hm][i][j] = mfma16(vn[hn][i][kk], vm[j][kk], acc[hn][hm][i][j]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight) : "memory");
+    if (wm == 1)
+        asm volatile("s_barrier" ::: "memory");
+    for (int t = 0; t < nk; ++t) {
+        const int stage = t & 1;
+        const char *s = lds + stage * kStage;
+        const uint32_t here = base + stage * kStage, other = base + (stage ^ 1) * kStage;
+        read_n(vn[0], s + 2 * kHalf);
+        read_m(s);
+        tn[1].load(c1.pn2, c1.left, other + 3 * kHalf);
+        multiply(0, 0);
+        read_n(vn[1], s + 3 * kHalf);
+        tm[1].load(c1.pm + m1, c1.left, other + kHalf);
+        multiply(1, 0);
+        read_m(s + kHalf);
+        tm[0].load(c2.pm, c2.left, here);
+        multiply(0, 1);
+        tn[0].load(c2.pn, c2.left, here + 2 * kHalf);
+        advance();
+        multiply(1, 1);
+    }
+    if (wm == 0)
+        asm volatile("s_barrier" ::: "memory");
+    gt_wait<0>();  // no load outlives the workgroup's LDS
+
+#pragma unroll
+    for (int hm = 0; hm < 2; ++hm)
+#pragma unroll
+        for (int hn = 0; hn < (kTwo ? 1 : 2); ++hn)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j) {
+                    const int m = m0 + hm * 128 + (wm * FM + j) * 16 + lane % 16;
+                    const int n = n0 + hn * 128 + (wn * FN + i) * 16 + lane / 16 * 4;
+                    if (m >= M || n >= N)
+                        continue;
+                    if constexpr (KIND == kGtForward) {
+                        gt_forward4(a, m, n, acc[0][hm][i][j], acc[1][hm][i][j]);
+                    } else if constexpr (KIND == kGtBackward) {
+                        gt_backward4(a, m, n, acc[0][hm][i][j], acc[1][hm][i][j]);
+                    } else {
+                        const f32x4_t &c = acc[hn][hm][i][j];
+                        const float v[4] = {c[0], c[1], c[2], c[3]};
+                        gt_store4(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, v);
+                    }
+                }
+}
+
 // dx from its parts, in their order; four columns a thread
 __global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a, int splits)
 {
@@ -428,6 +602,15 @@ void gt_product(GtArgs a, int M, int N, int splits, hipStream_t s)
         k_gt_sum<<<(unsigned)(((size_t)a.T * a.m / 4 + 255) / 256), 256, 0, s>>>(a, splits);
 }
 
+template <int KIND>
+void gt_large(GtArgs a, int M, int N, hipStream_t s)
+{
+    a.mt = ad_ceil(M, 256);
+    a.nt = ad_ceil(N, KIND == kGtForward || KIND == kGtBackward ? 128 : 256);
+    const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
+    k_gt_large<KIND><<<ad_ceil(tiles, 8) * 8, 512, 0, s>>>(a);
+}
+
 // g and u over T tokens, and what KIND makes of them
 template <int KIND>
 void gt_projections(const GtArgs &a, hipStream_t s)
@@ -438,11 +621,11 @@ void gt_projections(const GtArgs &a, hipStream_t s)
         gt_product<KIND, 32, 32, 128, 1, 2, 2, 3>(a, a.T, a.f, 1, s);
     else if (a.T <= 256)
         gt_product<KIND, 64, 32, 64, 2, 2, 1, 3>(a, a.T, a.f, 1, s);
-    else
+    else if (ad_ceil(a.T, 256) * ad_ceil(a.f, 128) <= 192)
         gt_product<KIND, 128, 64, 64, 2, 2, 1, 2>(a, a.T, a.f, 1, s);
+    else
+        gt_large<KIND>(a, a.T, a.f, s);
 }
-
-bool gt_ld_ok(size_t ld, int width) { return ad_ld_ok(ld, width) && ld <= kGtMaxStride; }
 
 // what the two calls share; in: the operands that are read, out: those that are written
 cd_status gt_check(const cd_gated *p, const AdRows *in, int nin, const AdRows *out, int nout)
@@ -604,8 +787,10 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
         const int splits = std::max(1, std::min(most, 512 / tiles));
         if (tiles <= 512)
             gt_product<kGtDx, 64, 64, 64, 2, 2, 1, 3>(a, a.T, a.m, splits, s);
-        else
+        else if (ad_ceil(a.T, 256) * ad_ceil(a.m, 256) <= 192)
             gt_product<kGtDx, 128, 128, 64, 2, 2, 1, 2>(a, a.T, a.m, 1, s);
+        else
+            gt_large<kGtDx>(a, a.T, a.m, s);
     }
     if (dW_gate || dW_up) {
         a.out = dW_gate;
@@ -613,8 +798,10 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
         a.ldo = a.m;
         if (ad_ceil(a.f, 128) * ad_ceil(a.m, 128) <= 128)
             gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, 1, s);
-        else
+        else if (ad_ceil(a.f, 256) * ad_ceil(a.m, 256) <= 96)
             gt_product<kGtDw, 128, 128, 64, 2, 2, 1, 2>(a, a.f, a.m, 1, s);
+        else
+            gt_large<kGtDw>(a, a.f, a.m, s);
     }
     return launched(hipGetLastError());
 }
