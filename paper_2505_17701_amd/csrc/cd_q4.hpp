@@ -24,8 +24,7 @@ namespace {
 constexpr int kQ4MaxDim = 65536, kQ4Tokens = 16;
 constexpr int kQ4Rows = 16, kQ4Cols = 128;  // of a block
 constexpr int kQ4Waves = 8, kQ4Block = kQ4Waves * cdk::kWave;
-constexpr int kQ4Flight = 4;  // blocks of a wave (and matrix) in flight
-constexpr int kQ4XUnits = 4096;  // 16-byte units of the tokens in LDS
+constexpr int kQ4Step = kQ4Waves * kQ4Cols;  // columns that a workgroup takes at a time
 
 __host__ __device__ constexpr int q4_block(int group) { return 1024 + 32 * (kQ4Cols / group); }
 
@@ -38,29 +37,8 @@ struct Q4Args {
     size_t ldb;
     void *out;
     size_t ldo;
-    int type;   // of base and out
-    int chunk;  // columns that LDS holds of each token
+    int type;  // of base and out
 };
-
-template <int NM, int G>
-struct Q4Block {  // what a lane holds of a block of each of NM matrices
-    u32x4 code[NM];
-    uint64_t scale[NM][kQ4Cols / G];
-};
-
-template <int NM, int G, bool NT>
-__device__ __forceinline__ void q4_load(Q4Block<NM, G> &b, const uint8_t *const (&w)[NM], int kt)
-{
-    const int lane = threadIdx.x % cdk::kWave;
-#pragma unroll
-    for (int q = 0; q < NM; ++q) {
-        const uint8_t *p = w[q] + (size_t)kt * q4_block(G);
-        b.code[q] = ad_load16<NT>(reinterpret_cast<const uint16_t *>(p + lane * 16));
-#pragma unroll
-        for (int g = 0; g < kQ4Cols / G; ++g)
-            b.scale[q][g] = *reinterpret_cast<const uint64_t *>(p + 1024 + g * 32 + lane / 16 * 8);
-    }
-}
 
 // the 8 weights of a word as an MFMA operand, each 24 too large
 __device__ __forceinline__ u32x4 q4_operand(uint32_t w)
@@ -69,115 +47,152 @@ __device__ __forceinline__ u32x4 q4_operand(uint32_t w)
     return u32x4{(w << 3 & mask) | one, (w >> 1 & mask) | one, (w >> 5 & mask) | one, (w >> 9 & mask) | one};
 }
 
-// A workgroup per 16 rows; its waves take the blocks of a row tile in turn.
-template <int NM, int G, bool NT>
+// out of four rows
+__device__ __forceinline__ void q4_store(const Q4Args &a, int t, int row, const f32x4_t &y)
+{
+    float o[4] = {y[0], y[1], y[2], y[3]};
+    const size_t at = t * a.ldb + row;
+    if (a.base && a.type == CD_TYPE_F32) {
+        const f32x4_t b = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(a.base) + at);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            o[r] += b[r];
+    } else if (a.base) {
+        const uint64_t b = *reinterpret_cast<const uint64_t *>(static_cast<const uint16_t *>(a.base) + at);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            o[r] += __uint_as_float((uint32_t)(b >> (16 * r)) << 16);
+    }
+    gt_store4(a.out, a.type, t * a.ldo + row, o);
+}
+
+// A workgroup per 16 rows of both matrices (gated), or NM x 16 rows of one. A step is 1024 columns, a block
+// of each of NM row tiles for each wave; its codes, scales and tokens go to LDS without passing
+// registers, kStages - 1 steps ahead. XL: the loads of tokens that a wave makes for a step, for up to 4 XL tokens.
+template <int NM, int G, int XL, bool GATED>
 __global__ __launch_bounds__(kQ4Block) void k_q4(const Q4Args a)
 {
-    __shared__ u32x4 xs[kQ4XUnits + kQ4Tokens];
+    constexpr int kScale = 32 * (kQ4Cols / G), kCodes = kQ4Waves * NM * 1024, kScales = kQ4Waves * NM * kScale;
+    constexpr int kXRow = kQ4Step * 2 + 16;  // (+ 16: 16 tokens' columns on different banks)
+    constexpr int kStage = kCodes + kScales + 4 * XL * kXRow;
+    // two workgroups a CU with three stages and more, else one
+    constexpr int kStages = 3 * kStage <= 80 * 1024 ? 80 * 1024 / kStage : 160 * 1024 / kStage;
+    constexpr int kLoads = 2 * NM + XL;
+    static_assert(kStages >= 3 && (kStages - 2) * kLoads < 64, "stages");
+    static_assert(kStages * kStage >= kQ4Waves * NM * cdk::kWave * 16, "the waves' sums");
+    __shared__ __align__(1024) char lds[kStages * kStage];
     const int wave = ad_wave(), lane = threadIdx.x % cdk::kWave, i16 = lane % 16, j = lane / 16;
-    const int nkt = (a.cols + kQ4Cols - 1) / kQ4Cols;
-    const size_t tile = (size_t)blockIdx.x * nkt * q4_block(G);
-    const uint8_t *w[NM];
-    w[0] = a.W + tile;
-    if constexpr (NM > 1)
-        w[1] = a.W2 + tile;
-
-    Q4Block<NM, G> blk[kQ4Flight];
+    const int nkt = (a.cols + kQ4Cols - 1) / kQ4Cols, steps = (nkt + kQ4Waves - 1) / kQ4Waves;
+    const int tiles = (a.rows + kQ4Rows - 1) / kQ4Rows;
+    const uint8_t *w[NM];  // this wave's next block
 #pragma unroll
-    for (int d = 0; d < kQ4Flight; ++d)
-        q4_load<NM, G, NT>(blk[d], w, min(wave + d * kQ4Waves, nkt - 1));
+    for (int q = 0; q < NM; ++q) {
+        const int tile = GATED ? (int)blockIdx.x : min((int)blockIdx.x * NM + q, tiles - 1);
+        w[q] = (GATED && q ? a.W2 : a.W) + ((size_t)tile * nkt + wave) * q4_block(G);
+    }
+    // Load i of the tokens is half a step of one of them: 64 lanes of 8 columns.
+    const uint16_t *xp[XL];
+    int xcol[XL];
+    uint32_t xat[XL];
+#pragma unroll
+    for (int i = 0; i < XL; ++i) {
+        const int n = min(wave + i * kQ4Waves, 2 * a.T - 1);  // (past them: the last again)
+        xp[i] = a.x + n / 2 * a.ldx;
+        xcol[i] = n % 2 * 512 + lane * 8;
+        xat[i] = kCodes + kScales + n / 2 * kXRow + n % 2 * 1024;
+    }
+    const uint32_t base = gt_lds(lds);
+    int next = 0;  // the step that is loaded next
+    const auto issue = [&](int stage) {
+        const uint32_t at = base + stage * kStage;
+        const bool in = next * kQ4Waves + wave < nkt;  // uniform
+#pragma unroll
+        for (int q = 0; q < NM; ++q) {
+            const u32x4 r = gt_resource(reinterpret_cast<const uint16_t *>(w[q]));
+            gt_load_lds(r, in ? lane * 16 : kGtOutside, at + (wave * NM + q) * 1024);
+            if (lane < kScale / 16)
+                gt_load_lds(r, in ? 1024 + lane * 16 : kGtOutside, at + kCodes + (wave * NM + q) * kScale);
+            w[q] += kQ4Waves * q4_block(G);
+        }
+#pragma unroll
+        for (int i = 0; i < XL; ++i)
+            gt_load_lds(gt_resource(xp[i]), next * kQ4Step + xcol[i] < a.cols ? (next * kQ4Step + xcol[i]) * 2 : kGtOutside,
+                        at + xat[i]);
+        ++next;
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s)
+        issue(s);
+
     f32x4_t y[NM];
 #pragma unroll
     for (int q = 0; q < NM; ++q)
         y[q] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int units = a.chunk / 8, stride = units + 1;  // (+ 1: 16 tokens' units on different banks)
-    const u32x4 *xr = xs + min(i16, a.T - 1) * stride + j;  // lanes past the tokens read the last one's
     const uint32_t m24 = 0xC1C0C1C0u;
     const u32x4 minus24 = {m24, m24, m24, m24};
-
-    const int steps = (nkt + kQ4Waves - 1) / kQ4Waves, held = a.chunk / (kQ4Cols * kQ4Waves);
-    for (int n0 = 0; n0 < steps; n0 += kQ4Flight) {
+    // lanes past the tokens read the last one's
+    const int xread = kCodes + kScales + min(i16, a.T - 1) * kXRow + wave * (kQ4Cols * 2) + j * 16;
+    int stage = 0;
+    for (int n = 0; n < steps; ++n) {
+        gt_wait<(kStages - 2) * kLoads>();
+        issue(stage == 0 ? kStages - 1 : stage - 1);
+        const char *s = lds + stage * kStage;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        u32x4 xv[4], code[NM];
 #pragma unroll
-        for (int d = 0; d < kQ4Flight; ++d) {
-            const int n = n0 + d, k = n * kQ4Waves + wave;  // (uniform; n for the workgroup)
-            if (n >= steps)
-                break;
-            if (n % held == 0) {  // the next columns of the tokens
-                const int c0 = n * kQ4Waves * kQ4Cols;
-                if (n)
-                    __syncthreads();
-                for (int u = threadIdx.x; u < a.T * units; u += kQ4Block) {
-                    const int t = u / units, c = u % units;
-                    xs[t * stride + c] = load16(or_zero(c0 + c * 8 < a.cols, a.x + t * a.ldx + c0 + c * 8));
-                }
-                __syncthreads();
+        for (int k = 0; k < 4; ++k)
+            xv[k] = *reinterpret_cast<const u32x4 *>(s + xread + k * 64);
+#pragma unroll
+        for (int q = 0; q < NM; ++q)
+            code[q] = *reinterpret_cast<const u32x4 *>(s + (wave * NM + q) * 1024 + lane * 16);
+#pragma unroll
+        for (int g = 0; g < kQ4Cols / G; ++g) {
+            f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < G / 32; ++k)
+                start = mfma16(minus24, xv[g * (G / 32) + k], start);
+#pragma unroll
+            for (int q = 0; q < NM; ++q) {
+                const uint64_t scale =
+                    *reinterpret_cast<const uint64_t *>(s + kCodes + (wave * NM + q) * kScale + g * 32 + j * 8);
+                f32x4_t acc = start;
+#pragma unroll
+                for (int k = 0; k < G / 32; ++k)
+                    acc = mfma16(q4_operand(code[q][g * (G / 32) + k]), xv[g * (G / 32) + k], acc);
+                const uint32_t lo = (uint32_t)scale, hi = (uint32_t)(scale >> 32);
+                y[q][0] += acc[0] * cdk::bf16_lo(lo);
+                y[q][1] += acc[1] * cdk::bf16_hi(lo);
+                y[q][2] += acc[2] * cdk::bf16_lo(hi);
+                y[q][3] += acc[3] * cdk::bf16_hi(hi);
             }
-            if (k < nkt) {
-                const u32x4 *xp = xr + (n % held * kQ4Waves + wave) * (kQ4Cols / 8);
-                u32x4 xv[4];
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    xv[s] = xp[4 * s];
-#pragma unroll
-                for (int g = 0; g < kQ4Cols / G; ++g) {
-                    f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int s = 0; s < G / 32; ++s)
-                        start = mfma16(minus24, xv[g * (G / 32) + s], start);
-#pragma unroll
-                    for (int q = 0; q < NM; ++q) {
-                        f32x4_t acc = start;
-#pragma unroll
-                        for (int s = 0; s < G / 32; ++s)
-                            acc = mfma16(q4_operand(blk[d].code[q][g * (G / 32) + s]), xv[g * (G / 32) + s], acc);
-                        const uint32_t lo = (uint32_t)blk[d].scale[q][g], hi = (uint32_t)(blk[d].scale[q][g] >> 32);
-                        y[q][0] += acc[0] * cdk::bf16_lo(lo);
-                        y[q][1] += acc[1] * cdk::bf16_hi(lo);
-                        y[q][2] += acc[2] * cdk::bf16_lo(hi);
-                        y[q][3] += acc[3] * cdk::bf16_hi(hi);
-                    }
-                }
-            }
-            q4_load<NM, G, NT>(blk[d], w, min(k + kQ4Flight * kQ4Waves, nkt - 1));
         }
     }
-    f32x4_t *sums = reinterpret_cast<f32x4_t *>(xs);  // [NM][waves][lane]
-    __syncthreads();
+    gt_wait<0>();  // no load outlives the workgroup's LDS
+
+    f32x4_t *sums = reinterpret_cast<f32x4_t *>(lds);  // [NM][waves][lane]
 #pragma unroll
     for (int q = 0; q < NM; ++q)
         sums[(q * kQ4Waves + wave) * cdk::kWave + lane] = y[q];
     __syncthreads();
-    const int row = blockIdx.x * kQ4Rows + j * 4;
-    if (wave > 0 || i16 >= a.T || row >= a.rows)
+    const auto total = [&](int q) {
+        f32x4_t v = sums[q * kQ4Waves * cdk::kWave + lane];
+#pragma unroll
+        for (int k = 1; k < kQ4Waves; ++k)
+            v += sums[(q * kQ4Waves + k) * cdk::kWave + lane];
+        return v;
+    };
+    if (GATED ? wave > 0 : wave >= NM)
         return;
-#pragma unroll
-    for (int q = 0; q < NM; ++q)
-        for (int v = 1; v < kQ4Waves; ++v)
-            y[q] += sums[(q * kQ4Waves + v) * cdk::kWave + lane];
-    float o[4];
-    if constexpr (NM > 1) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            o[r] = cdk::silu(y[0][r]) * y[1][r];
+    const int row = (GATED ? (int)blockIdx.x : (int)blockIdx.x * NM + wave) * kQ4Rows + j * 4;
+    if (i16 >= a.T || row >= a.rows)
+        return;
+    if constexpr (GATED) {
+        const f32x4_t g = total(0), u = total(1);
+        q4_store(a, i16, row, f32x4_t{cdk::silu(g[0]) * u[0], cdk::silu(g[1]) * u[1], cdk::silu(g[2]) * u[2],
+                                      cdk::silu(g[3]) * u[3]});
     } else {
-        const size_t at = i16 * a.ldb + row;
-        if (!a.base) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                o[r] = y[0][r];
-        } else if (a.type == CD_TYPE_F32) {
-            const f32x4_t b = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(a.base) + at);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                o[r] = b[r] + y[0][r];
-        } else {
-            const uint64_t b = *reinterpret_cast<const uint64_t *>(static_cast<const uint16_t *>(a.base) + at);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                o[r] = __uint_as_float((uint32_t)(b >> (16 * r)) << 16) + y[0][r];
-        }
+        q4_store(a, i16, row, total(wave));
     }
-    gt_store4(a.out, a.type, i16 * a.ldo + row, o);
 }
 
 // The four words' place of 8 columns (c: a multiple of 8) of a row, and its scale's.
@@ -285,27 +300,27 @@ size_t q4_bytes(int rows, int cols, int group)
     return (size_t)ad_ceil(rows, kQ4Rows) * ad_ceil(cols, kQ4Cols) * q4_block(group);
 }
 
-template <int NM, int G>
+template <int NM, int G, bool GATED>
 void q4_launch(const Q4Args &a, hipStream_t s)
 {
-    const int grid = ad_ceil(a.rows, kQ4Rows);
-    if (NM * q4_bytes(a.rows, a.cols, G) > ((size_t)64 << 20))
-        k_q4<NM, G, true><<<grid, kQ4Block, 0, s>>>(a);
+    const int grid = ad_ceil(a.rows, kQ4Rows * (GATED ? 1 : NM));
+    if (a.T <= 4)
+        k_q4<NM, G, 1, GATED><<<grid, kQ4Block, 0, s>>>(a);
+    else if (a.T <= 8)
+        k_q4<NM, G, 2, GATED><<<grid, kQ4Block, 0, s>>>(a);
     else
-        k_q4<NM, G, false><<<grid, kQ4Block, 0, s>>>(a);
+        k_q4<NM, G, 4, GATED><<<grid, kQ4Block, 0, s>>>(a);
 }
 
-template <int NM>
-cd_status q4_run(Q4Args a, int group, hipStream_t s)
+template <int NM, bool GATED>
+cd_status q4_run(const Q4Args &a, int group, hipStream_t s)
 {
-    const int whole = ad_ceil(a.cols, kQ4Cols * kQ4Waves) * kQ4Cols * kQ4Waves;
-    a.chunk = std::min(whole, kQ4XUnits / a.T / (kQ4Cols * kQ4Waves / 8) * (kQ4Cols * kQ4Waves));
     if (group == 32)
-        q4_launch<NM, 32>(a, s);
+        q4_launch<NM, 32, GATED>(a, s);
     else if (group == 64)
-        q4_launch<NM, 64>(a, s);
+        q4_launch<NM, 64, GATED>(a, s);
     else
-        q4_launch<NM, 128>(a, s);
+        q4_launch<NM, 128, GATED>(a, s);
     return launched(hipGetLastError());
 }
 
@@ -397,18 +412,22 @@ cd_status countdown_q4_project(const uint16_t *x, size_t ldx, int T, const void 
                                int group, int type, const void *base, size_t ldb, void *y, size_t ldy,
                                void *stream)
 {
-    const Q4Args a{x, ldx, static_cast<const uint8_t *>(W), nullptr, T, d_out, d_in, base, ldb, y, ldy, type, 0};
+    const Q4Args a{x, ldx, static_cast<const uint8_t *>(W), nullptr, T, d_out, d_in, base, ldb, y, ldy, type};
     const cd_status st = q4_check(a, group, false);
-    return st != CD_OK || T == 0 ? st : q4_run<1>(a, group, reinterpret_cast<hipStream_t>(stream));
+    if (st != CD_OK || T == 0)
+        return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    // two row tiles a workgroup, which then read the tokens once, where enough workgroups are left
+    return d_out >= 32 * 224 ? q4_run<2, false>(a, group, s) : q4_run<1, false>(a, group, s);
 }
 
 cd_status countdown_q4_gated(const uint16_t *x, size_t ldx, int T, const void *W_gate, const void *W_up,
                              int d_model, int d_ff, int group, int type, void *h, size_t ldh, void *stream)
 {
     const Q4Args a{x, ldx, static_cast<const uint8_t *>(W_gate), static_cast<const uint8_t *>(W_up), T, d_ff,
-                   d_model, nullptr, 0, h, ldh, type, 0};
+                   d_model, nullptr, 0, h, ldh, type};
     const cd_status st = q4_check(a, group, true);
-    return st != CD_OK || T == 0 ? st : q4_run<2>(a, group, reinterpret_cast<hipStream_t>(stream));
+    return st != CD_OK || T == 0 ? st : q4_run<2, true>(a, group, reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
