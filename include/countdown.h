@@ -525,9 +525,10 @@ cd_status countdown_gated_backward(cd_gated *gated, const uint16_t *x, size_t ld
  * group 32, 64 or 128 (the last group of a row may be shorter), rows and cols positive multiples
  * of 8 up to 65536. It is kept in a packed DEVICE buffer of countdown_q4_bytes bytes, owned by the
  * caller, 16-byte aligned, written whole by countdown_q4_quantize or countdown_q4_pack: blocks of
- * 16 rows x 128 columns, a row tile's blocks one after another; a block holds 1024
- * bytes of codes, then 16 scales for each of its 128 / group groups. Bytes 16 l..16 l + 15 of the
- * codes (l = 16 j + i) are row i; the 32-bit word k of them has columns 32 k + 8 j + e, the code of
+ * 16 rows x 128 columns, those of 16 rows one after another in groups of eight blocks (the last may
+ * have fewer); a group holds 1024 bytes of codes for each block, then 16 scales for each of the
+ * 128 / group groups of columns of each block. Bytes 16 l..16 l + 15 of a block's codes
+ * (l = 16 j + i) are row i; the 32-bit word k of them has columns 32 k + 8 j + e, the code of
  * e = 2 p plus 8 at bits 4 p, that of e = 2 p + 1 at bits 16 + 4 p. Padding has code 0, scale 0.
  *
  * Products and sums are fp32: a code enters as 24 + code and 24 times the group's sum of x leaves

@@ -44,7 +44,7 @@ struct GtArgs {
 };
 
 // a buffer resource over 2^30 bytes at p (uniform): what lies past them reads as zero
-__device__ __forceinline__ u32x4 gt_resource(const uint16_t *p)
+__device__ __forceinline__ u32x4 gt_resource(const void *p)
 {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
@@ -54,10 +54,16 @@ __device__ __forceinline__ u32x4 gt_resource(const uint16_t *p)
 // 16 bytes a lane from the resource to LDS at `lds` + 16 lane. The builtin would do, but the compiler
 // then waits for every load in flight before each LDS read. Nothing is written but LDS and m0 (which
 // compiled code sets where it uses it, and does not in these kernels); the waits and barriers are gt_wait's.
+// NT: past the caches.
+template <bool NT = false>
 __device__ __forceinline__ void gt_load_lds(const u32x4 &r, int off, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 ::"s"(lds), "v"(off), "s"(r) : "memory");
+    if constexpr (NT)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+                     ::"s"(lds), "v"(off), "s"(r) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     ::"s"(lds), "v"(off), "s"(r) : "memory");
 }
 
 // All but the last N loads of this wave have come, and its LDS reads; then every wave's have.

@@ -10,11 +10,12 @@
 // of -24 and the same tokens, that the sums of a group start from. Sums are fp32, the group's scale
 // multiplies a group's sum, not its weights.
 //
-// Packed layout: blocks of 16 rows x 128 columns, the blocks of 16 rows one after another. A block is
-// 1024 bytes of codes and 32 for each of its 128 / G groups (the 16 rows' scales). Lane l = 16 j + i of
-// a wave owns bytes 16 l..16 l + 15: word w holds row i, columns 32 w + 8 j + e; the code of e = 2 p lies
-// at bits 4 p, that of e = 2 p + 1 at bits 16 + 4 p, each as c + 8. So a wave's load is 1 KB on end
-// and each word is an operand. Rows and columns that pad the matrix have code 0 and scale 0.
+// Packed layout: blocks of 16 rows x 128 columns, the blocks of 16 rows one after another in groups of eight
+// (the last group may have fewer): the codes of a group's blocks, 1024 bytes each, then their
+// scales, 32 bytes for each of the 128 / G groups of columns of a block (16 rows). Lane l = 16 j + i of
+// a wave owns bytes 16 l..16 l + 15 of a block's codes: word w holds row i, columns 32 w + 8 j + e; the code of
+// e = 2 p lies at bits 4 p, that of e = 2 p + 1 at bits 16 + 4 p, each as c + 8. So a wave's load is 1 KB
+// on end and each word is an operand. Rows and columns that pad the matrix have code 0 and scale 0.
 #pragma once
 
 #include "cd_device.hpp"
@@ -23,10 +24,22 @@ namespace {
 
 constexpr int kQ4MaxDim = 65536, kQ4Tokens = 16;
 constexpr int kQ4Rows = 16, kQ4Cols = 128;  // of a block
-constexpr int kQ4Waves = 8, kQ4Block = kQ4Waves * cdk::kWave;
-constexpr int kQ4Step = kQ4Waves * kQ4Cols;  // columns that a workgroup takes at a time
+
+constexpr int kQ4Group = 8;  // blocks whose codes lie together
 
 __host__ __device__ constexpr int q4_block(int group) { return 1024 + 32 * (kQ4Cols / group); }
+
+// byte offsets of a block's codes and scales from its row tile of nkt blocks (at most 512 of 1152 bytes)
+__host__ __device__ constexpr int q4_codes_at(int kt, int group)
+{
+    return kt / kQ4Group * kQ4Group * q4_block(group) + kt % kQ4Group * 1024;
+}
+
+__host__ __device__ constexpr int q4_scales_at(int kt, int nkt, int group)
+{
+    const int first = kt / kQ4Group * kQ4Group, n = nkt - first < kQ4Group ? nkt - first : kQ4Group;
+    return first * q4_block(group) + n * 1024 + (kt - first) * 32 * (kQ4Cols / group);
+}
 
 struct Q4Args {
     const uint16_t *x;
@@ -41,9 +54,8 @@ struct Q4Args {
 };
 
 // the 8 weights of a word as an MFMA operand, each 24 too large
-__device__ __forceinline__ u32x4 q4_operand(uint32_t w)
+__device__ __forceinline__ u32x4 q4_operand(uint32_t w, uint32_t mask, uint32_t one)
 {
-    constexpr uint32_t mask = 0x00780078u, one = 0x41804180u;
     return u32x4{(w << 3 & mask) | one, (w >> 1 & mask) | one, (w >> 5 & mask) | one, (w >> 9 & mask) | one};
 }
 
@@ -66,77 +78,118 @@ __device__ __forceinline__ void q4_store(const Q4Args &a, int t, int row, const 
     gt_store4(a.out, a.type, t * a.ldo + row, o);
 }
 
-// A workgroup per 16 rows of both matrices (gated), or NM x 16 rows of one. A step is 1024 columns, a block
-// of each of NM row tiles for each wave; its codes, scales and tokens go to LDS without passing
-// registers, kStages - 1 steps ahead. XL: the loads of tokens that a wave makes for a step, for up to 4 XL tokens.
-template <int NM, int G, int XL, bool GATED>
-__global__ __launch_bounds__(kQ4Block) void k_q4(const Q4Args a)
+// Stages of LDS: what leaves two workgroups a CU, if that is three, else three; at most four (each costs
+// its loads before the first product)
+__host__ __device__ constexpr int q4_stages(int stage)
 {
-    constexpr int kScale = 32 * (kQ4Cols / G), kCodes = kQ4Waves * NM * 1024, kScales = kQ4Waves * NM * kScale;
-    constexpr int kXRow = kQ4Step * 2 + 16;  // (+ 16: 16 tokens' columns on different banks)
-    constexpr int kStage = kCodes + kScales + 4 * XL * kXRow;
-    // two workgroups a CU with three stages and more, else one
-    constexpr int kStages = 3 * kStage <= 80 * 1024 ? 80 * 1024 / kStage : 160 * 1024 / kStage;
-    constexpr int kLoads = 2 * NM + XL;
-    static_assert(kStages >= 3 && (kStages - 2) * kLoads < 64, "stages");
-    static_assert(kStages * kStage >= kQ4Waves * NM * cdk::kWave * 16, "the waves' sums");
+    const int n = 80 * 1024 / stage;
+    return n < 3 ? 3 : n < 4 ? n : 4;
+}
+
+// A part is 16 rows of both matrices (gated), or NM x 16 rows of one; a workgroup takes part after part. A
+// step is 1024 columns, a block of each of NM row tiles for each wave; its codes, scales and tokens go to
+// LDS without passing registers, kStages - 1 steps ahead, the next part's while the last one ends.
+// XT: the tokens that LDS has room for.
+template <int NM, int G, int XT, int WAVES, bool GATED, bool NT>
+__global__ __launch_bounds__(WAVES *cdk::kWave) void k_q4(const Q4Args a)
+{
+    constexpr int kStep = WAVES * kQ4Cols, kHalf = cdk::kWave * 8;  // columns of a step, of a load
+    constexpr int kScale = 32 * (kQ4Cols / G), kCodes = WAVES * NM * 1024, kScales = WAVES * NM * kScale;
+    constexpr int kXRow = kStep * 2 + 16;  // (+ 16: 16 tokens' columns on different banks)
+    constexpr int kStage = kCodes + kScales + XT * kXRow;
+    constexpr int XL = XT > 4 ? XT / 4 : 1;  // the loads of tokens that a wave makes for a step
+    constexpr int kStages = q4_stages(kStage);
+    static_assert(XL * WAVES >= XT * (kStep / kHalf) && WAVES % NM == 0 && (kStages - 2) * (NM + 1 + XL) < 64, "loads");
     __shared__ __align__(1024) char lds[kStages * kStage];
     const int wave = ad_wave(), lane = threadIdx.x % cdk::kWave, i16 = lane % 16, j = lane / 16;
-    const int nkt = (a.cols + kQ4Cols - 1) / kQ4Cols, steps = (nkt + kQ4Waves - 1) / kQ4Waves;
+    const int nkt = (a.cols + kQ4Cols - 1) / kQ4Cols, steps = (nkt + WAVES - 1) / WAVES;
     const int tiles = (a.rows + kQ4Rows - 1) / kQ4Rows;
-    const uint8_t *w[NM];  // this wave's next block
+    const int parts = (tiles + (GATED ? 0 : NM - 1)) / (GATED ? 1 : NM);
+    const uint8_t *w[NM];  // the row tiles that are loaded next
+    int ahead = blockIdx.x, next = 0;  // their part, and the step
+    const auto begin = [&]() {
 #pragma unroll
-    for (int q = 0; q < NM; ++q) {
-        const int tile = GATED ? (int)blockIdx.x : min((int)blockIdx.x * NM + q, tiles - 1);
-        w[q] = (GATED && q ? a.W2 : a.W) + ((size_t)tile * nkt + wave) * q4_block(G);
-    }
-    // Load i of the tokens is half a step of one of them: 64 lanes of 8 columns.
+        for (int q = 0; q < NM; ++q) {
+            const int tile = GATED ? ahead : min(ahead * NM + q, tiles - 1);
+            w[q] = (GATED && q ? a.W2 : a.W) + (size_t)tile * nkt * q4_block(G);
+        }
+    };
+    begin();
+    // Load i of the tokens: 64 lanes of 8 columns of one of them. With many tokens every wave makes as
+    // many loads a step (past the last token that one again) and takes the scales of NM blocks; with few, waves
+    // without a token make fewer, and wave q takes all scales of matrix q. (One way for all: 8192 -> 28672 gated at
+    // one token 48.7 us against 46.8, 3000 -> 8008 at 16 tokens 7.6 against 7.4.)
+    constexpr bool kEven = XL > 2;
+    constexpr int kPer = kStep / kHalf;
     const uint16_t *xp[XL];
-    int xcol[XL];
+    int xcol[XL], xloads = 0;
     uint32_t xat[XL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-        const int n = min(wave + i * kQ4Waves, 2 * a.T - 1);  // (past them: the last again)
-        xp[i] = a.x + n / 2 * a.ldx;
-        xcol[i] = n % 2 * 512 + lane * 8;
-        xat[i] = kCodes + kScales + n / 2 * kXRow + n % 2 * 1024;
+        const int n = min(wave + i * WAVES, kPer * a.T - 1);
+        xloads += kEven || wave + i * WAVES < kPer * a.T;
+        xp[i] = a.x + n / kPer * a.ldx;
+        xcol[i] = n % kPer * kHalf + lane * 8;
+        xat[i] = kCodes + kScales + n / kPer * kXRow + n % kPer * 1024;
     }
+    const int sq = kEven ? wave % NM : wave, sfirst = kEven ? wave / NM * NM : 0;
+    constexpr int kSLanes = (kEven ? NM : WAVES) * kScale / 16;
+    const int loads = xloads + (kEven || wave < NM);
+    const auto wait = [&]() {  // the loads of the last kStages - 2 steps may be in flight
+#pragma unroll
+        for (int n = kEven ? XL + 1 : 0; n <= XL + 1; ++n)
+            if (kEven || loads == n)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * (NM + n)) : "memory");
+        asm volatile("s_barrier" ::: "memory");
+    };
     const uint32_t base = gt_lds(lds);
-    int next = 0;  // the step that is loaded next
     const auto issue = [&](int stage) {
         const uint32_t at = base + stage * kStage;
-        const bool in = next * kQ4Waves + wave < nkt;  // uniform
+        const int first = next * WAVES, kt = first + wave;
+        const bool in = ahead < parts;  // uniform
 #pragma unroll
-        for (int q = 0; q < NM; ++q) {
-            const u32x4 r = gt_resource(reinterpret_cast<const uint16_t *>(w[q]));
-            gt_load_lds(r, in ? lane * 16 : kGtOutside, at + (wave * NM + q) * 1024);
-            if (lane < kScale / 16)
-                gt_load_lds(r, in ? 1024 + lane * 16 : kGtOutside, at + kCodes + (wave * NM + q) * kScale);
-            w[q] += kQ4Waves * q4_block(G);
+        for (int q = 0; q < NM; ++q)
+            gt_load_lds<NT>(gt_resource(w[q] + q4_codes_at(kt, G)), in && kt < nkt ? lane * 16 : kGtOutside,
+                            at + (q * WAVES + wave) * 1024);
+        if ((kEven || wave < NM) && lane < kSLanes) {
+            const u32x4 r = gt_resource((sq ? w[NM - 1] : w[0]) + q4_scales_at(first + sfirst, nkt, G));
+            gt_load_lds<NT>(r, in && lane * 16 < (nkt - first - sfirst) * kScale ? lane * 16 : kGtOutside,
+                            at + kCodes + (sq * WAVES + sfirst) * kScale);
         }
 #pragma unroll
         for (int i = 0; i < XL; ++i)
-            gt_load_lds(gt_resource(xp[i]), next * kQ4Step + xcol[i] < a.cols ? (next * kQ4Step + xcol[i]) * 2 : kGtOutside,
-                        at + xat[i]);
-        ++next;
+            if (kEven || i < xloads)
+                gt_load_lds(gt_resource(xp[i]), next * kStep + xcol[i] < a.cols ? (next * kStep + xcol[i]) * 2 : kGtOutside,
+                            at + xat[i]);
+        if (++next == steps) {
+            next = 0;
+            ahead += gridDim.x;
+            begin();
+        }
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s)
         issue(s);
 
+    const uint32_t m24 = 0xC1C0C1C0u;
+    const u32x4 minus24 = {m24, m24, m24, m24};
+    // In registers, which the compiler cannot see through: as literals they would cost an instruction more a pair.
+    uint32_t mask, one;
+    asm("s_mov_b32 %0, 0x00780078" : "=s"(mask));
+    asm("v_mov_b32 %0, 0x41804180" : "=v"(one));
+    // lanes past the tokens read the last one's
+    const int xread = kCodes + kScales + min(i16, a.T - 1) * kXRow + wave * (kQ4Cols * 2) + j * 16;
+    int stage = 0;
+    for (int part = blockIdx.x; part < parts; part += gridDim.x) {
     f32x4_t y[NM];
 #pragma unroll
     for (int q = 0; q < NM; ++q)
         y[q] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const uint32_t m24 = 0xC1C0C1C0u;
-    const u32x4 minus24 = {m24, m24, m24, m24};
-    // lanes past the tokens read the last one's
-    const int xread = kCodes + kScales + min(i16, a.T - 1) * kXRow + wave * (kQ4Cols * 2) + j * 16;
-    int stage = 0;
+    char *done = lds;  // the last step's codes
     for (int n = 0; n < steps; ++n) {
-        gt_wait<(kStages - 2) * kLoads>();
+        wait();
         issue(stage == 0 ? kStages - 1 : stage - 1);
-        const char *s = lds + stage * kStage;
+        char *s = done = lds + stage * kStage;
         stage = stage + 1 == kStages ? 0 : stage + 1;
         u32x4 xv[4], code[NM];
 #pragma unroll
@@ -144,7 +197,7 @@ __global__ __launch_bounds__(kQ4Block) void k_q4(const Q4Args a)
             xv[k] = *reinterpret_cast<const u32x4 *>(s + xread + k * 64);
 #pragma unroll
         for (int q = 0; q < NM; ++q)
-            code[q] = *reinterpret_cast<const u32x4 *>(s + (wave * NM + q) * 1024 + lane * 16);
+            code[q] = *reinterpret_cast<const u32x4 *>(s + (q * WAVES + wave) * 1024 + lane * 16);
 #pragma unroll
         for (int g = 0; g < kQ4Cols / G; ++g) {
             f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -154,11 +207,11 @@ __global__ __launch_bounds__(kQ4Block) void k_q4(const Q4Args a)
 #pragma unroll
             for (int q = 0; q < NM; ++q) {
                 const uint64_t scale =
-                    *reinterpret_cast<const uint64_t *>(s + kCodes + (wave * NM + q) * kScale + g * 32 + j * 8);
+                    *reinterpret_cast<const uint64_t *>(s + kCodes + (q * WAVES + wave) * kScale + g * 32 + j * 8);
                 f32x4_t acc = start;
 #pragma unroll
                 for (int k = 0; k < G / 32; ++k)
-                    acc = mfma16(q4_operand(code[q][g * (G / 32) + k]), xv[g * (G / 32) + k], acc);
+                    acc = mfma16(q4_operand(code[q][g * (G / 32) + k], mask, one), xv[g * (G / 32) + k], acc);
                 const uint32_t lo = (uint32_t)scale, hi = (uint32_t)(scale >> 32);
                 y[q][0] += acc[0] * cdk::bf16_lo(lo);
                 y[q][1] += acc[1] * cdk::bf16_hi(lo);
@@ -167,25 +220,25 @@ __global__ __launch_bounds__(kQ4Block) void k_q4(const Q4Args a)
             }
         }
     }
-    gt_wait<0>();  // no load outlives the workgroup's LDS
-
-    f32x4_t *sums = reinterpret_cast<f32x4_t *>(lds);  // [NM][waves][lane]
+    // The waves' sums, each over the codes that it alone read. (They are read before the next barrier,
+    // and overwritten by loads after it.)
 #pragma unroll
     for (int q = 0; q < NM; ++q)
-        sums[(q * kQ4Waves + wave) * cdk::kWave + lane] = y[q];
-    __syncthreads();
+        reinterpret_cast<f32x4_t *>(done)[(q * WAVES + wave) * cdk::kWave + lane] = y[q];
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (GATED ? wave > 0 : wave >= NM)
+        continue;
     const auto total = [&](int q) {
-        f32x4_t v = sums[q * kQ4Waves * cdk::kWave + lane];
+        const f32x4_t *sums = reinterpret_cast<const f32x4_t *>(done) + q * WAVES * cdk::kWave + lane;
+        f32x4_t v = sums[0];
 #pragma unroll
-        for (int k = 1; k < kQ4Waves; ++k)
-            v += sums[(q * kQ4Waves + k) * cdk::kWave + lane];
+        for (int k = 1; k < WAVES; ++k)
+            v += sums[k * cdk::kWave];
         return v;
     };
-    if (GATED ? wave > 0 : wave >= NM)
-        return;
-    const int row = (GATED ? (int)blockIdx.x : (int)blockIdx.x * NM + wave) * kQ4Rows + j * 4;
+    const int row = (GATED ? part : part * NM + wave) * kQ4Rows + j * 4;
     if (i16 >= a.T || row >= a.rows)
-        return;
+        continue;
     if constexpr (GATED) {
         const f32x4_t g = total(0), u = total(1);
         q4_store(a, i16, row, f32x4_t{cdk::silu(g[0]) * u[0], cdk::silu(g[1]) * u[1], cdk::silu(g[2]) * u[2],
@@ -193,19 +246,21 @@ __global__ __launch_bounds__(kQ4Block) void k_q4(const Q4Args a)
     } else {
         q4_store(a, i16, row, total(wave));
     }
+    }
+    gt_wait<0>();  // no load outlives the workgroup's LDS
 }
 
-// The four words' place of 8 columns (c: a multiple of 8) of a row, and its scale's.
+// The place of the word of 8 columns (c: a multiple of 8) of a row, and of a group's scale.
 __device__ __forceinline__ size_t q4_word_at(int row, int c, int nkt, int group)
 {
-    return ((size_t)(row / kQ4Rows) * nkt + c / kQ4Cols) * q4_block(group) +
+    return (size_t)(row / kQ4Rows) * nkt * q4_block(group) + q4_codes_at(c / kQ4Cols, group) +
            (16 * (c % 32 / 8) + row % kQ4Rows) * 16 + c % kQ4Cols / 32 * 4;
 }
 
 __device__ __forceinline__ size_t q4_scale_at(int row, int g, int nkt, int group)
 {
     const int c = g * group;
-    return ((size_t)(row / kQ4Rows) * nkt + c / kQ4Cols) * q4_block(group) + 1024 +
+    return (size_t)(row / kQ4Rows) * nkt * q4_block(group) + q4_scales_at(c / kQ4Cols, nkt, group) +
            c % kQ4Cols / group * 32 + row % kQ4Rows * 2;
 }
 
@@ -300,16 +355,40 @@ size_t q4_bytes(int rows, int cols, int group)
     return (size_t)ad_ceil(rows, kQ4Rows) * ad_ceil(cols, kQ4Cols) * q4_block(group);
 }
 
+template <int NM, int G, int XT, int W, bool GATED>
+void q4_launch(const Q4Args &a, int parts, hipStream_t s)
+{
+    // persistent: as many workgroups as run at once
+    constexpr int stage = W * NM * q4_block(G) + XT * (W * kQ4Cols * 2 + 16);
+    const int grid = std::min(parts, 256 * (160 * 1024 / (q4_stages(stage) * stage)));
+    if ((GATED ? 2 : 1) * q4_bytes(a.rows, a.cols, G) > ((size_t)64 << 20))
+        k_q4<NM, G, XT, W, GATED, true><<<grid, W * cdk::kWave, 0, s>>>(a);
+    else
+        k_q4<NM, G, XT, W, GATED, false><<<grid, W * cdk::kWave, 0, s>>>(a);
+}
+
+template <int NM, int G, int XT, bool GATED>
+void q4_launch(const Q4Args &a, hipStream_t s)
+{
+    const int parts = ad_ceil(a.rows, kQ4Rows * (GATED ? 1 : NM));
+    constexpr int W1 = XT > 8 ? 8 : 8, W2 = XT > 8 ? 4 : 8;
+    if (parts <= 256)
+        q4_launch<NM, G, XT, W1, GATED>(a, parts, s);
+    else
+        q4_launch<NM, G, XT, W2, GATED>(a, parts, s);
+}
+
 template <int NM, int G, bool GATED>
 void q4_launch(const Q4Args &a, hipStream_t s)
 {
-    const int grid = ad_ceil(a.rows, kQ4Rows * (GATED ? 1 : NM));
-    if (a.T <= 4)
-        k_q4<NM, G, 1, GATED><<<grid, kQ4Block, 0, s>>>(a);
+    if (a.T == 1)
+        q4_launch<NM, G, 1, GATED>(a, s);
+    else if (a.T <= 4)
+        q4_launch<NM, G, 4, GATED>(a, s);
     else if (a.T <= 8)
-        k_q4<NM, G, 2, GATED><<<grid, kQ4Block, 0, s>>>(a);
+        q4_launch<NM, G, 8, GATED>(a, s);
     else
-        k_q4<NM, G, 4, GATED><<<grid, kQ4Block, 0, s>>>(a);
+        q4_launch<NM, G, 16, GATED>(a, s);
 }
 
 template <int NM, bool GATED>
