@@ -21,7 +21,7 @@ constexpr int kGtMaxDim = 65536, kGtMaxTokens = 1 << 20;
 constexpr size_t kGtMaxStride = (size_t)1 << 20;  // row strides: 256 rows stay below 2^30 bytes
 constexpr int kGtTerms = 3;                       // bf16 terms of an fp32 number
 constexpr int kGtOutside = 0x40000000;            // an offset past every resource: reads zeros
-constexpr size_t kGtPartFloats = (size_t)4 << 20; // place for dx's partial sums (16 MiB)
+constexpr size_t kGtPartFloats = (size_t)16 << 20; // place for dx's partial sums (64 MiB)
 
 enum GtKind { kGtForward, kGtBackward, kGtDx, kGtDw };
 
@@ -172,29 +172,45 @@ __device__ __forceinline__ void gt_store4(void *out, int type, size_t i, const f
     }
 }
 
+// 1 / (1 + exp(-g)) to a few units in the last place, on the hardware's exp2 and reciprocal: with the
+// library's expf and division the last step of a 256 x 256 tile costs three times the instructions. exp2's
+// argument is rounded, for large |g| by more than exp2 itself; its rounding error goes back in as a factor.
+__device__ __forceinline__ float gt_sigmoid(float g)
+{
+    constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147182f;
+    const float t = -g * log2e;
+    const float err = fmaf(-g, rest, fmaf(-g, log2e, -t));
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(err, ln2, 1.0f));
+}
+
 // h of four neurons
 __device__ __forceinline__ void gt_forward4(const GtArgs &a, size_t t, int n, const f32x4_t &g, const f32x4_t &u)
 {
     float v[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-        v[r] = cdk::silu(g[r]) * u[r];
+        v[r] = g[r] * gt_sigmoid(g[r]) * u[r];
     gt_store4(a.out, a.type, t * a.ldo + n, v);
 }
 
-// dg and du of four neurons, in a.terms bf16 terms: one is rounded to nearest even, the operand that
-// a bf16 product takes; two hold 16 bits, three all of an fp32 number.
-__device__ __forceinline__ void gt_backward4(const GtArgs &a, size_t t, int n, const f32x4_t &g, const f32x4_t &u)
+__device__ __forceinline__ uint64_t gt_dh(const GtArgs &a, int t, int n)
 {
-    const uint64_t w = *reinterpret_cast<const uint64_t *>(a.dh + t * a.lddh + n);
+    return *reinterpret_cast<const uint64_t *>(or_zero(t < a.T && n < a.f, a.dh + (size_t)t * a.lddh + n));
+}
+
+// dg and du of four neurons, in a.terms bf16 terms: one is rounded to nearest even, the operand that
+// a bf16 product takes; two hold 16 bits, three all of an fp32 number. w: dh of the four.
+__device__ __forceinline__ void gt_backward4(const GtArgs &a, size_t t, int n, uint64_t w, const f32x4_t &g,
+                                             const f32x4_t &u)
+{
     float d[2][4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const uint32_t p = (uint32_t)(w >> (r / 2 * 32));
         const float dh = r % 2 ? cdk::bf16_hi(p) : cdk::bf16_lo(p);
-        const float s = 1.0f / (1.0f + expf(-g[r]));
+        const float s = gt_sigmoid(g[r]);
         d[0][r] = dh * u[r] * (s * (1.0f + g[r] * (1.0f - s)));
-        d[1][r] = dh * cdk::silu(g[r]);
+        d[1][r] = dh * (g[r] * s);
     }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -366,6 +382,14 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
                     for (int j = 0; j < FM; ++j)
                         acc[p][i][j] += sums[at(w, p, i, j)];
     }
+    uint64_t dh[FN][FM];  // all loads before the first is used
+    if constexpr (KIND == kGtBackward) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                dh[i][j] = gt_dh(a, m0 + (wm * FM + j) * 16 + lane % 16, n0 + (wn * FN + i) * 16 + lane / 16 * 4);
+    }
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
@@ -376,7 +400,7 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
             if constexpr (KIND == kGtForward) {
                 gt_forward4(a, m, n, acc[0][i][j], acc[1][i][j]);
             } else if constexpr (KIND == kGtBackward) {
-                gt_backward4(a, m, n, acc[0][i][j], acc[1][i][j]);
+                gt_backward4(a, m, n, dh[i][j], acc[0][i][j], acc[1][i][j]);
             } else {
                 const float v[4] = {acc[0][i][j][0], acc[0][i][j][1], acc[0][i][j][2], acc[0][i][j][3]};
                 if (KIND == kGtDx && gridDim.y > 1)
@@ -394,16 +418,19 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
 // phase apart: while one half multiplies, the other reads. A half tile read in phase p is overwritten
 // by loads of phase p + 2 or later, when both halves' reads have returned, and is read five
 // phases after its loads were issued, of which the last eight may be in flight.
-template <int KIND>
+// MH 1: one half of m alone, 128 x 256, two phases a tile of k and three tiles in LDS; the loads are
+// issued four phases before they are read, and ten (eight) of them may be in flight.
+template <int KIND, int MH>
 __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
 {
     constexpr int BK = 64, FM = 4, FN = 2, KK = BK / 32, kFlight = 8;
     constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
     using TM = GtTile<128, BK, KIND != kGtDw, 512>;
     using TN = GtTile<128, BK, kTwo, 512>;
-    constexpr int kHalf = TM::kBytes, kStage = 4 * kHalf;  // m 0, m 1, n 0, n 1
+    constexpr int kHalf = TM::kBytes, kStages = 4 - MH, kStage = (MH + 2) * kHalf;  // m 0, (m 1,) n 0, n 1
+    constexpr int kN0 = MH * kHalf, kN1 = kN0 + kHalf;
     static_assert(TM::kBytes == TN::kBytes && TM::kLoads == 2 && TN::kLoads == 2, "loads of a phase");
-    __shared__ __align__(1024) char lds[2 * kStage];
+    __shared__ __align__(1024) char lds[kStages * kStage];
 
     int mi, ni;
     if (!gt_place(KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
@@ -411,19 +438,21 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
     if (KIND == kGtDw && mi >= a.mt)
         mi -= a.mt;
-    const int m0 = mi * 256, n0 = ni * (kTwo ? 128 : 256);
+    const int m0 = mi * (128 * MH), n0 = ni * (kTwo ? 128 : 256);
     const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
     const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
     const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
     const size_t plane = (size_t)a.T * 2 * a.f;
     const int per = (K + BK - 1) / BK;
     const int products = kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms;
-    const int nk = products * per;
+    const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;  // dx: a split of the tiles of k
+    const int nk = KIND == kGtDx ? min(a.ktiles, products * per - first) : products * per;
 
-    TM tm[2];
+    TM tm[MH];
     TN tn[2];
     tm[0].init(ldm, M - m0);
-    tm[1].init(ldm, M - m0 - 128);
+    if constexpr (MH == 2)
+        tm[1].init(ldm, M - m0 - 128);
     tn[0].init(ldn, N - n0);
     tn[1].init(ldn, N - n0 - (kTwo ? 0 : 128));
     const size_t m1 = KIND == kGtDw ? 128 : 128 * ldm, n1 = 128;  // the second halves (k across rows: columns)
@@ -433,14 +462,14 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         int left;
     };
     Cursor c2, c1;  // the tiles whose first and whose second halves are loaded next
-    int prod = 0;
+    int prod = KIND == kGtDx ? first / per : 0, kt = KIND == kGtDx ? first % per : 0;
     const auto begin = [&]() {
         if constexpr (kTwo) {
             c2 = {a.x + m0 * a.ldx, a.Wg + (size_t)n0 * a.m, a.Wu + (size_t)n0 * a.m, K};
         } else if constexpr (KIND == kGtDx) {
             const int term = a.terms - 1 - prod / 2;
-            const uint16_t *w = (prod % 2 ? a.Wu : a.Wg) + n0;
-            c2 = {a.d + term * plane + (size_t)(prod % 2) * a.f + m0 * ldm, w, w + n1, K};
+            const uint16_t *w = (prod % 2 ? a.Wu : a.Wg) + n0 + (size_t)kt * BK * a.m;
+            c2 = {a.d + term * plane + (size_t)(prod % 2) * a.f + m0 * ldm + (size_t)kt * BK, w, w + n1, K - kt * BK};
         } else {
             const int term = a.terms - 1 - prod;
             c2 = {a.d + term * plane + (size_t)second * a.f + m0, a.x + n0, a.x + n0 + n1, K};
@@ -454,30 +483,34 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         c2.left -= BK;
         if (!kTwo && c2.left <= 0 && prod + 1 < products) {
             ++prod;
+            kt = 0;
             begin();
         }
     };
     const uint32_t base = gt_lds(lds);
     begin();
     tm[0].load(c2.pm, c2.left, base);
-    tn[0].load(c2.pn, c2.left, base + 2 * kHalf);
+    tn[0].load(c2.pn, c2.left, base + kN0);
     advance();
-    tn[1].load(c1.pn2, c1.left, base + 3 * kHalf);
-    tm[1].load(c1.pm + m1, c1.left, base + kHalf);
+    tn[1].load(c1.pn2, c1.left, base + kN1);
+    if constexpr (MH == 2)
+        tm[1].load(c1.pm + m1, c1.left, base + kHalf);
     tm[0].load(c2.pm, c2.left, base + kStage);
-    tn[0].load(c2.pn, c2.left, base + kStage + 2 * kHalf);
+    tn[0].load(c2.pn, c2.left, base + kStage + kN0);
+    if constexpr (MH == 1)
+        tn[1].load(c2.pn2, c2.left, base + kStage + kN1);
     advance();
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave), lane = threadIdx.x % cdk::kWave;
     const int wn = wave % 4, wm = wave / 4;
-    f32x4_t acc[2][2][FN][FM];  // halves of n, of m
+    f32x4_t acc[2][MH][FN][FM];  // halves of n, of m
 #pragma unroll
-    for (int p = 0; p < 4; ++p)
+    for (int p = 0; p < 2 * MH; ++p)
 #pragma unroll
         for (int i = 0; i < FN; ++i)
 #pragma unroll
             for (int j = 0; j < FM; ++j)
-                acc[p / 2][p % 2][i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                acc[p / MH][p % MH][i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     u32x4 vm[FM][KK], vn[2][FN][KK];
     const auto read_m = [&](const char *s) {
 #pragma unroll
@@ -495,7 +528,10 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     };
     const auto multiply = [&](int hn, int hm) {
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight) : "memory");
+        if (MH == 1 && hn == 0)
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight + 2) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight) : "memory");
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -514,30 +550,55 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight) : "memory");
     if (wm == 1)
         asm volatile("s_barrier" ::: "memory");
+    int stage = 0;
     for (int t = 0; t < nk; ++t) {
-        const int stage = t & 1;
         const char *s = lds + stage * kStage;
-        const uint32_t here = base + stage * kStage, other = base + (stage ^ 1) * kStage;
-        read_n(vn[0], s + 2 * kHalf);
-        read_m(s);
-        tn[1].load(c1.pn2, c1.left, other + 3 * kHalf);
-        multiply(0, 0);
-        read_n(vn[1], s + 3 * kHalf);
-        tm[1].load(c1.pm + m1, c1.left, other + kHalf);
-        multiply(1, 0);
-        read_m(s + kHalf);
-        tm[0].load(c2.pm, c2.left, here);
-        multiply(0, 1);
-        tn[0].load(c2.pn, c2.left, here + 2 * kHalf);
-        advance();
-        multiply(1, 1);
+        const uint32_t here = base + stage * kStage;
+        const uint32_t other = base + (stage == 0 ? kStages - 1 : stage - 1) * kStage;
+        if constexpr (MH == 2) {
+            read_n(vn[0], s + kN0);
+            read_m(s);
+            tn[1].load(c1.pn2, c1.left, other + kN1);
+            multiply(0, 0);
+            read_n(vn[1], s + kN1);
+            tm[1].load(c1.pm + m1, c1.left, other + kHalf);
+            multiply(1, 0);
+            read_m(s + kHalf);
+            tm[0].load(c2.pm, c2.left, here);
+            multiply(0, 1);
+            tn[0].load(c2.pn, c2.left, here + kN0);
+            advance();
+            multiply(1, 1);
+        } else {
+            read_n(vn[0], s + kN0);
+            read_m(s);
+            tm[0].load(c2.pm, c2.left, other);
+            tn[0].load(c2.pn, c2.left, other + kN0);
+            multiply(0, 0);
+            read_n(vn[1], s + kN1);
+            tn[1].load(c2.pn2, c2.left, other + kN1);
+            advance();
+            multiply(1, 0);
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
     }
     if (wm == 0)
         asm volatile("s_barrier" ::: "memory");
     gt_wait<0>();  // no load outlives the workgroup's LDS
 
+    uint64_t dh[MH][FN][FM];  // all loads before the first is used
+    if constexpr (KIND == kGtBackward) {
 #pragma unroll
-    for (int hm = 0; hm < 2; ++hm)
+        for (int hm = 0; hm < MH; ++hm)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j)
+                    dh[hm][i][j] = gt_dh(a, m0 + hm * 128 + (wm * FM + j) * 16 + lane % 16,
+                                         n0 + (wn * FN + i) * 16 + lane / 16 * 4);
+    }
+#pragma unroll
+    for (int hm = 0; hm < MH; ++hm)
 #pragma unroll
         for (int hn = 0; hn < (kTwo ? 1 : 2); ++hn)
 #pragma unroll
@@ -551,11 +612,14 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
                     if constexpr (KIND == kGtForward) {
                         gt_forward4(a, m, n, acc[0][hm][i][j], acc[1][hm][i][j]);
                     } else if constexpr (KIND == kGtBackward) {
-                        gt_backward4(a, m, n, acc[0][hm][i][j], acc[1][hm][i][j]);
+                        gt_backward4(a, m, n, dh[hm][i][j], acc[0][hm][i][j], acc[1][hm][i][j]);
                     } else {
                         const f32x4_t &c = acc[hn][hm][i][j];
                         const float v[4] = {c[0], c[1], c[2], c[3]};
-                        gt_store4(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, v);
+                        if (KIND == kGtDx && gridDim.y > 1)
+                            gt_store4(a.part + blockIdx.y * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, v);
+                        else
+                            gt_store4(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, v);
                     }
                 }
 }
@@ -567,6 +631,7 @@ __global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a, int splits)
     if (i >= n)
         return;
     f32x4_t s = *reinterpret_cast<const f32x4_t *>(a.part + i);
+#pragma unroll 8
     for (int k = 1; k < splits; ++k)
         s += *reinterpret_cast<const f32x4_t *>(a.part + k * n + i);
     const float v[4] = {s[0], s[1], s[2], s[3]};
@@ -591,46 +656,95 @@ struct cd_gated {
 
 namespace {
 
-template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
-void gt_product(GtArgs a, int M, int N, int splits, hipStream_t s)
+// dx: the tiles of k of a workgroup, and how many workgroups then share a tile of dx
+int gt_split(GtArgs &a, int BK, int splits)
 {
-    a.mt = ad_ceil(M, BM);
-    a.nt = ad_ceil(N, BN);
-    if (KIND == kGtDx) {
-        const int all = 2 * a.terms * ad_ceil(a.f, BK);
-        a.ktiles = ad_ceil(all, splits);
-        splits = ad_ceil(all, a.ktiles);
-    }
-    const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
-    k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES>
-        <<<dim3(ad_ceil(tiles, 8) * 8, splits), WM * WN * WK * cdk::kWave, 0, s>>>(a);
-    if (KIND == kGtDx && splits > 1)
+    const int all = 2 * a.terms * ad_ceil(a.f, BK);
+    a.ktiles = ad_ceil(all, std::max(1, std::min(splits, all / 4)));
+    return ad_ceil(all, a.ktiles);
+}
+
+void gt_sum(const GtArgs &a, int splits, hipStream_t s)
+{
+    if (splits > 1)
         k_gt_sum<<<(unsigned)(((size_t)a.T * a.m / 4 + 255) / 256), 256, 0, s>>>(a, splits);
 }
 
-template <int KIND>
-void gt_large(GtArgs a, int M, int N, hipStream_t s)
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
+void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
-    a.mt = ad_ceil(M, 256);
-    a.nt = ad_ceil(N, KIND == kGtForward || KIND == kGtBackward ? 128 : 256);
+    a.mt = ad_ceil(M, BM);
+    a.nt = ad_ceil(N, BN);
+    splits = KIND == kGtDx ? gt_split(a, BK, splits) : 1;
     const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
-    k_gt_large<KIND><<<ad_ceil(tiles, 8) * 8, 512, 0, s>>>(a);
+    k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES>
+        <<<dim3(ad_ceil(tiles, 8) * 8, splits), WM * WN * WK * cdk::kWave, 0, s>>>(a);
+    gt_sum(a, splits, s);
 }
 
-// g and u over T tokens, and what KIND makes of them
+template <int KIND, int MH>
+void gt_large(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
+{
+    a.mt = ad_ceil(M, 128 * MH);
+    a.nt = ad_ceil(N, KIND == kGtForward || KIND == kGtBackward ? 128 : 256);
+    splits = KIND == kGtDx ? gt_split(a, 64, splits) : 1;
+    const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
+    k_gt_large<KIND, MH><<<dim3(ad_ceil(tiles, 8) * 8, splits), 512, 0, s>>>(a);
+    gt_sum(a, splits, s);
+}
+
+// 256 x 256 against 128 x 256: rounds of workgroups over the CUs, of which the former's take half as long again
+bool gt_wide(int64_t wide, int64_t narrow) { return 3 * ((wide + 255) / 256) <= 2 * ((narrow + 255) / 256); }
+
+// g and u over T tokens, and what KIND makes of them: the smallest tile that makes one round of
+// workgroups over the 256 CUs.
 template <int KIND>
 void gt_projections(const GtArgs &a, hipStream_t s)
 {
+    const auto fits = [&](int bm, int bn) { return (int64_t)ad_ceil(a.T, bm) * ad_ceil(a.f, bn) <= 256; };
     if (a.T <= 16)
-        gt_product<KIND, 16, 16, 256, 1, 1, 4, 3>(a, a.T, a.f, 1, s);
-    else if (a.T <= 32)
-        gt_product<KIND, 32, 32, 128, 1, 2, 2, 3>(a, a.T, a.f, 1, s);
-    else if (a.T <= 256)
-        gt_product<KIND, 64, 32, 64, 2, 2, 1, 3>(a, a.T, a.f, 1, s);
-    else if (ad_ceil(a.T, 256) * ad_ceil(a.f, 128) <= 192)
-        gt_product<KIND, 128, 64, 64, 2, 2, 1, 2>(a, a.T, a.f, 1, s);
+        gt_product<KIND, 16, 16, 256, 1, 1, 4, 3>(a, a.T, a.f, s);
+    else if (fits(32, 32))
+        gt_product<KIND, 32, 32, 128, 1, 2, 2, 4>(a, a.T, a.f, s);
+    else if (fits(64, 32))
+        gt_product<KIND, 64, 32, 128, 2, 2, 1, 4>(a, a.T, a.f, s);
+    else if (fits(64, 64))
+        gt_product<KIND, 64, 64, 128, 2, 4, 1, 3>(a, a.T, a.f, s);
+    else if (fits(128, 64))
+        gt_product<KIND, 128, 64, 64, 2, 4, 1, 3>(a, a.T, a.f, s);
+    else if (fits(192, 64))
+        gt_product<KIND, 192, 64, 64, 4, 2, 1, 3>(a, a.T, a.f, s);
+    else if (fits(128, 128) || !gt_wide((int64_t)ad_ceil(a.T, 256) * ad_ceil(a.f, 128),
+                                        (int64_t)ad_ceil(a.T, 128) * ad_ceil(a.f, 128)))
+        gt_large<KIND, 1>(a, a.T, a.f, s);
     else
-        gt_large<KIND>(a, a.T, a.f, s);
+        gt_large<KIND, 2>(a, a.T, a.f, s);
+}
+
+void gt_dx(const GtArgs &a, hipStream_t s)
+{
+    // workgroups that share a tile: one round over the CUs, and what the place for their sums holds
+    const int most = (int)std::min<size_t>(64, kGtPartFloats / ((size_t)a.T * a.m));
+    const auto splits = [&](int bm, int bn, int slots) {
+        return std::max(1, (int)std::min<int64_t>(most, slots / ((int64_t)ad_ceil(a.T, bm) * ad_ceil(a.m, bn))));
+    };
+    if (a.T <= 16)
+        gt_product<kGtDx, 16, 128, 128, 1, 2, 2, 2>(a, a.T, a.m, s, splits(16, 128, 512));
+    else if (a.T <= 64 || (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 128) <= 128)
+        gt_product<kGtDx, 64, 128, 64, 2, 2, 1, 3>(a, a.T, a.m, s, splits(64, 128, 512));
+    else
+        gt_large<kGtDx, 2>(a, a.T, a.m, s, splits(256, 256, 256));
+}
+
+void gt_dw(const GtArgs &a, hipStream_t s)
+{
+    const auto tiles = [&](int b) { return (int64_t)ad_ceil(a.f, b) * ad_ceil(a.m, b) * 2; };  // of both gradients
+    if (tiles(64) <= 512)
+        gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, s);
+    else if (tiles(128) <= 512)
+        gt_product<kGtDw, 128, 128, 64, 2, 2, 1, 2>(a, a.f, a.m, s);
+    else
+        gt_large<kGtDw, 2>(a, a.f, a.m, s);
 }
 
 // what the two calls share; in: the operands that are read, out: those that are written
@@ -788,26 +902,13 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     if (dx) {
         a.out = dx;
         a.ldo = lddx;
-        const int tiles = ad_ceil(a.T, 64) * ad_ceil(a.m, 64);
-        const int most = (int)std::min<size_t>(64, kGtPartFloats / ((size_t)a.T * a.m));
-        const int splits = std::max(1, std::min(most, 512 / tiles));
-        if (tiles <= 512)
-            gt_product<kGtDx, 64, 64, 64, 2, 2, 1, 3>(a, a.T, a.m, splits, s);
-        else if (ad_ceil(a.T, 256) * ad_ceil(a.m, 256) <= 192)
-            gt_product<kGtDx, 128, 128, 64, 2, 2, 1, 2>(a, a.T, a.m, 1, s);
-        else
-            gt_large<kGtDx>(a, a.T, a.m, s);
+        gt_dx(a, s);
     }
     if (dW_gate || dW_up) {
         a.out = dW_gate;
         a.out2 = dW_up;
         a.ldo = a.m;
-        if (ad_ceil(a.f, 128) * ad_ceil(a.m, 128) <= 128)
-            gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, 1, s);
-        else if (ad_ceil(a.f, 256) * ad_ceil(a.m, 256) <= 96)
-            gt_product<kGtDw, 128, 128, 64, 2, 2, 1, 2>(a, a.f, a.m, 1, s);
-        else
-            gt_large<kGtDw>(a, a.f, a.m, s);
+        gt_dw(a, s);
     }
     return launched(hipGetLastError());
 }

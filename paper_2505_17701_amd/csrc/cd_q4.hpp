@@ -241,8 +241,8 @@ __global__ __launch_bounds__(WAVES *cdk::kWave) void k_q4(const Q4Args a)
         continue;
     if constexpr (GATED) {
         const f32x4_t g = total(0), u = total(1);
-        q4_store(a, i16, row, f32x4_t{cdk::silu(g[0]) * u[0], cdk::silu(g[1]) * u[1], cdk::silu(g[2]) * u[2],
-                                      cdk::silu(g[3]) * u[3]});
+        q4_store(a, i16, row, f32x4_t{g[0] * gt_sigmoid(g[0]) * u[0], g[1] * gt_sigmoid(g[1]) * u[1],
+                                      g[2] * gt_sigmoid(g[2]) * u[2], g[3] * gt_sigmoid(g[3]) * u[3]});
     } else {
         q4_store(a, i16, row, total(wave));
     }

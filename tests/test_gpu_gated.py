@@ -94,6 +94,11 @@ SHAPES = [  # T, d_model, d_ff: every tile, its edges, one element of a tile, wh
     (32, 256, 512), (33, 136, 200), (64, 512, 256), (65, 1032, 136), (129, 64, 328), (256, 200, 64),
     (257, 328, 712), (300, 1000, 264), (512, 256, 512), (777, 264, 1032), (1025, 520, 136),
     (1300, 1544, 2056), (2048, 512, 1024), (4100, 72, 136),
+    # tiles of the projections by how many workgroups they make (test_host_gated_q4.py names them)
+    (100, 200, 2200), (200, 136, 3000), (500, 72, 3000), (700, 72, 3504), (900, 72, 4000), (2000, 264, 4104),
+    (384, 72, 16640),
+    # dx in one part; the gradients of the weights in 256 x 256 tiles, of few and of many tokens
+    (4100, 2104, 72), (70, 1032, 4104), (300, 2104, 2600), (1, 1032, 4104),
 ]
 
 

@@ -83,7 +83,7 @@ def test_a_failed_allocation_leaves_nothing(host):
 
 @pytest.mark.parametrize("flags,bytes_each", [(1, 4), (3, 12)])
 def test_the_workspace_takes_what_the_header_says(host, flags, bytes_each):
-    most = bytes_each * T * F + (16 << 20)
+    most = bytes_each * T * F + (64 << 20)
     for limit, status in ((most + 256, 0), (most - 1, host.cd.CD_ENOMEM)):
         host.limit(limit)
         try:
@@ -129,6 +129,39 @@ def test_backward_refuses(host, gated, kw):
     host.launches()
     assert backward(host, gated, **kw) == host.cd.CD_EINVAL
     assert host.launches() == []
+
+
+FWD = ["k_gt_product<%d,16,16,", "k_gt_product<%d,32,32,", "k_gt_product<%d,64,32,", "k_gt_product<%d,64,64,",
+       "k_gt_product<%d,128,64,", "k_gt_product<%d,192,64,", "k_gt_large<%d,1>", "k_gt_large<%d,2>"]
+
+
+@pytest.mark.parametrize("shape,proj,dx,dw", [  # T, d_model, d_ff; the kernels by what they start with
+    ((1, 256, 688), 0, "k_gt_product<2,16,128,", "k_gt_product<3,64,64,"),
+    ((16, 4096, 14336), 0, "k_gt_product<2,16,128,", "k_gt_large<3,2>"),
+    ((17, 256, 688), 1, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((100, 200, 2200), 2, "k_gt_large<2,1>", "k_gt_product<3,64,64,"),
+    ((200, 136, 3000), 3, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
+    ((500, 72, 3000), 4, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
+    ((700, 72, 3504), 5, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
+    ((900, 72, 4000), 6, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
+    ((384, 72, 16640), 6, "k_gt_large<2,1>", "k_gt_product<3,128,128,"),
+    ((2000, 264, 4104), 7, "k_gt_large<2,2>", "k_gt_product<3,128,128,"),
+    ((1300, 1544, 2056), 5, "k_gt_large<2,1>", "k_gt_product<3,128,128,"),
+    ((70, 1032, 4104), 3, "k_gt_large<2,1>", "k_gt_large<3,2>"),
+    ((8192, 4096, 14336), 7, "k_gt_large<2,2>", "k_gt_large<3,2>"),
+], ids=str)
+def test_kernels_by_the_sizes(host, shape, proj, dx, dw):
+    T, m, f = shape
+    st, h = create(host, m, f, T, 1)
+    assert st == 0
+    host.launches()
+    far = dict(ldx=m, T=T, Wg=P["Wg"], Wu=P["Wu"])
+    assert forward(host, h, ldh=f, **far) == 0
+    assert [k.startswith(FWD[proj] % 0) for k, _ in host.launches()] == [True]
+    assert backward(host, h, lddh=f, lddx=m, type=1, **far) == 0
+    got = [k for k, _ in host.launches() if k != "k_gt_sum"]
+    assert host.lib.countdown_gated_destroy(h) == 0
+    assert len(got) == 3 and got[0].startswith(FWD[proj] % 1) and got[1].startswith(dx) and got[2].startswith(dw), got
 
 
 def test_strides_past_what_the_kernels_reach(host, gated):
