@@ -412,18 +412,17 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
 }
 
 // Many tiles: 256 x 256 (256 x 128 of both projections), eight waves, each 64 rows of either half of
-// m and 32 of either half of n, so four quarters of 64 x 32 whose operands are read one half at a
-// time. A tile of 64 columns of k takes four phases: read a half's operands and start loading a half
-// tile of k two tiles ahead, then 16 MFMAs a wave. Waves 0-3 and 4-7 (one of each on a SIMD) are half a
-// phase apart: while one half multiplies, the other reads. A half tile read in phase p is overwritten
-// by loads of phase p + 2 or later, when both halves' reads have returned, and is read five
-// phases after its loads were issued, of which the last eight may be in flight.
-// MH 1: one half of m alone, 128 x 256, two phases a tile of k and three tiles in LDS; the loads are
-// issued four phases before they are read, and ten (eight) of them may be in flight.
+// m and 32 of either half of n. A tile of 64 columns of k takes two phases, one for each half of m: read the
+// operands and start loading what is needed three phases later, then 32 MFMAs a wave. Waves 0-3
+// and 4-7 (one of each on a SIMD) are half a phase apart: while one half multiplies, the other
+// reads. A wave's LDS reads have returned when it passes the barrier behind them, so a half tile read
+// in phase p may be overwritten by loads of phase p + 1; of the loads the last eight may be in flight.
+// MH 1: one half of m alone, 128 x 256, a phase a tile of k and three tiles in LDS; the loads are
+// issued two phases before they are read, and six of them may be in flight.
 template <int KIND, int MH>
 __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
 {
-    constexpr int BK = 64, FM = 4, FN = 2, KK = BK / 32, kFlight = 8;
+    constexpr int BK = 64, FM = 4, FN = 2, KK = BK / 32, kFlight = MH == 2 ? 8 : 6;
     constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
     using TM = GtTile<128, BK, KIND != kGtDw, 512>;
     using TN = GtTile<128, BK, kTwo, 512>;
@@ -488,18 +487,17 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         }
     };
     const uint32_t base = gt_lds(lds);
+    const auto load0 = [&](uint32_t at) {  // all but the second half of m
+        tm[0].load(c2.pm, c2.left, at);
+        tn[0].load(c2.pn, c2.left, at + kN0);
+        tn[1].load(c2.pn2, c2.left, at + kN1);
+        advance();
+    };
     begin();
-    tm[0].load(c2.pm, c2.left, base);
-    tn[0].load(c2.pn, c2.left, base + kN0);
-    advance();
-    tn[1].load(c1.pn2, c1.left, base + kN1);
+    load0(base);
     if constexpr (MH == 2)
         tm[1].load(c1.pm + m1, c1.left, base + kHalf);
-    tm[0].load(c2.pm, c2.left, base + kStage);
-    tn[0].load(c2.pn, c2.left, base + kStage + kN0);
-    if constexpr (MH == 1)
-        tn[1].load(c2.pn2, c2.left, base + kStage + kN1);
-    advance();
+    load0(base + kStage);
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave), lane = threadIdx.x % cdk::kWave;
     const int wn = wave % 4, wm = wave / 4;
@@ -526,21 +524,20 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
             for (int i = 0; i < FN; ++i)
                 v[i][kk] = TN::read(s, (wn * FN + i) * 16, kk);
     };
-    const auto multiply = [&](int hn, int hm) {
+    const auto multiply = [&](int hm) {
         __builtin_amdgcn_sched_barrier(0);
-        if (MH == 1 && hn == 0)
-            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight + 2) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kFlight) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kFlight) : "memory");
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
+        for (int hn = 0; hn < 2; ++hn)
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
+            for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-                for (int j = 0; j < FM; ++j)
-                    acc[hn][hm][i][j] = mfma16(vn[hn][i][kk], vm[j][kk], acc[hn][hm][i][j]);
+                for (int i = 0; i < FN; ++i)
+#pragma unroll
+                    for (int j = 0; j < FM; ++j)
+                        acc[hn][hm][i][j] = mfma16(vn[hn][i][kk], vm[j][kk], acc[hn][hm][i][j]);
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_barrier" ::: "memory");
@@ -555,30 +552,18 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         const char *s = lds + stage * kStage;
         const uint32_t here = base + stage * kStage;
         const uint32_t other = base + (stage == 0 ? kStages - 1 : stage - 1) * kStage;
+        read_n(vn[0], s + kN0);
+        read_n(vn[1], s + kN1);
+        read_m(s);
         if constexpr (MH == 2) {
-            read_n(vn[0], s + kN0);
-            read_m(s);
-            tn[1].load(c1.pn2, c1.left, other + kN1);
-            multiply(0, 0);
-            read_n(vn[1], s + kN1);
             tm[1].load(c1.pm + m1, c1.left, other + kHalf);
-            multiply(1, 0);
+            multiply(0);
             read_m(s + kHalf);
-            tm[0].load(c2.pm, c2.left, here);
-            multiply(0, 1);
-            tn[0].load(c2.pn, c2.left, here + kN0);
-            advance();
-            multiply(1, 1);
+            load0(here);
+            multiply(1);
         } else {
-            read_n(vn[0], s + kN0);
-            read_m(s);
-            tm[0].load(c2.pm, c2.left, other);
-            tn[0].load(c2.pn, c2.left, other + kN0);
-            multiply(0, 0);
-            read_n(vn[1], s + kN1);
-            tn[1].load(c2.pn2, c2.left, other + kN1);
-            advance();
-            multiply(1, 0);
+            load0(other);
+            multiply(0);
         }
         stage = stage + 1 == kStages ? 0 : stage + 1;
     }
