@@ -119,13 +119,14 @@ struct GtTile {
     }
 
     // the tile at base (uniform), of whose k `left` remain
+    template <bool NT = false>
     __device__ __forceinline__ void load(const uint16_t *base, int left, uint32_t lds) const
     {
         const u32x4 r = gt_resource(base);
         const uint32_t at = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave) * 1024;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            gt_load_lds(r, k[i] < left ? off[i] : kGtOutside, at + i * (THREADS * 16));
+            gt_load_lds<NT>(r, k[i] < left ? off[i] : kGtOutside, at + i * (THREADS * 16));
     }
 
     // operand of rows r0..r0 + 15 and k 32 kk..32 kk + 31 (lane: row lane % 16, k 8 (lane / 16)..)
@@ -150,14 +151,15 @@ struct GtTile {
 // stretch of n, so that its L2 holds what they share. False: no tile.
 __device__ __forceinline__ bool gt_place(int mt, int nt, int &mi, int &ni)
 {
-    constexpr int group = 8;
+    constexpr int group = 4;
     const int total = mt * nt, per = (total + 7) / 8;
     const int t = (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8;
     if ((int)blockIdx.x / 8 >= per || t >= total)
         return false;
     const int width = group * nt, first = t / width * group, rows = min(group, mt - first);
-    mi = first + t % width % rows;
-    ni = t % width / rows;
+    // known to be uniform: what follows from them stays in scalar registers
+    mi = __builtin_amdgcn_readfirstlane(first + t % width % rows);
+    ni = __builtin_amdgcn_readfirstlane(t % width / rows);
     return true;
 }
 
@@ -239,8 +241,8 @@ __device__ __forceinline__ void gt_backward4(const GtArgs &a, size_t t, int n, u
 
 // One tile of BM x BN (twice BN for the two projections, of which a lane holds g and u of the same
 // elements). WM x WN waves share it, WK of them each a part of every BK columns of k. STAGES tiles
-// of k are in LDS, STAGES - 1 of them in flight. One barrier a tile.
-template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
+// of k are in LDS, STAGES - 1 of them in flight. One barrier a tile. NT: the weights past the caches.
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT>
 __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtArgs a)
 {
     constexpr int kThreads = WM * WN * WK * cdk::kWave;
@@ -297,9 +299,9 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
     const auto issue = [&](int stage) {  // the next tile of k (zeros behind the last)
         const uint32_t at = base + stage * kStage;
         tm.load(pm, left, at);
-        tn.load(pn, left, at + TM::kBytes);
+        tn.template load<NT>(pn, left, at + TM::kBytes);
         if constexpr (kTwo)
-            tn.load(pn2, left, at + TM::kBytes + TN::kBytes);
+            tn.template load<NT>(pn2, left, at + TM::kBytes + TN::kBytes);
         pm += KIND == kGtDw ? (size_t)BK * ldm : BK;
         pn += kTwo ? BK : (size_t)BK * ldn;
         pn2 += BK;
@@ -662,8 +664,13 @@ void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
     a.nt = ad_ceil(N, BN);
     splits = KIND == kGtDx ? gt_split(a, BK, splits) : 1;
     const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
-    k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES>
-        <<<dim3(ad_ceil(tiles, 8) * 8, splits), WM * WN * WK * cdk::kWave, 0, s>>>(a);
+    const dim3 grid(ad_ceil(tiles, 8) * 8, splits), block(WM * WN * WK * cdk::kWave);
+    // Weights that are read once and would sweep most of the last-level cache go past it.
+    constexpr bool weights = KIND != kGtDw && BM <= 64;
+    if (weights && a.mt == 1 && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
+        k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, weights><<<grid, block, 0, s>>>(a);
+    else
+        k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, false><<<grid, block, 0, s>>>(a);
     gt_sum(a, splits, s);
 }
 
