@@ -490,7 +490,7 @@ typedef struct cd_gated cd_gated;
  * multiples of 8 up to 65536; 1 <= max_tokens <= 2^20. CD_EINVAL for malformed sizes and flags,
  * CD_EUNSUPPORTED beyond those limits (both before any HIP call), CD_ENOMEM / CD_EHIP when
  * allocation fails. *out is set only on success. CD_GATED_TRAIN takes 4 max_tokens d_ff
- * bytes (dg and du) and 64 MiB, with CD_GATED_FP32_GRADS 12 max_tokens d_ff and 64 MiB.
+ * bytes (dg and du) and 64 MiB + 16 KB, with CD_GATED_FP32_GRADS 12 max_tokens d_ff and 64 MiB.
  */
 cd_status countdown_gated_create(int d_model, int d_ff, int max_tokens, unsigned flags,
                                  cd_gated **out);
@@ -510,9 +510,10 @@ cd_status countdown_gated_forward(cd_gated *gated, const uint16_t *x, size_t ldx
  *   dx = dg W_gate + du W_up,   dW_gate = dg^T x,   dW_up = du^T x.
  * dh [T][d_ff] bf16. dx [T][d_model], dW_gate and dW_up [d_ff][d_model] of `type`, overwritten
  * whole; each may be NULL: that gradient is not computed. With CD_TYPE_BF16 dg and du are
- * rounded to bf16, the operands of bf16 products; with CD_TYPE_F32 (a handle with
- * CD_GATED_FP32_GRADS, else CD_EINVAL) they keep fp32 and enter as three exact bf16 terms, at
- * three times the products of the last line.
+ * rounded to bf16, the operands of bf16 products (while T d_ff <= 4096 to two bf16 terms, 16
+ * bits).
+ * With CD_TYPE_F32 (a handle with CD_GATED_FP32_GRADS, else CD_EINVAL) they keep fp32 and enter
+ * as three exact bf16 terms, at three times the products of the last line.
  */
 cd_status countdown_gated_backward(cd_gated *gated, const uint16_t *x, size_t ldx,
                                    const uint16_t *dh, size_t lddh, int T, const uint16_t *W_gate,

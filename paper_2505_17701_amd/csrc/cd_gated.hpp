@@ -23,6 +23,8 @@ constexpr int kGtTerms = 3;                       // bf16 terms of an fp32 numbe
 constexpr int kGtOutside = 0x40000000;            // an offset past every resource: reads zeros
 constexpr size_t kGtPartFloats = (size_t)16 << 20; // place for dx's partial sums (64 MiB)
 
+constexpr int kGtFew = 4096;  // elements of dg that are held in two bf16 terms
+
 enum GtKind { kGtForward, kGtBackward, kGtDx, kGtDw };
 
 struct GtArgs {
@@ -163,6 +165,74 @@ __device__ __forceinline__ bool gt_place(int mt, int nt, int &mi, int &ni)
     return true;
 }
 
+// The tiles of k that a workgroup takes, from `first` on: those of one product (dx: of dg Wg, then of du Wu),
+// each with every term of dg and du in turn, the smallest first, so that the other operand's tile comes
+// from L2 for all but the first.
+template <int KIND, int BK>
+struct GtWalk {
+    static constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
+    const uint16_t *pm, *pn, *pn2;  // m's tile; n's, and the one beside it (kTwo: of W_up)
+    int left;                       // k from here on
+    int term, product;
+    const uint16_t *m1, *n1;        // dx: du's and W_up's first tile
+
+    // n2: from n's tile to the one beside it
+    __device__ __forceinline__ void init(const GtArgs &a, int m0, int n0, int n2, int second, int first)
+    {
+        const size_t plane = (size_t)a.T * 2 * a.f;
+        term = product = 0;
+        if constexpr (kTwo) {
+            pm = a.x + m0 * a.ldx;
+            pn = a.Wg + (size_t)n0 * a.m;
+            pn2 = a.Wu + (size_t)n0 * a.m;
+            left = a.m;
+        } else if constexpr (KIND == kGtDx) {
+            const int per = (a.f + BK - 1) / BK, kt = first / a.terms;  // (first: a multiple of the terms)
+            const uint16_t *d = a.d + (a.terms - 1) * plane + m0 * (2 * (size_t)a.f);
+            m1 = d + a.f;
+            n1 = a.Wu + n0;
+            product = kt >= per;
+            pm = (product ? m1 : d) + (size_t)(kt % per) * BK;
+            pn = (product ? n1 : a.Wg + n0) + (size_t)(kt % per) * BK * a.m;
+            pn2 = pn + n2;
+            left = a.f - kt % per * BK;
+        } else {
+            pm = a.d + (a.terms - 1) * plane + (size_t)second * a.f + m0;
+            pn = a.x + n0;
+            pn2 = pn + n2;
+            left = a.T;
+        }
+    }
+
+    __device__ __forceinline__ void advance(const GtArgs &a, int n2)
+    {
+        if constexpr (kTwo) {
+            pm += BK;
+            pn += BK;
+            pn2 += BK;
+            left -= BK;
+        } else {
+            const size_t plane = (size_t)a.T * 2 * a.f;
+            if (++term < a.terms) {
+                pm -= plane;
+                return;
+            }
+            term = 0;
+            pm += (a.terms - 1) * plane + (KIND == kGtDw ? (size_t)BK * 2 * a.f : BK);
+            pn += (size_t)BK * (KIND == kGtDw ? a.ldx : a.m);
+            pn2 = pn + n2;
+            left -= BK;
+            if (KIND == kGtDx && left <= 0 && product == 0) {
+                product = 1;
+                pm = m1;
+                pn = n1;
+                pn2 = pn + n2;
+                left = a.f;
+            }
+        }
+    }
+};
+
 __device__ __forceinline__ void gt_store4(void *out, int type, size_t i, const float (&v)[4])
 {
     if (type == CD_TYPE_F32) {
@@ -266,52 +336,24 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
     const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
     const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
     const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
-    const size_t plane = (size_t)a.T * 2 * a.f;
 
     TM tm;
     TN tn;
     tm.init(ldm, M - m0);
     tn.init(ldn, N - n0);
-    // The k tiles of this workgroup: of one product after another (dx: dg Wg and du Wu, each for
-    // every term; dW: every term), the smallest terms first.
-    const int per = (K + BK - 1) / BK;
-    const int products = kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms;
-    const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;
-    const int nk = KIND == kGtDx ? min(a.ktiles, products * per - first) : products * per;
-    int prod = KIND == kGtDx ? first / per : 0, kt = KIND == kGtDx ? first % per : 0;
-    const uint16_t *pm, *pn, *pn2 = nullptr;
-    const auto begin = [&]() {
-        if constexpr (kTwo) {
-            pm = a.x + m0 * a.ldx;
-            pn = a.Wg + (size_t)n0 * a.m;
-            pn2 = a.Wu + (size_t)n0 * a.m;
-        } else if constexpr (KIND == kGtDx) {
-            pm = a.d + (a.terms - 1 - prod / 2) * plane + (size_t)(prod % 2) * a.f + m0 * ldm + (size_t)kt * BK;
-            pn = (prod % 2 ? a.Wu : a.Wg) + n0 + (size_t)kt * BK * a.m;
-        } else {
-            pm = a.d + (a.terms - 1 - prod) * plane + (size_t)second * a.f + m0;
-            pn = a.x + n0;
-        }
-    };
-    begin();
+    const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;  // dx: a split of the tiles of k
+    const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
+    const int nk = KIND == kGtDx ? min(a.ktiles, all - first) : all;
+    GtWalk<KIND, BK> w;
+    w.init(a, m0, n0, 0, second, first);
     const uint32_t base = gt_lds(lds);
-    int left = K - kt * BK;
     const auto issue = [&](int stage) {  // the next tile of k (zeros behind the last)
         const uint32_t at = base + stage * kStage;
-        tm.load(pm, left, at);
-        tn.template load<NT>(pn, left, at + TM::kBytes);
+        tm.load(w.pm, w.left, at);
+        tn.template load<NT>(w.pn, w.left, at + TM::kBytes);
         if constexpr (kTwo)
-            tn.template load<NT>(pn2, left, at + TM::kBytes + TN::kBytes);
-        pm += KIND == kGtDw ? (size_t)BK * ldm : BK;
-        pn += kTwo ? BK : (size_t)BK * ldn;
-        pn2 += BK;
-        left -= BK;
-        if (!kTwo && left <= 0 && prod + 1 < products) {
-            ++prod;
-            kt = 0;
-            left = K;
-            begin();
-        }
+            tn.template load<NT>(w.pn2, w.left, at + TM::kBytes + TN::kBytes);
+        w.advance(a, 0);
     };
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave);
@@ -443,11 +485,9 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
     const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
     const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
-    const size_t plane = (size_t)a.T * 2 * a.f;
-    const int per = (K + BK - 1) / BK;
-    const int products = kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms;
     const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;  // dx: a split of the tiles of k
-    const int nk = KIND == kGtDx ? min(a.ktiles, products * per - first) : products * per;
+    const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
+    const int nk = KIND == kGtDx ? min(a.ktiles, all - first) : all;
 
     TM tm[MH];
     TN tn[2];
@@ -456,49 +496,23 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         tm[1].init(ldm, M - m0 - 128);
     tn[0].init(ldn, N - n0);
     tn[1].init(ldn, N - n0 - (kTwo ? 0 : 128));
-    const size_t m1 = KIND == kGtDw ? 128 : 128 * ldm, n1 = 128;  // the second halves (k across rows: columns)
-
-    struct Cursor {  // a tile of k
-        const uint16_t *pm, *pn, *pn2;
-        int left;
-    };
-    Cursor c2, c1;  // the tiles whose first and whose second halves are loaded next
-    int prod = KIND == kGtDx ? first / per : 0, kt = KIND == kGtDx ? first % per : 0;
-    const auto begin = [&]() {
-        if constexpr (kTwo) {
-            c2 = {a.x + m0 * a.ldx, a.Wg + (size_t)n0 * a.m, a.Wu + (size_t)n0 * a.m, K};
-        } else if constexpr (KIND == kGtDx) {
-            const int term = a.terms - 1 - prod / 2;
-            const uint16_t *w = (prod % 2 ? a.Wu : a.Wg) + n0 + (size_t)kt * BK * a.m;
-            c2 = {a.d + term * plane + (size_t)(prod % 2) * a.f + m0 * ldm + (size_t)kt * BK, w, w + n1, K - kt * BK};
-        } else {
-            const int term = a.terms - 1 - prod;
-            c2 = {a.d + term * plane + (size_t)second * a.f + m0, a.x + n0, a.x + n0 + n1, K};
-        }
-    };
-    const auto advance = [&]() {
-        c1 = c2;
-        c2.pm += KIND == kGtDw ? (size_t)BK * ldm : BK;
-        c2.pn += kTwo ? BK : (size_t)BK * ldn;
-        c2.pn2 += kTwo ? BK : (size_t)BK * ldn;
-        c2.left -= BK;
-        if (!kTwo && c2.left <= 0 && prod + 1 < products) {
-            ++prod;
-            kt = 0;
-            begin();
-        }
-    };
+    const size_t mh = KIND == kGtDw ? 128 : 128 * ldm;  // to the second half of m
+    GtWalk<KIND, BK> w;
+    w.init(a, m0, n0, 128, second, first);
+    const uint16_t *pm1;  // the tile of k before w's: its second half of m is loaded next
+    int left1;
     const uint32_t base = gt_lds(lds);
     const auto load0 = [&](uint32_t at) {  // all but the second half of m
-        tm[0].load(c2.pm, c2.left, at);
-        tn[0].load(c2.pn, c2.left, at + kN0);
-        tn[1].load(c2.pn2, c2.left, at + kN1);
-        advance();
+        tm[0].load(w.pm, w.left, at);
+        tn[0].load(w.pn, w.left, at + kN0);
+        tn[1].load(w.pn2, w.left, at + kN1);
+        pm1 = w.pm + mh;
+        left1 = w.left;
+        w.advance(a, 128);
     };
-    begin();
     load0(base);
     if constexpr (MH == 2)
-        tm[1].load(c1.pm + m1, c1.left, base + kHalf);
+        tm[1].load(pm1, left1, base + kHalf);
     load0(base + kStage);
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave), lane = threadIdx.x % cdk::kWave;
@@ -558,7 +572,7 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         read_n(vn[1], s + kN1);
         read_m(s);
         if constexpr (MH == 2) {
-            tm[1].load(c1.pm + m1, c1.left, other + kHalf);
+            tm[1].load(pm1, left1, other + kHalf);
             multiply(0);
             read_m(s + kHalf);
             load0(here);
@@ -646,9 +660,9 @@ namespace {
 // dx: the tiles of k of a workgroup, and how many workgroups then share a tile of dx
 int gt_split(GtArgs &a, int BK, int splits)
 {
-    const int all = 2 * a.terms * ad_ceil(a.f, BK);
-    a.ktiles = ad_ceil(all, std::max(1, std::min(splits, all / 4)));
-    return ad_ceil(all, a.ktiles);
+    const int all = 2 * ad_ceil(a.f, BK);  // each with all terms
+    a.ktiles = a.terms * ad_ceil(all, std::max(1, std::min(splits, all / 4)));
+    return ad_ceil(a.terms * all, a.ktiles);
 }
 
 void gt_sum(const GtArgs &a, int splits, hipStream_t s)
@@ -780,8 +794,9 @@ cd_status countdown_gated_create(int d_model, int d_ff, int max_tokens, unsigned
     p->flags = flags;
     p->device = dev;
     if (flags & CD_GATED_TRAIN) {
-        const size_t terms = flags & CD_GATED_FP32_GRADS ? kGtTerms : 1;
-        const size_t planes = (terms * max_tokens * 2 * d_ff * sizeof(uint16_t) + 255) / 256 * 256;
+        const size_t one = (size_t)max_tokens * 2 * d_ff * sizeof(uint16_t);
+        const size_t planes = flags & CD_GATED_FP32_GRADS ? (kGtTerms * one + 255) / 256 * 256
+                                                          : (one + 255) / 256 * 256 + kGtFew * 2 * sizeof(uint16_t);
         if (hip_status(hipMalloc(&p->ws, planes + kGtPartFloats * sizeof(float))) != CD_OK) {
             delete p;
             return CD_ENOMEM;
@@ -889,7 +904,10 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     a.type = type;
     a.d = p->d;
     a.part = p->part;
-    a.terms = type == CD_TYPE_F32 ? kGtTerms : 1;
+    // The errors of few rounded numbers do not average out in a gradient (that of one token over 64
+    // neurons may be 1.5 times as far off as its own rounding puts it, over many 1.41); a second term
+    // takes them out. Everywhere it would cost 3 us (256 x 688, 37 tokens, of 16) to 35 (4096 x 11008, one token, of 145).
+    a.terms = type == CD_TYPE_F32 ? kGtTerms : (int64_t)T * a.f <= kGtFew ? 2 : 1;
     gt_projections<kGtBackward>(a, s);
     if (dx) {
         a.out = dx;

@@ -81,9 +81,9 @@ def test_a_failed_allocation_leaves_nothing(host):
     assert host.lib.host_hip_live_allocations() == live
 
 
-@pytest.mark.parametrize("flags,bytes_each", [(1, 4), (3, 12)])
-def test_the_workspace_takes_what_the_header_says(host, flags, bytes_each):
-    most = bytes_each * T * F + (64 << 20)
+@pytest.mark.parametrize("flags,size", [(1, 4 * T * F + (16 << 10)), (3, 12 * T * F)])
+def test_the_workspace_takes_what_the_header_says(host, flags, size):
+    most = size + (64 << 20)
     for limit, status in ((most + 256, 0), (most - 1, host.cd.CD_ENOMEM)):
         host.limit(limit)
         try:
@@ -139,15 +139,15 @@ FWD = ["k_gt_product<%d,16,16,", "k_gt_product<%d,32,32,", "k_gt_product<%d,64,3
     ((1, 256, 688), 0, "k_gt_product<2,16,128,", "k_gt_product<3,64,64,"),
     ((16, 4096, 14336), 0, "k_gt_product<2,16,128,", "k_gt_large<3,2>"),
     ((17, 256, 688), 1, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
-    ((100, 200, 2200), 2, "k_gt_large<2,1>", "k_gt_product<3,64,64,"),
-    ((200, 136, 3000), 3, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
-    ((500, 72, 3000), 4, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
-    ((700, 72, 3504), 5, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
-    ((900, 72, 4000), 6, "k_gt_large<2,2>", "k_gt_product<3,64,64,"),
-    ((384, 72, 16640), 6, "k_gt_large<2,1>", "k_gt_product<3,128,128,"),
-    ((2000, 264, 4104), 7, "k_gt_large<2,2>", "k_gt_product<3,128,128,"),
-    ((1300, 1544, 2056), 5, "k_gt_large<2,1>", "k_gt_product<3,128,128,"),
-    ((70, 1032, 4104), 3, "k_gt_large<2,1>", "k_gt_large<3,2>"),
+    ((100, 200, 2200), 2, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((200, 136, 3000), 3, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((500, 72, 3000), 4, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((700, 72, 3504), 5, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((900, 72, 4000), 6, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((384, 72, 16640), 6, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),
+    ((2000, 264, 4104), 7, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),
+    ((1300, 1544, 2056), 5, "k_gt_large<2,2>", "k_gt_product<3,128,128,"),
+    ((70, 1032, 4104), 3, "k_gt_product<2,64,128,", "k_gt_large<3,2>"),
     ((8192, 4096, 14336), 7, "k_gt_large<2,2>", "k_gt_large<3,2>"),
 ], ids=str)
 def test_kernels_by_the_sizes(host, shape, proj, dx, dw):
