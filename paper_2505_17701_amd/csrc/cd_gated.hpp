@@ -233,15 +233,60 @@ struct GtWalk {
     }
 };
 
-__device__ __forceinline__ void gt_store4(void *out, int type, size_t i, const float (&v)[4])
+__device__ __forceinline__ uint64_t gt_pack4(const f32x4_t &v)
 {
-    if (type == CD_TYPE_F32) {
-        f32x4_t w = {v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + i) = w;
-    } else {
-        const uint64_t w = ad_pack(v[0], v[1]) | (uint64_t)ad_pack(v[2], v[3]) << 32;
-        *reinterpret_cast<uint64_t *>(static_cast<uint16_t *>(out) + i) = w;
+    return ad_pack(v[0], v[1]) | (uint64_t)ad_pack(v[2], v[3]) << 32;
+}
+
+__device__ __forceinline__ void gt_store4(void *out, int type, size_t i, const f32x4_t &v)
+{
+    if (type == CD_TYPE_F32)
+        *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + i) = v;
+    else
+        *reinterpret_cast<uint64_t *>(static_cast<uint16_t *>(out) + i) = gt_pack4(v);
+}
+
+// Four bf16 a lane of NF neighbouring 16 x 16 tiles (lane: row lane % 16, columns 4 (lane / 16)..), `row` at
+// the first column; `left` columns of it exist, none where not ok. Two tiles at a time change hands between
+// rows of 16 lanes, so that a lane stores 16 bytes and a row 64 at once: 32-byte pieces cost L2 a request each
+// (8192 tokens of 4096 x 14336, backward: STORECOST).
+template <int NF>
+__device__ __forceinline__ void gt_store_tiles(uint16_t *row, bool ok, int left, const uint64_t (&v)[NF])
+{
+    const int j = threadIdx.x % cdk::kWave / 16;
+#pragma unroll
+    for (int i = 0; i < NF; i += 2) {
+        if constexpr (NF == 1) {
+            if (ok && 4 * j < left)
+                *reinterpret_cast<uint64_t *>(row + 4 * j) = v[0];
+        } else {
+            const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)v[i], (uint32_t)v[i + 1], false, false);
+            const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(v[i] >> 32), (uint32_t)(v[i + 1] >> 32), false,
+                                                             false);
+            const int c = 16 * i + j % 2 * 16 + j / 2 * 8;
+            if (ok && c < left)
+                *reinterpret_cast<u32x4 *>(row + c) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+        }
     }
+}
+
+// the same of fp32 sums, to out of `type` from element `at` on
+template <int NF>
+__device__ __forceinline__ void gt_store_sums(void *out, int type, size_t at, bool ok, int left, const f32x4_t (&v)[NF])
+{
+    const int j = threadIdx.x % cdk::kWave / 16;
+    if (type == CD_TYPE_F32) {
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+            if (ok && 16 * i + 4 * j < left)
+                *reinterpret_cast<f32x4_t *>(static_cast<float *>(out) + at + 16 * i + 4 * j) = v[i];
+        return;
+    }
+    uint64_t w[NF];
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+        w[i] = gt_pack4(v[i]);
+    gt_store_tiles(static_cast<uint16_t *>(out) + at, ok, left, w);
 }
 
 // 1 / (1 + exp(-g)) to a few units in the last place, on the hardware's exp2 and reciprocal: with the
@@ -255,14 +300,18 @@ __device__ __forceinline__ float gt_sigmoid(float g)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(err, ln2, 1.0f));
 }
 
-// h of four neurons
-__device__ __forceinline__ void gt_forward4(const GtArgs &a, size_t t, int n, const f32x4_t &g, const f32x4_t &u)
+// What KIND makes of a row's NF tiles (t, n: this lane's row and the first column; ok: the row exists).
+template <int NF>
+__device__ __forceinline__ void gt_forward(const GtArgs &a, size_t t, int n, bool ok, const f32x4_t (&g)[NF],
+                                           const f32x4_t (&u)[NF])
 {
-    float v[4];
+    f32x4_t h[NF];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        v[r] = g[r] * gt_sigmoid(g[r]) * u[r];
-    gt_store4(a.out, a.type, t * a.ldo + n, v);
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            h[i][r] = g[i][r] * gt_sigmoid(g[i][r]) * u[i][r];
+    gt_store_sums(a.out, a.type, t * a.ldo + n, ok, a.f - n, h);
 }
 
 __device__ __forceinline__ uint64_t gt_dh(const GtArgs &a, int t, int n)
@@ -270,42 +319,48 @@ __device__ __forceinline__ uint64_t gt_dh(const GtArgs &a, int t, int n)
     return *reinterpret_cast<const uint64_t *>(or_zero(t < a.T && n < a.f, a.dh + (size_t)t * a.lddh + n));
 }
 
-// dg and du of four neurons, in a.terms bf16 terms: one is rounded to nearest even, the operand that
-// a bf16 product takes; two hold 16 bits, three all of an fp32 number. w: dh of the four.
-__device__ __forceinline__ void gt_backward4(const GtArgs &a, size_t t, int n, uint64_t w, const f32x4_t &g,
-                                             const f32x4_t &u)
+// dg and du, in a.terms bf16 terms: one is rounded to nearest even, the operand that a bf16 product takes;
+// two hold 16 bits, three all of an fp32 number. w: dh.
+template <int NF>
+__device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bool ok, const uint64_t (&w)[NF],
+                                            const f32x4_t (&g)[NF], const f32x4_t (&u)[NF])
 {
-    float d[2][4];
+    f32x4_t d[2][NF];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const uint32_t p = (uint32_t)(w >> (r / 2 * 32));
-        const float dh = r % 2 ? cdk::bf16_hi(p) : cdk::bf16_lo(p);
-        const float s = gt_sigmoid(g[r]);
-        d[0][r] = dh * u[r] * (s * (1.0f + g[r] * (1.0f - s)));
-        d[1][r] = dh * (g[r] * s);
-    }
+    for (int i = 0; i < NF; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t p = (uint32_t)(w[i] >> (r / 2 * 32));
+            const float dh = r % 2 ? cdk::bf16_hi(p) : cdk::bf16_lo(p);
+            const float s = gt_sigmoid(g[i][r]);
+            d[0][i][r] = dh * u[i][r] * (s * (1.0f + g[i][r] * (1.0f - s)));
+            d[1][i][r] = dh * (g[i][r] * s);
+        }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         uint16_t *o = a.d + t * (2 * (size_t)a.f) + (size_t)q * a.f + n;
         if (a.terms == 1) {
-            gt_store4(o, CD_TYPE_BF16, 0, d[q]);
+            gt_store_sums(o, CD_TYPE_BF16, 0, ok, a.f - n, d[q]);
             continue;
         }
-        uint64_t out[kGtTerms] = {0, 0, 0};
+        uint64_t out[kGtTerms][NF];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            uint32_t w3[3];
-            ad_split(d[q][r], w3);
-            if (a.terms == 2)  // the second rounded
-                w3[1] = ad_pack(__uint_as_float(w3[1]) + __uint_as_float(w3[2]), 0.0f) << 16;
+        for (int i = 0; i < NF; ++i) {
+            uint32_t w3[4][3];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                ad_split(d[q][i][r], w3[r]);
+                if (a.terms == 2)  // the second rounded
+                    w3[r][1] = ad_pack(__uint_as_float(w3[r][1]) + __uint_as_float(w3[r][2]), 0.0f) << 16;
+            }
 #pragma unroll
             for (int k = 0; k < kGtTerms; ++k)
-                out[k] |= (uint64_t)(w3[k] >> 16) << (16 * r);
+                out[k][i] = (w3[0][k] >> 16 | w3[1][k]) | (uint64_t)(w3[2][k] >> 16 | w3[3][k]) << 32;
         }
 #pragma unroll
         for (int k = 0; k < kGtTerms; ++k)
             if (k < a.terms)
-                *reinterpret_cast<uint64_t *>(o + (size_t)k * a.T * 2 * a.f) = out[k];
+                gt_store_tiles(o + (size_t)k * a.T * 2 * a.f, ok, a.f - n, out[k]);
     }
 }
 
@@ -426,33 +481,32 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
                     for (int j = 0; j < FM; ++j)
                         acc[p][i][j] += sums[at(w, p, i, j)];
     }
-    uint64_t dh[FN][FM];  // all loads before the first is used
+    uint64_t dh[FM][FN];  // all loads before the first is used
     if constexpr (KIND == kGtBackward) {
 #pragma unroll
-        for (int i = 0; i < FN; ++i)
+        for (int j = 0; j < FM; ++j)
 #pragma unroll
-            for (int j = 0; j < FM; ++j)
-                dh[i][j] = gt_dh(a, m0 + (wm * FM + j) * 16 + lane % 16, n0 + (wn * FN + i) * 16 + lane / 16 * 4);
+            for (int i = 0; i < FN; ++i)
+                dh[j][i] = gt_dh(a, m0 + (wm * FM + j) * 16 + lane % 16, n0 + (wn * FN + i) * 16 + lane / 16 * 4);
     }
 #pragma unroll
-    for (int i = 0; i < FN; ++i)
+    for (int j = 0; j < FM; ++j) {
+        const int m = m0 + (wm * FM + j) * 16 + lane % 16, n = n0 + wn * FN * 16;
+        f32x4_t v[NP][FN];
 #pragma unroll
-        for (int j = 0; j < FM; ++j) {
-            const int m = m0 + (wm * FM + j) * 16 + lane % 16, n = n0 + (wn * FN + i) * 16 + lane / 16 * 4;
-            if (m >= M || n >= N)
-                continue;
-            if constexpr (KIND == kGtForward) {
-                gt_forward4(a, m, n, acc[0][i][j], acc[1][i][j]);
-            } else if constexpr (KIND == kGtBackward) {
-                gt_backward4(a, m, n, dh[i][j], acc[0][i][j], acc[1][i][j]);
-            } else {
-                const float v[4] = {acc[0][i][j][0], acc[0][i][j][1], acc[0][i][j][2], acc[0][i][j][3]};
-                if (KIND == kGtDx && gridDim.y > 1)
-                    gt_store4(a.part + blockIdx.y * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, v);
-                else
-                    gt_store4(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, v);
-            }
-        }
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+                v[p][i] = acc[p][i][j];
+        if constexpr (KIND == kGtForward)
+            gt_forward(a, m, n, m < M, v[0], v[1]);
+        else if constexpr (KIND == kGtBackward)
+            gt_backward(a, m, n, m < M, dh[j], v[0], v[1]);
+        else if (KIND == kGtDx && gridDim.y > 1)
+            gt_store_sums(a.part + blockIdx.y * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, m < M, N - n, v[0]);
+        else
+            gt_store_sums(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, m < M, N - n, v[0]);
+    }
 }
 
 // Many tiles: 256 x 256 (256 x 128 of both projections), eight waves, each 64 rows of either half of
@@ -587,42 +641,46 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         asm volatile("s_barrier" ::: "memory");
     gt_wait<0>();  // no load outlives the workgroup's LDS
 
-    uint64_t dh[MH][FN][FM];  // all loads before the first is used
+    uint64_t dh[MH][FM][FN];  // all loads before the first is used
     if constexpr (KIND == kGtBackward) {
 #pragma unroll
         for (int hm = 0; hm < MH; ++hm)
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
+            for (int j = 0; j < FM; ++j)
 #pragma unroll
-                for (int j = 0; j < FM; ++j)
-                    dh[hm][i][j] = gt_dh(a, m0 + hm * 128 + (wm * FM + j) * 16 + lane % 16,
+                for (int i = 0; i < FN; ++i)
+                    dh[hm][j][i] = gt_dh(a, m0 + hm * 128 + (wm * FM + j) * 16 + lane % 16,
                                          n0 + (wn * FN + i) * 16 + lane / 16 * 4);
     }
 #pragma unroll
     for (int hm = 0; hm < MH; ++hm)
 #pragma unroll
-        for (int hn = 0; hn < (kTwo ? 1 : 2); ++hn)
+        for (int j = 0; j < FM; ++j) {
+            const int m = m0 + hm * 128 + (wm * FM + j) * 16 + lane % 16, n = n0 + wn * FN * 16;
+            f32x4_t v[2][FN];
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
+            for (int p = 0; p < 2; ++p)
 #pragma unroll
-                for (int j = 0; j < FM; ++j) {
-                    const int m = m0 + hm * 128 + (wm * FM + j) * 16 + lane % 16;
-                    const int n = n0 + hn * 128 + (wn * FN + i) * 16 + lane / 16 * 4;
-                    if (m >= M || n >= N)
-                        continue;
-                    if constexpr (KIND == kGtForward) {
-                        gt_forward4(a, m, n, acc[0][hm][i][j], acc[1][hm][i][j]);
-                    } else if constexpr (KIND == kGtBackward) {
-                        gt_backward4(a, m, n, dh[hm][i][j], acc[0][hm][i][j], acc[1][hm][i][j]);
-                    } else {
-                        const f32x4_t &c = acc[hn][hm][i][j];
-                        const float v[4] = {c[0], c[1], c[2], c[3]};
-                        if (KIND == kGtDx && gridDim.y > 1)
-                            gt_store4(a.part + blockIdx.y * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, v);
-                        else
-                            gt_store4(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, v);
-                    }
+                for (int i = 0; i < FN; ++i)
+                    v[p][i] = acc[p][hm][i][j];
+            if constexpr (KIND == kGtForward) {
+                gt_forward(a, m, n, m < M, v[0], v[1]);
+            } else if constexpr (KIND == kGtBackward) {
+                gt_backward(a, m, n, m < M, dh[hm][j], v[0], v[1]);
+            } else {
+                void *out = KIND == kGtDw && second ? a.out2 : a.out;
+                int type = a.type;
+                size_t at = (size_t)m * a.ldo + n;
+                if (KIND == kGtDx && gridDim.y > 1) {
+                    out = a.part + blockIdx.y * (size_t)a.T * a.m;
+                    type = CD_TYPE_F32;
+                    at = (size_t)m * a.m + n;
                 }
+#pragma unroll
+                for (int p = 0; p < 2; ++p)
+                    gt_store_sums(out, type, at + p * 128, m < M, N - n - p * 128, v[p]);
+            }
+        }
 }
 
 // dx from its parts, in their order; four columns a thread
@@ -635,8 +693,7 @@ __global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a, int splits)
 #pragma unroll 8
     for (int k = 1; k < splits; ++k)
         s += *reinterpret_cast<const f32x4_t *>(a.part + k * n + i);
-    const float v[4] = {s[0], s[1], s[2], s[3]};
-    gt_store4(a.out, a.type, i / a.m * a.ldo + i % a.m, v);
+    gt_store4(a.out, a.type, i / a.m * a.ldo + i % a.m, s);
 }
 
 __global__ __launch_bounds__(256) void k_gt_zero(uint32_t *p, size_t words)

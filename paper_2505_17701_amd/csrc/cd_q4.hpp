@@ -62,7 +62,7 @@ __device__ __forceinline__ u32x4 q4_operand(uint32_t w, uint32_t mask, uint32_t 
 // out of four rows
 __device__ __forceinline__ void q4_store(const Q4Args &a, int t, int row, const f32x4_t &y)
 {
-    float o[4] = {y[0], y[1], y[2], y[3]};
+    f32x4_t o = y;
     const size_t at = t * a.ldb + row;
     if (a.base && a.type == CD_TYPE_F32) {
         const f32x4_t b = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(a.base) + at);
