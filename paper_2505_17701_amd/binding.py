@@ -556,12 +556,12 @@ def _rows(t, n, width, name, device):
         raise ValueError(f"{name} must have shape {(n, width)}, got {tuple(t.shape)}")
     if t.get_device() != device:
         raise ValueError(f"{name} must live on GPU {device}, where the pool was created")
+    if t.is_contiguous():
+        return t.data_ptr(), width
     row, col = t.stride()
-    if n <= 1 or t.is_contiguous():  # (the stride of a single row says nothing)
-        row = width
     if col != 1 and width > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    return t.data_ptr(), row
+    return t.data_ptr(), width if n <= 1 else row  # (the stride of a single row says nothing)
 
 
 def _whole(t, shape, dtype, name, device):

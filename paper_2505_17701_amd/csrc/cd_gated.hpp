@@ -42,7 +42,7 @@ struct GtArgs {
     int terms;
     float *part;     // dx split over k: [splits][T][m]
     int mt, nt;      // tiles
-    int ktiles;      // of a workgroup (a split)
+    int splits, ktiles;  // dx: workgroups that share a tile, and their tiles of k
 };
 
 // a buffer resource over 2^30 bytes at p (uniform): what lies past them reads as zero
@@ -151,12 +151,12 @@ struct GtTile {
 
 // The workgroup's tile. Neighbours in time on one XCD (blockIdx.x % 8) take `group` tiles of m by a
 // stretch of n, so that its L2 holds what they share. False: no tile.
-__device__ __forceinline__ bool gt_place(int mt, int nt, int &mi, int &ni)
+__device__ __forceinline__ bool gt_place(int block, int mt, int nt, int &mi, int &ni)
 {
     constexpr int group = 4;
     const int total = mt * nt, per = (total + 7) / 8;
-    const int t = (int)blockIdx.x % 8 * per + (int)blockIdx.x / 8;
-    if ((int)blockIdx.x / 8 >= per || t >= total)
+    const int t = block % 8 * per + block / 8;
+    if (block / 8 >= per || t >= total)
         return false;
     const int width = group * nt, first = t / width * group, rows = min(group, mt - first);
     // known to be uniform: what follows from them stays in scalar registers
@@ -292,9 +292,11 @@ __device__ __forceinline__ void gt_store_sums(void *out, int type, size_t at, bo
 // 1 / (1 + exp(-g)) to a few units in the last place, on the hardware's exp2 and reciprocal: with the
 // library's expf and division the last step of a 256 x 256 tile costs three times the instructions. exp2's
 // argument is rounded, for large |g| by more than exp2 itself; its rounding error goes back in as a factor.
+// Past 200 it is 0 or 1 (for NaN too: what it multiplies is not finite itself).
 __device__ __forceinline__ float gt_sigmoid(float g)
 {
     constexpr float log2e = 1.44269502f, rest = 1.92596299e-8f, ln2 = 0.693147182f;
+    g = __builtin_amdgcn_fmed3f(g, -200.0f, 200.0f);
     const float t = -g * log2e;
     const float err = fmaf(-g, rest, fmaf(-g, log2e, -t));
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(err, ln2, 1.0f));
@@ -367,8 +369,14 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
 // One tile of BM x BN (twice BN for the two projections, of which a lane holds g and u of the same
 // elements). WM x WN waves share it, WK of them each a part of every BK columns of k. STAGES tiles
 // of k are in LDS, STAGES - 1 of them in flight. One barrier a tile. NT: the weights past the caches.
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
+constexpr int kGtLds = std::max(STAGES * (BM + (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * BN) * BK * 2,
+                                (WK - 1) * WM * WN * (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * (BM / WM) *
+                                    (BN / WN) * 4);  // the waves' sums
+
+// block, split: of the grid; lds: kGtLds bytes
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT>
-__global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtArgs a)
+__device__ __forceinline__ void gt_tile(const GtArgs &a, int block, int split, char *lds)
 {
     constexpr int kThreads = WM * WN * WK * cdk::kWave;
     constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
@@ -377,11 +385,8 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
     using TN = GtTile<BN, BK, kTwo, kThreads>;
     constexpr int kStage = TM::kBytes + NP * TN::kBytes;
     constexpr int kFlight = (TM::kLoads + NP * TN::kLoads) * (STAGES - 2);
-    constexpr int kSums = WK > 1 ? (WK - 1) * WM * WN * NP * FM * FN * cdk::kWave * 16 : 0;
-    __shared__ __align__(1024) char lds[STAGES * kStage > kSums ? STAGES * kStage : kSums];
-
     int mi, ni;
-    if (!gt_place(KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
+    if (!gt_place(block, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
         return;
     // dW: the tiles of W_gate's gradient, then those of W_up's
     const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
@@ -396,7 +401,7 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
     TN tn;
     tm.init(ldm, M - m0);
     tn.init(ldn, N - n0);
-    const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;  // dx: a split of the tiles of k
+    const int first = KIND == kGtDx ? split * a.ktiles : 0;  // dx: a split of the tiles of k
     const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
     const int nk = KIND == kGtDx ? min(a.ktiles, all - first) : all;
     GtWalk<KIND, BK> w;
@@ -502,11 +507,29 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
             gt_forward(a, m, n, m < M, v[0], v[1]);
         else if constexpr (KIND == kGtBackward)
             gt_backward(a, m, n, m < M, dh[j], v[0], v[1]);
-        else if (KIND == kGtDx && gridDim.y > 1)
-            gt_store_sums(a.part + blockIdx.y * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, m < M, N - n, v[0]);
+        else if (KIND == kGtDx && a.splits > 1)
+            gt_store_sums(a.part + split * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, m < M, N - n, v[0]);
         else
             gt_store_sums(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, m < M, N - n, v[0]);
     }
+}
+
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT>
+__global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtArgs a)
+{
+    __shared__ __align__(1024) char lds[kGtLds<KIND, BM, BN, BK, WM, WN, WK, STAGES>];
+    gt_tile<KIND, BM, BN, BK, WM, WN, WK, STAGES, NT>(a, blockIdx.x, blockIdx.y, lds);
+}
+
+// Little work: dx (the first `blocks` of the grid) and the weights' gradients in one launch.
+__global__ __launch_bounds__(256) void k_gt_back(const GtArgs x, const GtArgs w, int blocks)
+{
+    constexpr int kLds = std::max(kGtLds<kGtDx, 64, 64, 128, 1, 2, 2, 3>, kGtLds<kGtDw, 64, 64, 64, 2, 2, 1, 3>);
+    __shared__ __align__(1024) char lds[kLds];
+    if ((int)blockIdx.x < blocks)
+        gt_tile<kGtDx, 64, 64, 128, 1, 2, 2, 3, false>(x, blockIdx.x, 0, lds);
+    else
+        gt_tile<kGtDw, 64, 64, 64, 2, 2, 1, 3, false>(w, (int)blockIdx.x - blocks, 0, lds);
 }
 
 // Many tiles: 256 x 256 (256 x 128 of both projections), eight waves, each 64 rows of either half of
@@ -530,7 +553,7 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     __shared__ __align__(1024) char lds[kStages * kStage];
 
     int mi, ni;
-    if (!gt_place(KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
+    if (!gt_place(blockIdx.x, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
         return;
     const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
     if (KIND == kGtDw && mi >= a.mt)
@@ -671,7 +694,7 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
                 void *out = KIND == kGtDw && second ? a.out2 : a.out;
                 int type = a.type;
                 size_t at = (size_t)m * a.ldo + n;
-                if (KIND == kGtDx && gridDim.y > 1) {
+                if (KIND == kGtDx && a.splits > 1) {
                     out = a.part + blockIdx.y * (size_t)a.T * a.m;
                     type = CD_TYPE_F32;
                     at = (size_t)m * a.m + n;
@@ -684,14 +707,14 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
 }
 
 // dx from its parts, in their order; four columns a thread
-__global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a, int splits)
+__global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a)
 {
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (size_t)a.T * a.m;
     if (i >= n)
         return;
     f32x4_t s = *reinterpret_cast<const f32x4_t *>(a.part + i);
 #pragma unroll 8
-    for (int k = 1; k < splits; ++k)
+    for (int k = 1; k < a.splits; ++k)
         s += *reinterpret_cast<const f32x4_t *>(a.part + k * n + i);
     gt_store4(a.out, a.type, i / a.m * a.ldo + i % a.m, s);
 }
@@ -714,46 +737,54 @@ struct cd_gated {
 
 namespace {
 
-// dx: the tiles of k of a workgroup, and how many workgroups then share a tile of dx
-int gt_split(GtArgs &a, int BK, int splits)
+// dx: how many workgroups share a tile of it
+void gt_split(GtArgs &a, int BK, int splits)
 {
     const int all = 2 * ad_ceil(a.f, BK);  // each with all terms
     a.ktiles = a.terms * ad_ceil(all, std::max(1, std::min(splits, all / 4)));
-    return ad_ceil(a.terms * all, a.ktiles);
+    a.splits = ad_ceil(a.terms * all, a.ktiles);
 }
 
-void gt_sum(const GtArgs &a, int splits, hipStream_t s)
+void gt_sum(const GtArgs &a, hipStream_t s)
 {
-    if (splits > 1)
-        k_gt_sum<<<(unsigned)(((size_t)a.T * a.m / 4 + 255) / 256), 256, 0, s>>>(a, splits);
+    if (a.splits > 1)
+        k_gt_sum<<<(unsigned)(((size_t)a.T * a.m / 4 + 255) / 256), 256, 0, s>>>(a);
+}
+
+// workgroups of tiles of bm x bn (of both gradients of weights, as far as they are wanted)
+template <int KIND>
+int gt_grid(GtArgs &a, int M, int N, int bm, int bn)
+{
+    a.mt = ad_ceil(M, bm);
+    a.nt = ad_ceil(N, bn);
+    return ad_ceil(a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1), 8) * 8;
 }
 
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
 void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
-    a.mt = ad_ceil(M, BM);
-    a.nt = ad_ceil(N, BN);
-    splits = KIND == kGtDx ? gt_split(a, BK, splits) : 1;
-    const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
-    const dim3 grid(ad_ceil(tiles, 8) * 8, splits), block(WM * WN * WK * cdk::kWave);
+    a.splits = 1;
+    if (KIND == kGtDx)
+        gt_split(a, BK, splits);
+    const dim3 grid(gt_grid<KIND>(a, M, N, BM, BN), a.splits), block(WM * WN * WK * cdk::kWave);
     // Weights that are read once and would sweep most of the last-level cache go past it.
     constexpr bool weights = KIND != kGtDw && BM <= 64;
     if (weights && a.mt == 1 && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
         k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, weights><<<grid, block, 0, s>>>(a);
     else
         k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, false><<<grid, block, 0, s>>>(a);
-    gt_sum(a, splits, s);
+    gt_sum(a, s);
 }
 
 template <int KIND, int MH>
 void gt_large(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
-    a.mt = ad_ceil(M, 128 * MH);
-    a.nt = ad_ceil(N, KIND == kGtForward || KIND == kGtBackward ? 128 : 256);
-    splits = KIND == kGtDx ? gt_split(a, 64, splits) : 1;
-    const int tiles = a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1);
-    k_gt_large<KIND, MH><<<dim3(ad_ceil(tiles, 8) * 8, splits), 512, 0, s>>>(a);
-    gt_sum(a, splits, s);
+    a.splits = 1;
+    if (KIND == kGtDx)
+        gt_split(a, 64, splits);
+    const int grid = gt_grid<KIND>(a, M, N, 128 * MH, KIND == kGtForward || KIND == kGtBackward ? 128 : 256);
+    k_gt_large<KIND, MH><<<dim3(grid, a.splits), 512, 0, s>>>(a);
+    gt_sum(a, s);
 }
 
 // 256 x 256 against 128 x 256: rounds of workgroups over the CUs, of which the former's take half as long again
@@ -782,6 +813,16 @@ void gt_projections(const GtArgs &a, hipStream_t s)
         gt_large<KIND, 1>(a, a.T, a.f, s);
     else
         gt_large<KIND, 2>(a, a.T, a.f, s);
+}
+
+// dx and the weights' gradients in one launch, while a tile of dx needs no more than 16 tiles of k and both
+// make one or two rounds of workgroups. Captured us a call against launches of their own:
+//    37 tokens, 256 x 688 14.6 / 16.5   300, 256 x 1024 18.1 / 20.0   4000, 128 x 512 30.6 / 43.2
+//   with 32 tiles of k: 1000, 256 x 2048 31.2 / 34.6, but one token of 256 x 688 in two terms 19.6 / 16.5
+bool gt_little(const GtArgs &a)
+{
+    return 2 * a.terms * ad_ceil(a.f, 128) <= 16 && (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 64) <= 512 &&
+           (int64_t)ad_ceil(a.f, 64) * ad_ceil(a.m, 64) * 2 <= 512;
 }
 
 void gt_dx(const GtArgs &a, hipStream_t s)
@@ -966,16 +1007,23 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     // takes them out. Everywhere it would cost 3 us (256 x 688, 37 tokens, of 16) to 35 (4096 x 11008, one token, of 145).
     a.terms = type == CD_TYPE_F32 ? kGtTerms : (int64_t)T * a.f <= kGtFew ? 2 : 1;
     gt_projections<kGtBackward>(a, s);
-    if (dx) {
-        a.out = dx;
-        a.ldo = lddx;
-        gt_dx(a, s);
-    }
-    if (dW_gate || dW_up) {
-        a.out = dW_gate;
-        a.out2 = dW_up;
-        a.ldo = a.m;
-        gt_dw(a, s);
+    GtArgs ax = a, aw = a;
+    ax.out = dx;
+    ax.ldo = lddx;
+    aw.out = dW_gate;
+    aw.out2 = dW_up;
+    aw.ldo = a.m;
+    if (gt_little(a)) {
+        ax.splits = aw.splits = 1;
+        ax.ktiles = 2 * a.terms * ad_ceil(a.f, 128);
+        const int nx = dx ? gt_grid<kGtDx>(ax, a.T, a.m, 64, 64) : 0;
+        const int nw = dW_gate || dW_up ? gt_grid<kGtDw>(aw, a.f, a.m, 64, 64) : 0;
+        k_gt_back<<<nx + nw, 256, 0, s>>>(ax, aw, nx);
+    } else {
+        if (dx)
+            gt_dx(ax, s);
+        if (dW_gate || dW_up)
+            gt_dw(aw, s);
     }
     return launched(hipGetLastError());
 }

@@ -100,6 +100,7 @@ SHAPES = [  # T, d_model, d_ff: every tile, its edges, one element of a tile, wh
     (384, 72, 16640),
     # dx in one part; the gradients of the weights in 256 x 256 tiles, of few and of many tokens
     (4100, 2104, 72), (70, 1032, 4104), (300, 2104, 2600), (1, 1032, 4104),
+    (17, 264, 1032), (4000, 128, 512), (65, 520, 1000),  # launches of their own; one for dx and the weights' gradients
 ]
 
 
@@ -234,6 +235,24 @@ def test_large_gates(cd):
     assert torch.allclose(h.double(), (g * s)[:, None].expand(8, f), rtol=1e-5, atol=1e-30)
     want = f * torch.where(s == 0, 0.0, s * (1 + g * (1 - s)))  # u = 1
     assert torch.allclose(dx[:, 0].double(), want, rtol=1e-5, atol=1e-30)
+
+
+def test_gates_next_to_the_largest_number(cd):
+    """h = g u or 0 and the slope 1 or 0 where g times a constant would overflow."""
+    x = torch.zeros((4, 64), device="cuda")
+    x[:, 0] = torch.tensor([3.3e38, -3.3e38, 1e38, -1e38])
+    x[:, 1] = 2.0 ** -100
+    W, V = torch.zeros((8, 64), device="cuda"), torch.zeros((8, 64), device="cuda")
+    W[:, 0], V[:, 1] = 1.0, 1.0
+    x, W, V = x.to(BF16), W.to(BF16), V.to(BF16)
+    dh = torch.ones((4, 8), device="cuda", dtype=BF16)
+    with cd.Gated(64, 8, 4, train=True, fp32_grads=True) as p:
+        h = cd.countdown_gated_forward(p, x, W, V, h=torch.empty((4, 8), device="cuda"))
+        dx, _, _ = cd.countdown_gated_backward(p, x, dh, W, V)
+    open_ = (x[:, 0] > 0).double()
+    want = open_ * x[:, 0].double() * 2.0 ** -100
+    assert bool(((h.double() - want[:, None]).abs() <= 2.0 ** -21 * want[:, None]).all())
+    assert bool(((dx[:, 0].double() - 8 * open_ * 2.0 ** -100).abs() <= 2.0 ** -20 * 2.0 ** -100).all())
 
 
 def test_empty_call(cd):

@@ -136,9 +136,13 @@ FWD = ["k_gt_product<%d,16,16,", "k_gt_product<%d,32,32,", "k_gt_product<%d,64,3
 
 
 @pytest.mark.parametrize("shape,proj,dx,dw", [  # T, d_model, d_ff; the kernels by what they start with
-    ((1, 256, 688), 0, "k_gt_product<2,16,128,", "k_gt_product<3,64,64,"),
+    ((1, 256, 688), 0, "k_gt_product<2,16,128,", "k_gt_product<3,64,64,"),  # dg in two terms
+    ((6, 256, 688), 0, "k_gt_back", None),
+    ((1, 1032, 4104), 0, "k_gt_product<2,16,128,", "k_gt_large<3,2>"),
     ((16, 4096, 14336), 0, "k_gt_product<2,16,128,", "k_gt_large<3,2>"),
-    ((17, 256, 688), 1, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((17, 256, 688), 1, "k_gt_back", None),
+    ((4000, 128, 512), 4, "k_gt_back", None),
+    ((17, 256, 1032), 1, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((100, 200, 2200), 2, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((200, 136, 3000), 3, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((500, 72, 3000), 4, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
@@ -161,7 +165,8 @@ def test_kernels_by_the_sizes(host, shape, proj, dx, dw):
     assert backward(host, h, lddh=f, lddx=m, type=1, **far) == 0
     got = [k for k, _ in host.launches() if k != "k_gt_sum"]
     assert host.lib.countdown_gated_destroy(h) == 0
-    assert len(got) == 3 and got[0].startswith(FWD[proj] % 1) and got[1].startswith(dx) and got[2].startswith(dw), got
+    assert [k.startswith(w) for k, w in zip(got, (FWD[proj] % 1, dx, dw) if dw else (FWD[proj] % 1, dx))] == \
+        [True] * (3 if dw else 2), got
 
 
 def test_strides_past_what_the_kernels_reach(host, gated):
