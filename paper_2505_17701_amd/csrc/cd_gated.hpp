@@ -840,12 +840,16 @@ void gt_dx(const GtArgs &a, hipStream_t s)
         gt_large<kGtDx, 2>(a, a.T, a.m, s, splits(256, 256, 256));
 }
 
+// The weights' gradients. Past 512 tiles of 64 x 64: 128 x 128, two workgroups a CU, for few tokens (which
+// leave writing to be done: 256 tokens of 4096 x 11008, backward 225 us against 229) and where their rounds
+// are shorter than those of 256 x 256, which take 200 where they take 113 (4096 tokens of 2048 x 5504 504
+// against 521; of 4096 x 11008 1811 against 1726).
 void gt_dw(const GtArgs &a, hipStream_t s)
 {
     const auto tiles = [&](int b) { return (int64_t)ad_ceil(a.f, b) * ad_ceil(a.m, b) * 2; };  // of both gradients
     if (tiles(64) <= 512)
         gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, s);
-    else if (tiles(128) <= 512)
+    else if (a.T * a.terms <= 256 || 113 * ((tiles(128) + 511) / 512) <= 200 * ((tiles(256) + 255) / 256))
         gt_product<kGtDw, 128, 128, 64, 2, 2, 1, 2>(a, a.f, a.m, s);
     else
         gt_large<kGtDw, 2>(a, a.f, a.m, s);

@@ -99,7 +99,7 @@ SHAPES = [  # T, d_model, d_ff: every tile, its edges, one element of a tile, wh
     (100, 200, 2200), (200, 136, 3000), (500, 72, 3000), (700, 72, 3504), (900, 72, 4000), (2000, 264, 4104),
     (384, 72, 16640),
     # dx in one part; the gradients of the weights in 256 x 256 tiles, of few and of many tokens
-    (4100, 2104, 72), (70, 1032, 4104), (300, 2104, 2600), (1, 1032, 4104),
+    (4100, 2104, 72), (70, 1032, 4104), (300, 2104, 2600), (257, 2056, 2056), (1, 1032, 4104),
     (17, 264, 1032), (4000, 128, 512), (65, 520, 1000),  # launches of their own; one for dx and the weights' gradients
 ]
 
