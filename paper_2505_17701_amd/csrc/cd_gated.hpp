@@ -49,7 +49,8 @@ struct GtArgs {
 __device__ __forceinline__ u32x4 gt_resource(const void *p)
 {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
     return u32x4{lo, hi, (uint32_t)kGtOutside, 0x00027000u};
 }
 
@@ -249,7 +250,7 @@ __device__ __forceinline__ void gt_store4(void *out, int type, size_t i, const f
 // Four bf16 a lane of NF neighbouring 16 x 16 tiles (lane: row lane % 16, columns 4 (lane / 16)..), `row` at
 // the first column; `left` columns of it exist, none where not ok. Two tiles at a time change hands between
 // rows of 16 lanes, so that a lane stores 16 bytes and a row 64 at once: 32-byte pieces cost L2 a request each
-// (8192 tokens of 4096 x 14336, backward: STORECOST).
+// (backward of 1024 tokens of 4096 x 14336 626 us against 651).
 template <int NF>
 __device__ __forceinline__ void gt_store_tiles(uint16_t *row, bool ok, int left, const uint64_t (&v)[NF])
 {
@@ -369,6 +370,11 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
 // One tile of BM x BN (twice BN for the two projections, of which a lane holds g and u of the same
 // elements). WM x WN waves share it, WK of them each a part of every BK columns of k. STAGES tiles
 // of k are in LDS, STAGES - 1 of them in flight. One barrier a tile. NT: the weights past the caches.
+//
+// Few tokens wait for the weights, which long tiles of k (512 bytes of a row at a time) and 64 to 100 KB in
+// flight a CU bring at 5.8 to 6.4 TB/s: 4 tokens of 4096 x 11008 31 us, of 8192 x 28672 146. Some hundreds
+// wait for their tiles: a CU takes 35 to 45 bytes a ns of them, whatever their shape and the stages (rows
+// that do not begin on 128 bytes less: 333 tokens of 3000 x 8008 56 us, of 3008 x 8008 43).
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
 constexpr int kGtLds = std::max(STAGES * (BM + (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * BN) * BK * 2,
                                 (WK - 1) * WM * WN * (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * (BM / WM) *
@@ -540,6 +546,13 @@ __global__ __launch_bounds__(256) void k_gt_back(const GtArgs x, const GtArgs w,
 // in phase p may be overwritten by loads of phase p + 1; of the loads the last eight may be in flight.
 // MH 1: one half of m alone, 128 x 256, a phase a tile of k and three tiles in LDS; the loads are
 // issued two phases before they are read, and six of them may be in flight.
+//
+// What bounds it is the matrix cores' clock under load (80 % busy in the forward call, 78 in dx) and, where an
+// operand has k across its rows, twice as many LDS reads of half the size (61 % in the weights' gradients,
+// 1352 us if they were whole reads, 1600 so). 8192 tokens of 4096 x 14336: forward 1284 us (1498 TFLOP/s),
+// projections of the backward call 1437 (470 MB are stored, 235 loaded at the end of a tile), dx 1320,
+// weights 1570. Four barriers a phase of 16 MFMAs instead: 1360. Persistent workgroups that load the next
+// tile while they store: 1334 and, backward, 4468 against 4262.
 template <int KIND, int MH>
 __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
 {
@@ -787,11 +800,23 @@ void gt_large(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
     gt_sum(a, s);
 }
 
-// 256 x 256 against 128 x 256: rounds of workgroups over the CUs, of which the former's take half as long again
+// 256 x 256 against 128 x 256: rounds of workgroups over the CUs, of which the former's take half as long
+// again (768 tokens of 4096 x 14336, 2 against 3 rounds, 171 us against 180; 512 tokens of 3000 x 8008, 1 against 1, 85
+// against 68).
 bool gt_wide(int64_t wide, int64_t narrow) { return 3 * ((wide + 255) / 256) <= 2 * ((narrow + 255) / 256); }
 
 // g and u over T tokens, and what KIND makes of them: the smallest tile that makes one round of
-// workgroups over the 256 CUs.
+// workgroups over the 256 CUs. Forward, captured us a call (tile: tokens x neurons, of both matrices):
+//                                16x16  32x32  64x32  64x64  128x64  192x64  128x128  256x128
+//   1 token,    4096 x 14336      41.7   44.9   46.0   42.6    47.5    54.9     57.8     78.6
+//   64 tokens,  1024 x 2816        8.6    6.9    7.7    9.3    11.5    13.6     16.0     22.4
+//   64 tokens,  3000 x 8008       49.5   34.1   26.6   35.4    42.0    43.7     65.8     70.5
+//   128 tokens, 3000 x 8008       87.3   54.0   42.1   35.2    50.1    53.1     72.9     78.0
+//   128 tokens, 4096 x 14336     167.1   95.5   90.3   72.7    58.7    63.1     73.7     81.9
+//   333 tokens, 3000 x 8008      181    117     97.3   78.2    77.3    55.1     65.9     79.8
+//   256 tokens, 4096 x 14336     303    165    140    117      89.2   102       74.1     86.1
+//   512 tokens, 4096 x 14336     594    297    260    192     159     150      124       95.5
+// (16 x 16 for up to 16 tokens always: what is read there counts.)
 template <int KIND>
 void gt_projections(const GtArgs &a, hipStream_t s)
 {
@@ -825,6 +850,9 @@ bool gt_little(const GtArgs &a)
            (int64_t)ad_ceil(a.f, 64) * ad_ceil(a.m, 64) * 2 <= 512;
 }
 
+// dx. 64 x 128 tiles up to 64 tokens and while there are 128 of them at most, shared by workgroups that fill
+// the CUs twice, else 256 x 256 (backward us a call, the first against the second: 256 tokens of 1024 x 2816 41
+// against 52, 1024 of them 68 against 83, 512 tokens of 4096 x 14336, 256 tiles, 448 against 386).
 void gt_dx(const GtArgs &a, hipStream_t s)
 {
     // workgroups that share a tile: one round over the CUs, and what the place for their sums holds
@@ -832,9 +860,7 @@ void gt_dx(const GtArgs &a, hipStream_t s)
     const auto splits = [&](int bm, int bn, int slots) {
         return std::max(1, (int)std::min<int64_t>(most, slots / ((int64_t)ad_ceil(a.T, bm) * ad_ceil(a.m, bn))));
     };
-    if (a.T <= 16)
-        gt_product<kGtDx, 16, 128, 128, 1, 2, 2, 2>(a, a.T, a.m, s, splits(16, 128, 512));
-    else if (a.T <= 64 || (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 128) <= 128)
+    if (a.T <= 64 || (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 128) <= 128)
         gt_product<kGtDx, 64, 128, 64, 2, 2, 1, 3>(a, a.T, a.m, s, splits(64, 128, 512));
     else
         gt_large<kGtDx, 2>(a, a.T, a.m, s, splits(256, 256, 256));
@@ -1008,7 +1034,8 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     a.part = p->part;
     // The errors of few rounded numbers do not average out in a gradient (that of one token over 64
     // neurons may be 1.5 times as far off as its own rounding puts it, over many 1.41); a second term
-    // takes them out. Everywhere it would cost 3 us (256 x 688, 37 tokens, of 16) to 35 (4096 x 11008, one token, of 145).
+    // takes them out. Everywhere it would cost 3 us (of 16: 37 tokens, 256 x 688) to 35 (of 145: one
+    // token, 4096 x 11008).
     a.terms = type == CD_TYPE_F32 ? kGtTerms : (int64_t)T * a.f <= kGtFew ? 2 : 1;
     gt_projections<kGtBackward>(a, s);
     GtArgs ax = a, aw = a;

@@ -86,6 +86,11 @@ __host__ __device__ constexpr int q4_stages(int stage)
     return n < 3 ? 3 : n < 4 ? n : 4;
 }
 
+// Bound by the stream of the codes and, with many tokens, by that of the tokens (each workgroup reads them
+// all from L2; two row tiles a part halve that): 8192 -> 28672 gated at one token, 242 MB, 46 us (5.2 TB/s; the
+// same loads without products 42, a plain stream 35); 4096 -> 11008 gated at 13 tokens, 51 MB, 19.5 (4 of
+// them the tokens' loads). Deeper rings, tokens whole in LDS and twice the waves measured the same or slower.
+//
 // A part is 16 rows of both matrices (gated), or NM x 16 rows of one; a workgroup takes part after part. A
 // step is 1024 columns, a block of each of NM row tiles for each wave; its codes, scales and tokens go to
 // LDS without passing registers, kStages - 1 steps ahead, the next part's while the last one ends.
@@ -97,7 +102,7 @@ __global__ __launch_bounds__(WAVES *cdk::kWave) void k_q4(const Q4Args a)
     constexpr int kScale = 32 * (kQ4Cols / G), kCodes = WAVES * NM * 1024, kScales = WAVES * NM * kScale;
     constexpr int kXRow = kStep * 2 + 16;  // (+ 16: 16 tokens' columns on different banks)
     constexpr int kStage = kCodes + kScales + XT * kXRow;
-    constexpr int XL = XT > 4 ? XT / 4 : 1;  // the loads of tokens that a wave makes for a step
+    constexpr int XL = XT / 4;  // the loads of tokens that a wave makes for a step
     constexpr int kStages = q4_stages(kStage);
     static_assert(XL * WAVES >= XT * (kStep / kHalf) && WAVES % NM == 0 && (kStages - 2) * (NM + 1 + XL) < 64, "loads");
     __shared__ __align__(1024) char lds[kStages * kStage];
@@ -159,8 +164,8 @@ __global__ __launch_bounds__(WAVES *cdk::kWave) void k_q4(const Q4Args a)
 #pragma unroll
         for (int i = 0; i < XL; ++i)
             if (kEven || i < xloads)
-                gt_load_lds(gt_resource(xp[i]), next * kStep + xcol[i] < a.cols ? (next * kStep + xcol[i]) * 2 : kGtOutside,
-                            at + xat[i]);
+                gt_load_lds(gt_resource(xp[i]),
+                            next * kStep + xcol[i] < a.cols ? (next * kStep + xcol[i]) * 2 : kGtOutside, at + xat[i]);
         if (++next == steps) {
             next = 0;
             ahead += gridDim.x;
@@ -181,71 +186,71 @@ __global__ __launch_bounds__(WAVES *cdk::kWave) void k_q4(const Q4Args a)
     const int xread = kCodes + kScales + min(i16, a.T - 1) * kXRow + wave * (kQ4Cols * 2) + j * 16;
     int stage = 0;
     for (int part = blockIdx.x; part < parts; part += gridDim.x) {
-    f32x4_t y[NM];
-#pragma unroll
-    for (int q = 0; q < NM; ++q)
-        y[q] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    char *done = lds;  // the last step's codes
-    for (int n = 0; n < steps; ++n) {
-        wait();
-        issue(stage == 0 ? kStages - 1 : stage - 1);
-        char *s = done = lds + stage * kStage;
-        stage = stage + 1 == kStages ? 0 : stage + 1;
-        u32x4 xv[4], code[NM];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            xv[k] = *reinterpret_cast<const u32x4 *>(s + xread + k * 64);
+        f32x4_t y[NM];
 #pragma unroll
         for (int q = 0; q < NM; ++q)
-            code[q] = *reinterpret_cast<const u32x4 *>(s + (q * WAVES + wave) * 1024 + lane * 16);
+            y[q] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        char *done = lds;  // the last step's codes
+        for (int n = 0; n < steps; ++n) {
+            wait();
+            issue(stage == 0 ? kStages - 1 : stage - 1);
+            char *s = done = lds + stage * kStage;
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+            u32x4 xv[4], code[NM];
 #pragma unroll
-        for (int g = 0; g < kQ4Cols / G; ++g) {
-            f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < 4; ++k)
+                xv[k] = *reinterpret_cast<const u32x4 *>(s + xread + k * 64);
 #pragma unroll
-            for (int k = 0; k < G / 32; ++k)
-                start = mfma16(minus24, xv[g * (G / 32) + k], start);
+            for (int q = 0; q < NM; ++q)
+                code[q] = *reinterpret_cast<const u32x4 *>(s + (q * WAVES + wave) * 1024 + lane * 16);
 #pragma unroll
-            for (int q = 0; q < NM; ++q) {
-                const uint64_t scale =
-                    *reinterpret_cast<const uint64_t *>(s + kCodes + (q * WAVES + wave) * kScale + g * 32 + j * 8);
-                f32x4_t acc = start;
+            for (int g = 0; g < kQ4Cols / G; ++g) {
+                f32x4_t start = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int k = 0; k < G / 32; ++k)
-                    acc = mfma16(q4_operand(code[q][g * (G / 32) + k], mask, one), xv[g * (G / 32) + k], acc);
-                const uint32_t lo = (uint32_t)scale, hi = (uint32_t)(scale >> 32);
-                y[q][0] += acc[0] * cdk::bf16_lo(lo);
-                y[q][1] += acc[1] * cdk::bf16_hi(lo);
-                y[q][2] += acc[2] * cdk::bf16_lo(hi);
-                y[q][3] += acc[3] * cdk::bf16_hi(hi);
+                    start = mfma16(minus24, xv[g * (G / 32) + k], start);
+#pragma unroll
+                for (int q = 0; q < NM; ++q) {
+                    const uint64_t scale =
+                        *reinterpret_cast<const uint64_t *>(s + kCodes + (q * WAVES + wave) * kScale + g * 32 + j * 8);
+                    f32x4_t acc = start;
+#pragma unroll
+                    for (int k = 0; k < G / 32; ++k)
+                        acc = mfma16(q4_operand(code[q][g * (G / 32) + k], mask, one), xv[g * (G / 32) + k], acc);
+                    const uint32_t lo = (uint32_t)scale, hi = (uint32_t)(scale >> 32);
+                    y[q][0] += acc[0] * cdk::bf16_lo(lo);
+                    y[q][1] += acc[1] * cdk::bf16_hi(lo);
+                    y[q][2] += acc[2] * cdk::bf16_lo(hi);
+                    y[q][3] += acc[3] * cdk::bf16_hi(hi);
+                }
             }
         }
-    }
-    // The waves' sums, each over the codes that it alone read. (They are read before the next barrier,
-    // and overwritten by loads after it.)
+        // The waves' sums, each over the codes that it alone read. (They are read before the next barrier,
+        // and overwritten by loads after it.)
 #pragma unroll
-    for (int q = 0; q < NM; ++q)
-        reinterpret_cast<f32x4_t *>(done)[(q * WAVES + wave) * cdk::kWave + lane] = y[q];
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (GATED ? wave > 0 : wave >= NM)
-        continue;
-    const auto total = [&](int q) {
-        const f32x4_t *sums = reinterpret_cast<const f32x4_t *>(done) + q * WAVES * cdk::kWave + lane;
-        f32x4_t v = sums[0];
+        for (int q = 0; q < NM; ++q)
+            reinterpret_cast<f32x4_t *>(done)[(q * WAVES + wave) * cdk::kWave + lane] = y[q];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (GATED ? wave > 0 : wave >= NM)
+            continue;
+        const auto total = [&](int q) {
+            const f32x4_t *sums = reinterpret_cast<const f32x4_t *>(done) + q * WAVES * cdk::kWave + lane;
+            f32x4_t v = sums[0];
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k)
-            v += sums[k * cdk::kWave];
-        return v;
-    };
-    const int row = (GATED ? part : part * NM + wave) * kQ4Rows + j * 4;
-    if (i16 >= a.T || row >= a.rows)
-        continue;
-    if constexpr (GATED) {
-        const f32x4_t g = total(0), u = total(1);
-        q4_store(a, i16, row, f32x4_t{g[0] * gt_sigmoid(g[0]) * u[0], g[1] * gt_sigmoid(g[1]) * u[1],
-                                      g[2] * gt_sigmoid(g[2]) * u[2], g[3] * gt_sigmoid(g[3]) * u[3]});
-    } else {
-        q4_store(a, i16, row, total(wave));
-    }
+            for (int k = 1; k < WAVES; ++k)
+                v += sums[k * cdk::kWave];
+            return v;
+        };
+        const int row = (GATED ? part : part * NM + wave) * kQ4Rows + j * 4;
+        if (i16 >= a.T || row >= a.rows)
+            continue;
+        if constexpr (GATED) {
+            const f32x4_t g = total(0), u = total(1);
+            q4_store(a, i16, row, f32x4_t{g[0] * gt_sigmoid(g[0]) * u[0], g[1] * gt_sigmoid(g[1]) * u[1],
+                                          g[2] * gt_sigmoid(g[2]) * u[2], g[3] * gt_sigmoid(g[3]) * u[3]});
+        } else {
+            q4_store(a, i16, row, total(wave));
+        }
     }
     gt_wait<0>();  // no load outlives the workgroup's LDS
 }
@@ -367,23 +372,22 @@ void q4_launch(const Q4Args &a, int parts, hipStream_t s)
         k_q4<NM, G, XT, W, GATED, false><<<grid, W * cdk::kWave, 0, s>>>(a);
 }
 
+// Many tokens and more parts than CUs: two workgroups of four waves a CU, whose steps are half as large
+// (16 tokens, 4096 -> 11008 gated 17.3 us against 19.2; 14336 -> 4096, 256 parts, 16.3 against 14.0).
 template <int NM, int G, int XT, bool GATED>
 void q4_launch(const Q4Args &a, hipStream_t s)
 {
     const int parts = ad_ceil(a.rows, kQ4Rows * (GATED ? 1 : NM));
-    constexpr int W1 = XT > 8 ? 8 : 8, W2 = XT > 8 ? 4 : 8;
-    if (parts <= 256)
-        q4_launch<NM, G, XT, W1, GATED>(a, parts, s);
+    if (XT > 8 && parts > 256)
+        q4_launch<NM, G, XT, (XT > 8 ? 4 : 8), GATED>(a, parts, s);
     else
-        q4_launch<NM, G, XT, W2, GATED>(a, parts, s);
+        q4_launch<NM, G, XT, 8, GATED>(a, parts, s);
 }
 
 template <int NM, int G, bool GATED>
 void q4_launch(const Q4Args &a, hipStream_t s)
 {
-    if (a.T == 1)
-        q4_launch<NM, G, 1, GATED>(a, s);
-    else if (a.T <= 4)
+    if (a.T <= 4)
         q4_launch<NM, G, 4, GATED>(a, s);
     else if (a.T <= 8)
         q4_launch<NM, G, 8, GATED>(a, s);
@@ -496,8 +500,10 @@ cd_status countdown_q4_project(const uint16_t *x, size_t ldx, int T, const void 
     if (st != CD_OK || T == 0)
         return st;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    // two row tiles a workgroup, which then read the tokens once, where enough workgroups are left
-    return d_out >= 32 * 224 ? q4_run<2, false>(a, group, s) : q4_run<1, false>(a, group, s);
+    // Two row tiles a workgroup, which then read the tokens once, where there are enough of either (16
+    // tokens, 4096 -> 14336 12.7 us against 15.4, 6144 7.6 against 8.2, 4096 7.4 against 6.2; one token, 4096 ->
+    // 14336 11.5 against 10.8).
+    return T > 4 && d_out >= 6144 ? q4_run<2, false>(a, group, s) : q4_run<1, false>(a, group, s);
 }
 
 cd_status countdown_q4_gated(const uint16_t *x, size_t ldx, int T, const void *W_gate, const void *W_up,
