@@ -527,15 +527,17 @@ __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtA
     gt_tile<KIND, BM, BN, BK, WM, WN, WK, STAGES, NT>(a, blockIdx.x, blockIdx.y, lds);
 }
 
+constexpr int kGtBackK = 256;  // columns of k of its tiles of dx
+
 // Little work: dx (the first `blocks` of the grid) and the weights' gradients in one launch.
-__global__ __launch_bounds__(256) void k_gt_back(const GtArgs x, const GtArgs w, int blocks)
+__global__ __launch_bounds__(512) void k_gt_back(const GtArgs x, const GtArgs w, int blocks)
 {
-    constexpr int kLds = std::max(kGtLds<kGtDx, 64, 64, 128, 1, 2, 2, 3>, kGtLds<kGtDw, 64, 64, 64, 2, 2, 1, 3>);
+    constexpr int kLds = std::max(kGtLds<kGtDx, 64, 64, kGtBackK, 1, 2, 4, 2>, kGtLds<kGtDw, 64, 64, 64, 2, 4, 1, 3>);
     __shared__ __align__(1024) char lds[kLds];
     if ((int)blockIdx.x < blocks)
-        gt_tile<kGtDx, 64, 64, 128, 1, 2, 2, 3, false>(x, blockIdx.x, 0, lds);
+        gt_tile<kGtDx, 64, 64, kGtBackK, 1, 2, 4, 2, false>(x, blockIdx.x, 0, lds);
     else
-        gt_tile<kGtDw, 64, 64, 64, 2, 2, 1, 3, false>(w, (int)blockIdx.x - blocks, 0, lds);
+        gt_tile<kGtDw, 64, 64, 64, 2, 4, 1, 3, false>(w, (int)blockIdx.x - blocks, 0, lds);
 }
 
 // Many tiles: 256 x 256 (256 x 128 of both projections), eight waves, each 64 rows of either half of
@@ -842,11 +844,11 @@ void gt_projections(const GtArgs &a, hipStream_t s)
 
 // dx and the weights' gradients in one launch, while a tile of dx needs no more than 16 tiles of k and both
 // make one or two rounds of workgroups. Captured us a call against launches of their own:
-//    37 tokens, 256 x 688 14.6 / 16.5   300, 256 x 1024 18.1 / 20.0   4000, 128 x 512 30.6 / 43.2
-//   with 32 tiles of k: 1000, 256 x 2048 31.2 / 34.6, but one token of 256 x 688 in two terms 19.6 / 16.5
+//    37 tokens, 256 x 688 13.7 / 16.6   300, 256 x 1024 17.6 / 20.0   1000, 256 x 2048 28.8 / 35.2
+//   4000 tokens, 128 x 512 32 / 43; with 24 tiles of k: 90 tokens, 504 x 952 in fp32 34.1 / 25.8
 bool gt_little(const GtArgs &a)
 {
-    return 2 * a.terms * ad_ceil(a.f, 128) <= 16 && (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 64) <= 512 &&
+    return 2 * a.terms * ad_ceil(a.f, kGtBackK) <= 16 && (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 64) <= 512 &&
            (int64_t)ad_ceil(a.f, 64) * ad_ceil(a.m, 64) * 2 <= 512;
 }
 
@@ -1046,10 +1048,10 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     aw.ldo = a.m;
     if (gt_little(a)) {
         ax.splits = aw.splits = 1;
-        ax.ktiles = 2 * a.terms * ad_ceil(a.f, 128);
+        ax.ktiles = 2 * a.terms * ad_ceil(a.f, kGtBackK);
         const int nx = dx ? gt_grid<kGtDx>(ax, a.T, a.m, 64, 64) : 0;
         const int nw = dW_gate || dW_up ? gt_grid<kGtDw>(aw, a.f, a.m, 64, 64) : 0;
-        k_gt_back<<<nx + nw, 256, 0, s>>>(ax, aw, nx);
+        k_gt_back<<<nx + nw, 512, 0, s>>>(ax, aw, nx);
     } else {
         if (dx)
             gt_dx(ax, s);

@@ -136,7 +136,8 @@ FWD = ["k_gt_product<%d,16,16,", "k_gt_product<%d,32,32,", "k_gt_product<%d,64,3
 
 
 @pytest.mark.parametrize("shape,proj,dx,dw", [  # T, d_model, d_ff; the kernels by what they start with
-    ((1, 256, 688), 0, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),  # dg in two terms
+    ((1, 256, 688), 0, "k_gt_back", None),
+    ((1, 256, 1400), 0, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),  # dg in two terms
     ((6, 256, 688), 0, "k_gt_back", None),
     ((1, 1032, 4104), 0, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),
     ((257, 2056, 2056), 3, "k_gt_product<2,64,128,", "k_gt_large<3,2>"),
@@ -144,7 +145,7 @@ FWD = ["k_gt_product<%d,16,16,", "k_gt_product<%d,32,32,", "k_gt_product<%d,64,3
     ((16, 4096, 14336), 0, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),
     ((17, 256, 688), 1, "k_gt_back", None),
     ((4000, 128, 512), 4, "k_gt_back", None),
-    ((17, 256, 1032), 1, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((17, 256, 2056), 1, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((100, 200, 2200), 2, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((200, 136, 3000), 3, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((500, 72, 3000), 4, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
