@@ -21,7 +21,7 @@ constexpr int kGtMaxDim = 65536, kGtMaxTokens = 1 << 20;
 constexpr size_t kGtMaxStride = (size_t)1 << 20;  // row strides: 256 rows stay below 2^30 bytes
 constexpr int kGtTerms = 3;                       // bf16 terms of an fp32 number
 constexpr int kGtOutside = 0x40000000;            // an offset past every resource: reads zeros
-constexpr size_t kGtPartFloats = (size_t)16 << 20; // place for dx's partial sums (64 MiB)
+constexpr size_t kGtPartFloats = (size_t)16 << 20;  // place for partial sums (64 MiB)
 
 constexpr int kGtFew = 4096;  // elements of dg that are held in two bf16 terms
 
@@ -40,9 +40,9 @@ struct GtArgs {
     size_t ldo;
     uint16_t *d;  // [terms][T][2 f]: dg and du of a token side by side
     int terms;
-    float *part;     // dx split over k: [splits][T][m]
+    float *part;     // their sums (gt_part)
     int mt, nt;      // tiles
-    int splits, ktiles;  // dx: workgroups that share a tile, and their tiles of k
+    int splits, ktiles;  // dx and dW: workgroups that share a tile, and their tiles of k
 };
 
 // a buffer resource over 2^30 bytes at p (uniform): what lies past them reads as zero
@@ -150,15 +150,18 @@ struct GtTile {
     }
 };
 
-// The workgroup's tile. Neighbours in time on one XCD (blockIdx.x % 8) take `group` tiles of m by a
-// stretch of n, so that its L2 holds what they share. False: no tile.
-__device__ __forceinline__ bool gt_place(int block, int mt, int nt, int &mi, int &ni)
+// The workgroup's tile, and its part of k: all tiles of one part after another, an even stretch of them on each
+// XCD (blockIdx.x % 8). Neighbours in time there take `group` tiles of m by a stretch of n, so that its L2
+// holds what they share. False: no tile.
+__device__ __forceinline__ bool gt_place(int block, int mt, int nt, int splits, int &mi, int &ni, int &split)
 {
     constexpr int group = 4;
-    const int total = mt * nt, per = (total + 7) / 8;
-    const int t = block % 8 * per + block / 8;
+    const int total = mt * nt * splits, per = (total + 7) / 8;
+    int t = block % 8 * per + block / 8;
     if (block / 8 >= per || t >= total)
         return false;
+    split = splits > 1 ? __builtin_amdgcn_readfirstlane(t / (mt * nt)) : 0;
+    t -= split * (mt * nt);
     const int width = group * nt, first = t / width * group, rows = min(group, mt - first);
     // known to be uniform: what follows from them stays in scalar registers
     mi = __builtin_amdgcn_readfirstlane(first + t % width % rows);
@@ -198,10 +201,11 @@ struct GtWalk {
             pn2 = pn + n2;
             left = a.f - kt % per * BK;
         } else {
-            pm = a.d + (a.terms - 1) * plane + (size_t)second * a.f + m0;
-            pn = a.x + n0;
+            const int kt = first / a.terms;
+            pm = a.d + (a.terms - 1) * plane + (size_t)second * a.f + m0 + (size_t)kt * BK * 2 * a.f;
+            pn = a.x + n0 + (size_t)kt * BK * a.ldx;
             pn2 = pn + n2;
-            left = a.T;
+            left = a.T - kt * BK;
         }
     }
 
@@ -303,6 +307,13 @@ __device__ __forceinline__ float gt_sigmoid(float g)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(err, ln2, 1.0f));
 }
 
+// where a split leaves its part: [splits][T][m], or [splits][2][f][m] of the gradients of W_gate and W_up
+template <int KIND>
+__device__ __forceinline__ float *gt_part(const GtArgs &a, int split, int second)
+{
+    return a.part + (KIND == kGtDx ? split * (size_t)a.T : (2 * split + second) * (size_t)a.f) * a.m;
+}
+
 // What KIND makes of a row's NF tiles (t, n: this lane's row and the first column; ok: the row exists).
 template <int NF>
 __device__ __forceinline__ void gt_forward(const GtArgs &a, size_t t, int n, bool ok, const f32x4_t (&g)[NF],
@@ -380,9 +391,9 @@ constexpr int kGtLds = std::max(STAGES * (BM + (KIND == kGtForward || KIND == kG
                                 (WK - 1) * WM * WN * (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * (BM / WM) *
                                     (BN / WN) * 4);  // the waves' sums
 
-// block, split: of the grid; lds: kGtLds bytes
+// block: of the grid; lds: kGtLds bytes
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT>
-__device__ __forceinline__ void gt_tile(const GtArgs &a, int block, int split, char *lds)
+__device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
 {
     constexpr int kThreads = WM * WN * WK * cdk::kWave;
     constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
@@ -391,8 +402,8 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, int split, c
     using TN = GtTile<BN, BK, kTwo, kThreads>;
     constexpr int kStage = TM::kBytes + NP * TN::kBytes;
     constexpr int kFlight = (TM::kLoads + NP * TN::kLoads) * (STAGES - 2);
-    int mi, ni;
-    if (!gt_place(block, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
+    int mi, ni, split;
+    if (!gt_place(block, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, kTwo ? 1 : a.splits, mi, ni, split))
         return;
     // dW: the tiles of W_gate's gradient, then those of W_up's
     const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
@@ -407,9 +418,9 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, int split, c
     TN tn;
     tm.init(ldm, M - m0);
     tn.init(ldn, N - n0);
-    const int first = KIND == kGtDx ? split * a.ktiles : 0;  // dx: a split of the tiles of k
+    const int first = kTwo ? 0 : split * a.ktiles;  // a split of the tiles of k
     const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
-    const int nk = KIND == kGtDx ? min(a.ktiles, all - first) : all;
+    const int nk = kTwo ? all : min(a.ktiles, all - first);
     GtWalk<KIND, BK> w;
     w.init(a, m0, n0, 0, second, first);
     const uint32_t base = gt_lds(lds);
@@ -513,8 +524,8 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, int split, c
             gt_forward(a, m, n, m < M, v[0], v[1]);
         else if constexpr (KIND == kGtBackward)
             gt_backward(a, m, n, m < M, dh[j], v[0], v[1]);
-        else if (KIND == kGtDx && a.splits > 1)
-            gt_store_sums(a.part + split * (size_t)a.T * a.m, CD_TYPE_F32, (size_t)m * a.m + n, m < M, N - n, v[0]);
+        else if (a.splits > 1)
+            gt_store_sums(gt_part<KIND>(a, split, second), CD_TYPE_F32, (size_t)m * a.m + n, m < M, N - n, v[0]);
         else
             gt_store_sums(KIND == kGtDw && second ? a.out2 : a.out, a.type, (size_t)m * a.ldo + n, m < M, N - n, v[0]);
     }
@@ -524,7 +535,7 @@ template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, 
 __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtArgs a)
 {
     __shared__ __align__(1024) char lds[kGtLds<KIND, BM, BN, BK, WM, WN, WK, STAGES>];
-    gt_tile<KIND, BM, BN, BK, WM, WN, WK, STAGES, NT>(a, blockIdx.x, blockIdx.y, lds);
+    gt_tile<KIND, BM, BN, BK, WM, WN, WK, STAGES, NT>(a, blockIdx.x, lds);
 }
 
 constexpr int kGtBackK = 256;  // columns of k of its tiles of dx
@@ -535,9 +546,9 @@ __global__ __launch_bounds__(512) void k_gt_back(const GtArgs x, const GtArgs w,
     constexpr int kLds = std::max(kGtLds<kGtDx, 64, 64, kGtBackK, 1, 2, 4, 2>, kGtLds<kGtDw, 64, 64, 64, 2, 4, 1, 3>);
     __shared__ __align__(1024) char lds[kLds];
     if ((int)blockIdx.x < blocks)
-        gt_tile<kGtDx, 64, 64, kGtBackK, 1, 2, 4, 2, false>(x, blockIdx.x, 0, lds);
+        gt_tile<kGtDx, 64, 64, kGtBackK, 1, 2, 4, 2, false>(x, blockIdx.x, lds);
     else
-        gt_tile<kGtDw, 64, 64, 64, 2, 4, 1, 3, false>(w, (int)blockIdx.x - blocks, 0, lds);
+        gt_tile<kGtDw, 64, 64, 64, 2, 4, 1, 3, false>(w, (int)blockIdx.x - blocks, lds);
 }
 
 // Many tiles: 256 x 256 (256 x 128 of both projections), eight waves, each 64 rows of either half of
@@ -567,8 +578,9 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     static_assert(TM::kBytes == TN::kBytes && TM::kLoads == 2 && TN::kLoads == 2, "loads of a phase");
     __shared__ __align__(1024) char lds[kStages * kStage];
 
-    int mi, ni;
-    if (!gt_place(blockIdx.x, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, mi, ni))
+    int mi, ni, split;
+    if (!gt_place(blockIdx.x, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, kTwo ? 1 : a.splits, mi, ni,
+                  split))
         return;
     const int second = KIND == kGtDw ? (!a.out || mi >= a.mt) : 0;
     if (KIND == kGtDw && mi >= a.mt)
@@ -577,9 +589,9 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
     const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
     const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
-    const int first = KIND == kGtDx ? (int)blockIdx.y * a.ktiles : 0;  // dx: a split of the tiles of k
+    const int first = kTwo ? 0 : split * a.ktiles;  // a split of the tiles of k
     const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
-    const int nk = KIND == kGtDx ? min(a.ktiles, all - first) : all;
+    const int nk = kTwo ? all : min(a.ktiles, all - first);
 
     TM tm[MH];
     TN tn[2];
@@ -709,8 +721,8 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
                 void *out = KIND == kGtDw && second ? a.out2 : a.out;
                 int type = a.type;
                 size_t at = (size_t)m * a.ldo + n;
-                if (KIND == kGtDx && a.splits > 1) {
-                    out = a.part + blockIdx.y * (size_t)a.T * a.m;
+                if (a.splits > 1) {
+                    out = gt_part<KIND>(a, split, second);
                     type = CD_TYPE_F32;
                     at = (size_t)m * a.m + n;
                 }
@@ -721,17 +733,21 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
         }
 }
 
-// dx from its parts, in their order; four columns a thread
+// dx, or the weights' gradients (blockIdx.y), from the parts in their order; four columns a thread
+template <int KIND>
 __global__ __launch_bounds__(256) void k_gt_sum(const GtArgs a)
 {
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (size_t)a.T * a.m;
-    if (i >= n)
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (KIND == kGtDx ? (size_t)a.T : a.f) * a.m;
+    void *out = blockIdx.y ? a.out2 : a.out;
+    if (i >= n || !out)
         return;
-    f32x4_t s = *reinterpret_cast<const f32x4_t *>(a.part + i);
+    const float *p = gt_part<KIND>(a, 0, blockIdx.y) + i;
+    const size_t step = KIND == kGtDx ? n : 2 * n;
+    f32x4_t s = *reinterpret_cast<const f32x4_t *>(p);
 #pragma unroll 8
     for (int k = 1; k < a.splits; ++k)
-        s += *reinterpret_cast<const f32x4_t *>(a.part + k * n + i);
-    gt_store4(a.out, a.type, i / a.m * a.ldo + i % a.m, s);
+        s += *reinterpret_cast<const f32x4_t *>(p + k * step);
+    gt_store4(out, a.type, i / a.m * a.ldo + i % a.m, s);
 }
 
 __global__ __launch_bounds__(256) void k_gt_zero(uint32_t *p, size_t words)
@@ -752,54 +768,58 @@ struct cd_gated {
 
 namespace {
 
-// dx: how many workgroups share a tile of it
+// How many workgroups share a tile of dx or of the weights' gradients: each takes four tiles of k and more.
+template <int KIND>
 void gt_split(GtArgs &a, int BK, int splits)
 {
-    const int all = 2 * ad_ceil(a.f, BK);  // each with all terms
+    a.splits = 1;
+    if (KIND != kGtDx && KIND != kGtDw)
+        return;
+    const int all = KIND == kGtDx ? 2 * ad_ceil(a.f, BK) : ad_ceil(a.T, BK);  // each with all terms
     a.ktiles = a.terms * ad_ceil(all, std::max(1, std::min(splits, all / 4)));
     a.splits = ad_ceil(a.terms * all, a.ktiles);
 }
 
+template <int KIND>
 void gt_sum(const GtArgs &a, hipStream_t s)
 {
+    const size_t n = (KIND == kGtDx ? (size_t)a.T : a.f) * a.m;
     if (a.splits > 1)
-        k_gt_sum<<<(unsigned)(((size_t)a.T * a.m / 4 + 255) / 256), 256, 0, s>>>(a);
+        k_gt_sum<KIND><<<dim3((unsigned)((n / 4 + 255) / 256), KIND == kGtDx ? 1 : 2), 256, 0, s>>>(a);
 }
 
-// workgroups of tiles of bm x bn (of both gradients of weights, as far as they are wanted)
+// workgroups of tiles of bm x bn (of both gradients of weights, as far as they are wanted), of all parts of k
 template <int KIND>
 int gt_grid(GtArgs &a, int M, int N, int bm, int bn)
 {
     a.mt = ad_ceil(M, bm);
     a.nt = ad_ceil(N, bn);
-    return ad_ceil(a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1), 8) * 8;
+    return ad_ceil(a.mt * a.nt * (KIND == kGtDw && a.out && a.out2 ? 2 : 1) * a.splits, 8) * 8;
 }
 
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
 void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
-    a.splits = 1;
-    if (KIND == kGtDx)
-        gt_split(a, BK, splits);
-    const dim3 grid(gt_grid<KIND>(a, M, N, BM, BN), a.splits), block(WM * WN * WK * cdk::kWave);
+    gt_split<KIND>(a, BK, splits);
+    const int grid = gt_grid<KIND>(a, M, N, BM, BN), block = WM * WN * WK * cdk::kWave;
     // Weights that are read once and would sweep most of the last-level cache go past it.
     constexpr bool weights = KIND != kGtDw && BM <= 64;
     if (weights && a.mt == 1 && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
         k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, weights><<<grid, block, 0, s>>>(a);
     else
         k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, false><<<grid, block, 0, s>>>(a);
-    gt_sum(a, s);
+    if constexpr (KIND == kGtDx || KIND == kGtDw)
+        gt_sum<KIND>(a, s);
 }
 
 template <int KIND, int MH>
 void gt_large(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
-    a.splits = 1;
-    if (KIND == kGtDx)
-        gt_split(a, 64, splits);
+    gt_split<KIND>(a, 64, splits);
     const int grid = gt_grid<KIND>(a, M, N, 128 * MH, KIND == kGtForward || KIND == kGtBackward ? 128 : 256);
-    k_gt_large<KIND, MH><<<dim3(grid, a.splits), 512, 0, s>>>(a);
-    gt_sum(a, s);
+    k_gt_large<KIND, MH><<<grid, 512, 0, s>>>(a);
+    if constexpr (KIND == kGtDx || KIND == kGtDw)
+        gt_sum<KIND>(a, s);
 }
 
 // 256 x 256 against 128 x 256: rounds of workgroups over the CUs, of which the former's take half as long
@@ -842,30 +862,48 @@ void gt_projections(const GtArgs &a, hipStream_t s)
         gt_large<KIND, 2>(a, a.T, a.f, s);
 }
 
+// Few tiles of 64 x 64 and many tokens: workgroups that share a tile and fill the CUs twice (their sums take
+// at most 512 tiles of the place). Backward us a call, so against whole tiles in one launch with dx: 4392 tokens
+// of 168 x 72 19.6 / 31.5, 8000 of 256 x 256 39.6 / 62.8, 3000 of 64 x 512 in fp32 36.9 / 61.0, but 1024 of 256 x 256
+// 20.8 / 13.8.
+int gt_dw_splits(const GtArgs &a)
+{
+    const int64_t tiles = (int64_t)ad_ceil(a.f, 64) * ad_ceil(a.m, 64) * 2;
+    return tiles <= 128 && a.T * a.terms > 2048 ? (int)(512 / tiles) : 1;
+}
+
 // dx and the weights' gradients in one launch, while a tile of dx needs no more than 16 tiles of k and both
 // make one or two rounds of workgroups. Captured us a call against launches of their own:
 //    37 tokens, 256 x 688 13.7 / 16.6   300, 256 x 1024 17.6 / 20.0   1000, 256 x 2048 28.8 / 35.2
-//   4000 tokens, 128 x 512 32 / 43; with 24 tiles of k: 90 tokens, 504 x 952 in fp32 34.1 / 25.8
+//   with 24 tiles of k: 90, 504 x 952 in fp32 34.1 / 25.8
 bool gt_little(const GtArgs &a)
 {
     return 2 * a.terms * ad_ceil(a.f, kGtBackK) <= 16 && (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 64) <= 512 &&
-           (int64_t)ad_ceil(a.f, 64) * ad_ceil(a.m, 64) * 2 <= 512;
+           (int64_t)ad_ceil(a.f, 64) * ad_ceil(a.m, 64) * 2 <= 512 && gt_dw_splits(a) == 1;
 }
 
-// dx. 64 x 128 tiles up to 64 tokens and while there are 128 of them at most, shared by workgroups that fill
-// the CUs twice, else 256 x 256 (backward us a call, the first against the second: 256 tokens of 1024 x 2816 41
-// against 52, 1024 of them 68 against 83, 512 tokens of 4096 x 14336, 256 tiles, 448 against 386).
+// dx: 64 x 128 tiles, shared by workgroups that fill the CUs twice, or 256 x 256, by what the two were
+// measured to take: 0.74 and 1.55 us a tile of k of a round, 2 and 4 around it, and for parts 3 and a write and a
+// read of each at 4 TB/s. (Backward us a call, the first against the second: 256 tokens of 1024 x 2816 41 against 52,
+// 512 tokens of 4096 x 14336 448 against 386, 655 tokens of 1336 x 6976 in fp32 276 against 244.)
 void gt_dx(const GtArgs &a, hipStream_t s)
 {
     // workgroups that share a tile: one round over the CUs, and what the place for their sums holds
     const int most = (int)std::min<size_t>(64, kGtPartFloats / ((size_t)a.T * a.m));
-    const auto splits = [&](int bm, int bn, int slots) {
-        return std::max(1, (int)std::min<int64_t>(most, slots / ((int64_t)ad_ceil(a.T, bm) * ad_ceil(a.m, bn))));
+    const auto time = [&](int bm, int bn, int slots, double tile, double around, int &splits) {
+        const int64_t tiles = (int64_t)ad_ceil(a.T, bm) * ad_ceil(a.m, bn);
+        GtArgs b = a;
+        gt_split<kGtDx>(b, 64, (int)std::min<int64_t>(most, slots / tiles));
+        splits = b.splits;
+        const double sums = b.splits > 1 ? 3 + (double)b.splits * a.T * a.m * 8 / 4e6 : 0;
+        return (double)((tiles * b.splits + slots - 1) / slots) * (b.ktiles * tile + around) + sums;
     };
-    if (a.T <= 64 || (int64_t)ad_ceil(a.T, 64) * ad_ceil(a.m, 128) <= 128)
-        gt_product<kGtDx, 64, 128, 64, 2, 2, 1, 3>(a, a.T, a.m, s, splits(64, 128, 512));
+    int narrow, wide;
+    const double tn = time(64, 128, 512, 0.74, 2, narrow), tw = time(256, 256, 256, 1.55, 4, wide);
+    if (tn <= tw)
+        gt_product<kGtDx, 64, 128, 64, 2, 2, 1, 3>(a, a.T, a.m, s, narrow);
     else
-        gt_large<kGtDx, 2>(a, a.T, a.m, s, splits(256, 256, 256));
+        gt_large<kGtDx, 2>(a, a.T, a.m, s, wide);
 }
 
 // The weights' gradients. Past 512 tiles of 64 x 64: 128 x 128, two workgroups a CU, for few tokens (which
@@ -876,7 +914,7 @@ void gt_dw(const GtArgs &a, hipStream_t s)
 {
     const auto tiles = [&](int b) { return (int64_t)ad_ceil(a.f, b) * ad_ceil(a.m, b) * 2; };  // of both gradients
     if (tiles(64) <= 512)
-        gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, s);
+        gt_product<kGtDw, 64, 64, 64, 2, 2, 1, 3>(a, a.f, a.m, s, gt_dw_splits(a));
     else if (a.T * a.terms <= 256 || 113 * ((tiles(128) + 511) / 512) <= 200 * ((tiles(256) + 255) / 256))
         gt_product<kGtDw, 128, 128, 64, 2, 2, 1, 2>(a, a.f, a.m, s);
     else
@@ -1049,6 +1087,7 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     if (gt_little(a)) {
         ax.splits = aw.splits = 1;
         ax.ktiles = 2 * a.terms * ad_ceil(a.f, kGtBackK);
+        aw.ktiles = a.terms * ad_ceil(a.T, 64);
         const int nx = dx ? gt_grid<kGtDx>(ax, a.T, a.m, 64, 64) : 0;
         const int nw = dW_gate || dW_up ? gt_grid<kGtDw>(aw, a.f, a.m, 64, 64) : 0;
         k_gt_back<<<nx + nw, 512, 0, s>>>(ax, aw, nx);

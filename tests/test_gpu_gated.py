@@ -100,7 +100,7 @@ SHAPES = [  # T, d_model, d_ff: every tile, its edges, one element of a tile, wh
     (384, 72, 16640),
     # dx in one part; the gradients of the weights in 256 x 256 tiles, of few and of many tokens
     (4100, 2104, 72), (70, 1032, 4104), (300, 2104, 2600), (257, 2056, 2056), (1, 1032, 4104),
-    (17, 264, 2056), (17, 264, 1032), (4000, 128, 512), (65, 520, 1000),  # launches of their own; one for dx and the weights' gradients
+    (4392, 168, 72), (1024, 256, 256), (1100, 8, 8), (655, 1336, 2000), (17, 264, 2056), (17, 264, 1032), (4000, 128, 512), (65, 520, 1000),  # launches of their own; one for dx and the weights' gradients
 ]
 
 
