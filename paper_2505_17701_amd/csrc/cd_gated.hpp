@@ -563,8 +563,8 @@ __global__ __launch_bounds__(512) void k_gt_back(const GtArgs x, const GtArgs w,
 // What bounds it is the matrix cores' clock under load (80 % busy in the forward call, 78 in dx) and, where an
 // operand has k across its rows, twice as many LDS reads of half the size (61 % in the weights' gradients,
 // 1352 us if they were whole reads, 1600 so). 8192 tokens of 4096 x 14336: forward 1284 us (1498 TFLOP/s),
-// projections of the backward call 1437 (470 MB are stored, 235 loaded at the end of a tile), dx 1320,
-// weights 1570. Four barriers a phase of 16 MFMAs instead: 1360. Persistent workgroups that load the next
+// projections of the backward call 1420 (470 MB are stored, 235 loaded at the end of a tile), dx 1320 to
+// 1430, weights 1480 to 1570. Four barriers a phase of 16 MFMAs instead: 1360. Persistent workgroups that load the next
 // tile while they store: 1334 and, backward, 4468 against 4262.
 template <int KIND, int MH>
 __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
@@ -838,7 +838,8 @@ bool gt_wide(int64_t wide, int64_t narrow) { return 3 * ((wide + 255) / 256) <= 
 //   333 tokens, 3000 x 8008      181    117     97.3   78.2    77.3    55.1     65.9     79.8
 //   256 tokens, 4096 x 14336     303    165    140    117      89.2   102       74.1     86.1
 //   512 tokens, 4096 x 14336     594    297    260    192     159     150      124       95.5
-// (16 x 16 for up to 16 tokens always: what is read there counts.)
+// (16 x 16 for up to 16 tokens always: what is read there counts; and 64 x 64 for up to 64: 32 tokens of
+// 8192 x 28672, 448 tiles, 175 us against 193 of 128 x 128.)
 template <int KIND>
 void gt_projections(const GtArgs &a, hipStream_t s)
 {
@@ -849,7 +850,7 @@ void gt_projections(const GtArgs &a, hipStream_t s)
         gt_product<KIND, 32, 32, 128, 1, 2, 2, 4>(a, a.T, a.f, s);
     else if (fits(64, 32))
         gt_product<KIND, 64, 32, 128, 2, 2, 1, 4>(a, a.T, a.f, s);
-    else if (fits(64, 64))
+    else if (a.T <= 64 || fits(64, 64))
         gt_product<KIND, 64, 64, 128, 2, 4, 1, 3>(a, a.T, a.f, s);
     else if (fits(128, 64))
         gt_product<KIND, 128, 64, 64, 2, 4, 1, 3>(a, a.T, a.f, s);

@@ -97,7 +97,7 @@ SHAPES = [  # T, d_model, d_ff: every tile, its edges, one element of a tile, wh
     (1300, 1544, 2056), (2048, 512, 1024), (4100, 72, 136),
     # tiles of the projections by how many workgroups they make (test_host_gated_q4.py names them)
     (100, 200, 2200), (200, 136, 3000), (500, 72, 3000), (700, 72, 3504), (900, 72, 4000), (2000, 264, 4104),
-    (384, 72, 16640),
+    (384, 72, 16640), (20, 72, 16400), (48, 1032, 16640),
     # dx in one part; the gradients of the weights in 256 x 256 tiles, of few and of many tokens
     (4100, 2104, 72), (70, 1032, 4104), (300, 2104, 2600), (257, 2056, 2056), (1, 1032, 4104),
     (4392, 168, 72), (1024, 256, 256), (1100, 8, 8), (655, 1336, 2000), (17, 264, 2056), (17, 264, 1032), (4000, 128, 512), (65, 520, 1000),  # launches of their own; one for dx and the weights' gradients
@@ -335,6 +335,44 @@ def test_rows_past_32_bits(cd):
         for a, b in zip(cd.countdown_gated_backward(p, x, c.dh, c.Wg, c.Wu),
                         cd.countdown_gated_backward(p, c.x, c.dh, c.Wg, c.Wu)):
             assert torch.equal(a, b)
+
+
+def test_tokens_past_32_bits(cd):
+    """h, dg and du of more than 2^32 bytes, against the last tokens alone."""
+    T, m, f, n = 131080, 64, 8200, 300  # T 2 f > 2^31 elements
+    last = Case(n, m, f)
+    x = torch.randn((T, m), device="cuda").to(BF16)
+    dh = torch.zeros((T, f), dtype=BF16, device="cuda")
+    x[-n:], dh[-n:] = last.x, last.dh
+    with cd.Gated(m, f, T, train=True) as p:
+        h = cd.countdown_gated_forward(p, x, last.Wg, last.Wu, h=torch.empty((T, f), device="cuda"))
+        check(h[-n:], *last.h(), "h")
+        del h
+        dx, dWg, dWu = cd.countdown_gated_backward(p, x, dh, last.Wg, last.Wu)
+    assert not bool(dx[:-n].any())
+    # the other tokens add zeros to the weights' gradients: the sum of n tokens, in whatever order
+    for got, (name, (ref, bound)) in zip((dx[-n:], dWg, dWu), last.grads(BF16).items()):
+        check(got, ref, bound, name)
+
+
+def test_largest_matrices(cd):
+    """65536 x 65536: 2^33 bytes a matrix; the last neurons, whose dh alone is not zero."""
+    T, m, n = 3, 65536, 64
+    f = m
+    last = Case(T, m, n)
+    Wg = torch.randn((f, m), dtype=BF16, device="cuda").mul_(0.005)
+    Wu = torch.randn((f, m), dtype=BF16, device="cuda").mul_(0.005)
+    Wg[-n:], Wu[-n:] = last.Wg, last.Wu
+    dh = torch.zeros((T, f), dtype=BF16, device="cuda")
+    dh[:, -n:] = last.dh
+    with cd.Gated(m, f, T, train=True) as p:
+        h = cd.countdown_gated_forward(p, last.x, Wg, Wu, h=torch.empty((T, f), device="cuda"))
+        check(h[:, -n:], *last.h(), "h")
+        dx, dWg, dWu = cd.countdown_gated_backward(p, last.x, dh, Wg, Wu)
+    assert not bool(dWg[:-n].any()) and not bool(dWu[:-n].any())
+    last.f = f  # (T d_ff > 4096: one bf16 term; and as many products for dx)
+    for got, (name, (ref, bound)) in zip((dx, dWg[-n:], dWu[-n:]), last.grads(BF16).items()):
+        check(got, ref, bound, name)
 
 
 def test_binding_refusals(cd):

@@ -108,6 +108,37 @@ def test_gated(cd, shape, group):
         check(h, silu * u, bound, "h")
 
 
+@pytest.mark.parametrize("T,rows", [(5, 6152), (9, 8008)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_two_row_tiles_of_an_odd_number(cd, T, rows, group):
+    g = rng(3)
+    W, x = Matrix(g, rows, 712, group), tokens(g, T, 712)
+    check(cd.countdown_q4_project(x, W.pack(cd)), *W.product(x), "y")
+
+
+def test_largest_matrices(cd):
+    """65536 x 65536: the last rows, past 2^31 bytes of the packed matrix."""
+    n, rows, cols, group = 48, 65536, 65536, 128
+    g = rng(4)
+    last, x = Matrix(g, n, cols, group), tokens(g, 16, cols)
+    W = Matrix(g, rows, cols, group)
+    W.codes[-n:], W.scale[-n:] = last.codes, last.scale
+    q = W.pack(cd)
+    assert q.data.numel() > 2 ** 31
+    ref, bound = last.product(x)
+    for T in (1, 16):
+        check(cd.countdown_q4_project(x[:T], q)[:, -n:], ref[:T], bound[:T], "y")
+        h = cd.countdown_q4_gated(x[:T], q, q, h=torch.empty((T, rows), device="cuda"))
+        a, e = ref[:T], bound[:T]
+        silu = a * torch.sigmoid(a)
+        check(h[:, -n:], silu * a, 1.1 * e * a.abs() + (silu.abs() + 1.1 * e) * e + 16 * U * (silu * a).abs(), "h")
+    dense = cd.countdown_q4_unpack(q)
+    check(dense[-n:], last.dense(), torch.zeros_like(last.dense()), "unpacked")
+    again = cd.countdown_q4_quantize(dense, group)
+    assert torch.equal(cd.countdown_q4_unpack(again)[-n:],
+                       cd.countdown_q4_unpack(cd.countdown_q4_quantize(dense[-n:], group)))
+
+
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("rows,cols", [(8, 8), (16, 128), (40, 1000), (256, 688), (24, 33000)])
 def test_unpack_gives_back_what_was_packed(cd, rows, cols, group):

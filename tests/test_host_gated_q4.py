@@ -153,6 +153,7 @@ FWD = ["k_gt_product<%d,16,16,", "k_gt_product<%d,32,32,", "k_gt_product<%d,64,3
     ((500, 72, 3000), 4, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((700, 72, 3504), 5, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
     ((900, 72, 4000), 6, "k_gt_product<2,64,128,", "k_gt_product<3,64,64,"),
+    ((48, 1032, 16640), 3, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),  # more than 256 tiles
     ((384, 72, 16640), 6, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),
     ((2000, 264, 4104), 7, "k_gt_product<2,64,128,", "k_gt_product<3,128,128,"),
     ((1300, 1544, 2056), 5, "k_gt_large<2,2>", "k_gt_product<3,128,128,"),
