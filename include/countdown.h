@@ -490,7 +490,8 @@ typedef struct cd_gated cd_gated;
  * multiples of 8 up to 65536; 1 <= max_tokens <= 2^20. CD_EINVAL for malformed sizes and flags,
  * CD_EUNSUPPORTED beyond those limits (both before any HIP call), CD_ENOMEM / CD_EHIP when
  * allocation fails. *out is set only on success. CD_GATED_TRAIN takes 4 max_tokens d_ff
- * bytes (dg and du) and 64 MiB + 16 KB, with CD_GATED_FP32_GRADS 12 max_tokens d_ff and 64 MiB.
+ * bytes (dg and du; d_ff rounded up to a multiple of 64) and 64 MiB + 128 KB, with
+ * CD_GATED_FP32_GRADS 12 max_tokens d_ff and 64 MiB.
  */
 cd_status countdown_gated_create(int d_model, int d_ff, int max_tokens, unsigned flags,
                                  cd_gated **out);

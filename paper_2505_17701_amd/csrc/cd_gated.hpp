@@ -38,7 +38,10 @@ struct GtArgs {
     void *out;   // h or dx; dW: the gradient of W_gate
     void *out2;  // dW: the gradient of W_up
     size_t ldo;
-    uint16_t *d;  // [terms][T][2 f]: dg and du of a token side by side
+    uint16_t *d;  // [terms][T][2][fd]: dg and du of a token side by side
+    // f rounded up to 128 bytes, so that rows begin on a cache line (backward of 2000 tokens of 1000 x 3000 in fp32 204 us
+    // against 214, of 1000 of 1024 x 2008 53.6 against 55.5)
+    int fd;
     int terms;
     float *part;     // their sums (gt_part)
     int mt, nt;      // tiles
@@ -183,7 +186,7 @@ struct GtWalk {
     // n2: from n's tile to the one beside it
     __device__ __forceinline__ void init(const GtArgs &a, int m0, int n0, int n2, int second, int first)
     {
-        const size_t plane = (size_t)a.T * 2 * a.f;
+        const size_t plane = (size_t)a.T * 2 * a.fd;
         term = product = 0;
         if constexpr (kTwo) {
             pm = a.x + m0 * a.ldx;
@@ -192,8 +195,8 @@ struct GtWalk {
             left = a.m;
         } else if constexpr (KIND == kGtDx) {
             const int per = (a.f + BK - 1) / BK, kt = first / a.terms;  // (first: a multiple of the terms)
-            const uint16_t *d = a.d + (a.terms - 1) * plane + m0 * (2 * (size_t)a.f);
-            m1 = d + a.f;
+            const uint16_t *d = a.d + (a.terms - 1) * plane + m0 * (2 * (size_t)a.fd);
+            m1 = d + a.fd;
             n1 = a.Wu + n0;
             product = kt >= per;
             pm = (product ? m1 : d) + (size_t)(kt % per) * BK;
@@ -202,7 +205,7 @@ struct GtWalk {
             left = a.f - kt % per * BK;
         } else {
             const int kt = first / a.terms;
-            pm = a.d + (a.terms - 1) * plane + (size_t)second * a.f + m0 + (size_t)kt * BK * 2 * a.f;
+            pm = a.d + (a.terms - 1) * plane + (size_t)second * a.fd + m0 + (size_t)kt * BK * 2 * a.fd;
             pn = a.x + n0 + (size_t)kt * BK * a.ldx;
             pn2 = pn + n2;
             left = a.T - kt * BK;
@@ -217,13 +220,13 @@ struct GtWalk {
             pn2 += BK;
             left -= BK;
         } else {
-            const size_t plane = (size_t)a.T * 2 * a.f;
+            const size_t plane = (size_t)a.T * 2 * a.fd;
             if (++term < a.terms) {
                 pm -= plane;
                 return;
             }
             term = 0;
-            pm += (a.terms - 1) * plane + (KIND == kGtDw ? (size_t)BK * 2 * a.f : BK);
+            pm += (a.terms - 1) * plane + (KIND == kGtDw ? (size_t)BK * 2 * a.fd : BK);
             pn += (size_t)BK * (KIND == kGtDw ? a.ldx : a.m);
             pn2 = pn + n2;
             left -= BK;
@@ -352,7 +355,7 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
         }
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        uint16_t *o = a.d + t * (2 * (size_t)a.f) + (size_t)q * a.f + n;
+        uint16_t *o = a.d + t * (2 * (size_t)a.fd) + (size_t)q * a.fd + n;
         if (a.terms == 1) {
             gt_store_sums(o, CD_TYPE_BF16, 0, ok, a.f - n, d[q]);
             continue;
@@ -374,7 +377,7 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
 #pragma unroll
         for (int k = 0; k < kGtTerms; ++k)
             if (k < a.terms)
-                gt_store_tiles(o + (size_t)k * a.T * 2 * a.f, ok, a.f - n, out[k]);
+                gt_store_tiles(o + (size_t)k * a.T * 2 * a.fd, ok, a.f - n, out[k]);
     }
 }
 
@@ -412,7 +415,7 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
     const int m0 = mi * BM, n0 = ni * BN;
     const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
     const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
-    const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
+    const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.fd, ldn = KIND == kGtDw ? a.ldx : a.m;
 
     TM tm;
     TN tn;
@@ -588,7 +591,7 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
     const int m0 = mi * (128 * MH), n0 = ni * (kTwo ? 128 : 256);
     const int M = KIND == kGtDw ? a.f : a.T, N = kTwo ? a.f : a.m;
     const int K = kTwo ? a.m : KIND == kGtDx ? a.f : a.T;
-    const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.f, ldn = KIND == kGtDw ? a.ldx : a.m;
+    const size_t ldm = kTwo ? a.ldx : 2 * (size_t)a.fd, ldn = KIND == kGtDw ? a.ldx : a.m;
     const int first = kTwo ? 0 : split * a.ktiles;  // a split of the tiles of k
     const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
     const int nk = kTwo ? all : min(a.ktiles, all - first);
@@ -767,6 +770,8 @@ struct cd_gated {
 };
 
 namespace {
+
+int gt_fd(int f) { return (f + 63) / 64 * 64; }
 
 // How many workgroups share a tile of dx or of the weights' gradients: each takes four tiles of k and more.
 template <int KIND>
@@ -963,9 +968,9 @@ cd_status countdown_gated_create(int d_model, int d_ff, int max_tokens, unsigned
     p->flags = flags;
     p->device = dev;
     if (flags & CD_GATED_TRAIN) {
-        const size_t one = (size_t)max_tokens * 2 * d_ff * sizeof(uint16_t);
-        const size_t planes = flags & CD_GATED_FP32_GRADS ? (kGtTerms * one + 255) / 256 * 256
-                                                          : (one + 255) / 256 * 256 + kGtFew * 2 * sizeof(uint16_t);
+        // two terms: T d_ff <= kGtFew, and rounding up to 64 makes at most eight times as much of it
+        const size_t one = (size_t)max_tokens * 2 * gt_fd(d_ff) * sizeof(uint16_t);
+        const size_t planes = flags & CD_GATED_FP32_GRADS ? kGtTerms * one : one + 8 * kGtFew * 2 * sizeof(uint16_t);
         if (hip_status(hipMalloc(&p->ws, planes + kGtPartFloats * sizeof(float))) != CD_OK) {
             delete p;
             return CD_ENOMEM;
@@ -1072,6 +1077,7 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     a.f = p->f;
     a.type = type;
     a.d = p->d;
+    a.fd = gt_fd(p->f);
     a.part = p->part;
     // The errors of few rounded numbers do not average out in a gradient (that of one token over 64
     // neurons may be 1.5 times as far off as its own rounding puts it, over many 1.41); a second term
