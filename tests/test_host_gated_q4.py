@@ -7,6 +7,7 @@ import pytest
 import host_hip
 
 M, F, T = 264, 520, 64
+F64 = -(-F // 64) * 64
 P = {n: 0x100000000 * (i + 1) for i, n in enumerate(
     ("x", "dh", "Wg", "Wu", "h", "dx", "dWg", "dWu", "W", "base", "y", "codes", "scale", "packed"))}
 
@@ -81,7 +82,7 @@ def test_a_failed_allocation_leaves_nothing(host):
     assert host.lib.host_hip_live_allocations() == live
 
 
-@pytest.mark.parametrize("flags,size", [(1, 4 * T * F + (16 << 10)), (3, 12 * T * F)])
+@pytest.mark.parametrize("flags,size", [(1, 4 * T * F64 + (128 << 10)), (3, 12 * T * F64)])
 def test_the_workspace_takes_what_the_header_says(host, flags, size):
     most = size + (64 << 20)
     for limit, status in ((most + 256, 0), (most - 1, host.cd.CD_ENOMEM)):
