@@ -92,7 +92,12 @@ __device__ __forceinline__ uint32_t gt_lds(const void *p)
 // rows of an operand over the banks. Otherwise BK rows of R; the 32-byte slots of row k are permuted
 // by k & 3 and bit 3 of k, so that what the lanes of a transposing read take (rows 8 j + 0..3 of one
 // slot for 16 lanes, j = lane / 16) lies on different banks.
-template <int R, int BK, bool KC, int THREADS>
+//
+// LINES (KC, BK 64): rows that begin inside a cache line. A tile then holds a whole line of each row, of which the first
+// chunks may belong to the tile of k before, so that its loads take one line a row and not two; products read
+// two tiles in a row. Row r begins p8 + r ld8 chunks behind a line's start; its chunks' places in the line are
+// permuted by the bits of r that this leaves alike.
+template <int R, int BK, bool KC, int THREADS, bool LINES = false>
 struct GtTile {
     static constexpr int kRowChunks = (KC ? BK : R) / 8;
     static constexpr int kLoads = R * BK / 8 / THREADS;
@@ -100,19 +105,29 @@ struct GtTile {
     static constexpr int kRowsALoad = THREADS / kRowChunks;
     static_assert(R * BK / 8 % THREADS == 0 && THREADS % kRowChunks == 0, "whole loads");
     static_assert(!KC || kRowsALoad % 8 == 0, "the row's swizzle is the same for every load");
+    static_assert(!LINES || (KC && BK == 64), "a line of a row");
 
     int off[kLoads];  // byte offset from the tile's first element
     int k[kLoads];    // k of this thread's chunks
+    uint32_t p8, ld8;
 
     static __device__ __forceinline__ int slot_key(int k) { return ((k & 3) | (k >> 1 & 4)) & (R / 16 - 1); }
 
-    // valid: rows (KC) or columns that the operand has from this tile on
-    __device__ __forceinline__ void init(size_t ld, int valid)
+    __device__ __forceinline__ int key(int r) const { return (r & 7) >> (3 - __builtin_ctz(ld8 | 8u)); }
+
+    // p: the operand; valid: its rows (KC) or columns from this tile on
+    __device__ __forceinline__ void init(const uint16_t *p, size_t ld, int valid)
     {
+        p8 = (uint32_t)(reinterpret_cast<uint64_t>(p) >> 4);
+        ld8 = (uint32_t)(ld / 8);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int row = threadIdx.x / kRowChunks + i * kRowsALoad, pos = threadIdx.x % kRowChunks;
-            if (KC) {
+            if (LINES) {
+                const int c = (pos ^ key(row)) - (int)((p8 + row * ld8) & 7);
+                k[i] = c * 8;
+                off[i] = row < valid ? row * (int)ld * 2 + c * 16 + 128 : kGtOutside;  // (from the line before on)
+            } else if (KC) {
                 const int c = pos ^ (row & 7);
                 k[i] = c * 8;
                 off[i] = row < valid ? row * (int)ld * 2 + c * 16 : kGtOutside;
@@ -125,14 +140,24 @@ struct GtTile {
     }
 
     // the tile at base (uniform), of whose k `left` remain
+    // (start: it is the first, LINES)
     template <bool NT = false>
-    __device__ __forceinline__ void load(const uint16_t *base, int left, uint32_t lds) const
+    __device__ __forceinline__ void load(const uint16_t *base, int left, uint32_t lds, bool start = false) const
     {
-        const u32x4 r = gt_resource(base);
+        const u32x4 r = gt_resource(LINES ? base - 64 : base);
         const uint32_t at = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / cdk::kWave) * 1024;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            gt_load_lds<NT>(r, k[i] < left ? off[i] : kGtOutside, at + i * (THREADS * 16));
+            gt_load_lds<NT>(r, k[i] < left && (!LINES || !start || k[i] >= 0) ? off[i] : kGtOutside,
+                            at + i * (THREADS * 16));
+    }
+
+    // the same operand, of LINES: its chunks lie in this tile (at `lds`) and the next
+    __device__ __forceinline__ u32x4 read_lines(const char *lds, int next, int r0, int kk) const
+    {
+        const int lane = threadIdx.x % cdk::kWave, i = lane % 16, c = kk * 4 + lane / 16 + (int)((p8 + i * ld8) & 7);
+        return *reinterpret_cast<const u32x4 *>(lds + (c < 8 ? 0 : next) + (r0 + i) * (BK * 2) +
+                                                (((c & 7) ^ key(i)) << 4));
     }
 
     // operand of rows r0..r0 + 15 and k 32 kk..32 kk + 31 (lane: row lane % 16, k 8 (lane / 16)..)
@@ -387,24 +412,24 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
 //
 // Few tokens wait for the weights, which long tiles of k (512 bytes of a row at a time) and 64 to 100 KB in
 // flight a CU bring at 5.8 to 6.4 TB/s: 4 tokens of 4096 x 11008 31 us, of 8192 x 28672 146. Some hundreds
-// wait for their tiles: a CU takes 35 to 45 bytes a ns of them, whatever their shape and the stages (rows
-// that do not begin on 128 bytes less: 333 tokens of 3000 x 8008 56 us, of 3008 x 8008 43).
+// wait for their tiles: a CU takes 35 to 45 bytes a ns of them, whatever their shape and the stages. Rows that
+// do not begin on 128 bytes cost two lines for one (333 tokens of 3000 x 8008 56 us, of 3008 x 8008 43): LINES.
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
 constexpr int kGtLds = std::max(STAGES * (BM + (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * BN) * BK * 2,
                                 (WK - 1) * WM * WN * (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * (BM / WM) *
                                     (BN / WN) * 4);  // the waves' sums
 
 // block: of the grid; lds: kGtLds bytes
-template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT>
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT, bool LINES = false>
 __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
 {
     constexpr int kThreads = WM * WN * WK * cdk::kWave;
     constexpr bool kTwo = KIND == kGtForward || KIND == kGtBackward;
     constexpr int NP = kTwo ? 2 : 1, FM = BM / WM / 16, FN = BN / WN / 16, KK = BK / 32 / WK;
-    using TM = GtTile<BM, BK, KIND != kGtDw, kThreads>;
-    using TN = GtTile<BN, BK, kTwo, kThreads>;
+    using TM = GtTile<BM, BK, KIND != kGtDw, kThreads, LINES>;
+    using TN = GtTile<BN, BK, kTwo, kThreads, LINES>;
     constexpr int kStage = TM::kBytes + NP * TN::kBytes;
-    constexpr int kFlight = (TM::kLoads + NP * TN::kLoads) * (STAGES - 2);
+    constexpr int kFlight = (TM::kLoads + NP * TN::kLoads) * (STAGES - (LINES ? 3 : 2));
     int mi, ni, split;
     if (!gt_place(block, KIND == kGtDw && a.out && a.out2 ? 2 * a.mt : a.mt, a.nt, kTwo ? 1 : a.splits, mi, ni, split))
         return;
@@ -419,8 +444,8 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
 
     TM tm;
     TN tn;
-    tm.init(ldm, M - m0);
-    tn.init(ldn, N - n0);
+    tm.init(kTwo ? a.x : a.d, ldm, M - m0);
+    tn.init(a.Wg, ldn, N - n0);
     const int first = kTwo ? 0 : split * a.ktiles;  // a split of the tiles of k
     const int all = (K + BK - 1) / BK * (kTwo ? 1 : KIND == kGtDx ? 2 * a.terms : a.terms);
     const int nk = kTwo ? all : min(a.ktiles, all - first);
@@ -429,10 +454,11 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
     const uint32_t base = gt_lds(lds);
     const auto issue = [&](int stage) {  // the next tile of k (zeros behind the last)
         const uint32_t at = base + stage * kStage;
-        tm.load(w.pm, w.left, at);
-        tn.template load<NT>(w.pn, w.left, at + TM::kBytes);
+        const bool start = LINES && w.left == K;
+        tm.load(w.pm, w.left, at, start);
+        tn.template load<NT>(w.pn, w.left, at + TM::kBytes, start);
         if constexpr (kTwo)
-            tn.template load<NT>(w.pn2, w.left, at + TM::kBytes + TN::kBytes);
+            tn.template load<NT>(w.pn2, w.left, at + TM::kBytes + TN::kBytes, start);
         w.advance(a, 0);
     };
 
@@ -452,20 +478,29 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
         issue(s);
     int stage = 0;
     for (int t = 0; t < nk; ++t) {
-        gt_wait<kFlight>();  // tile t is there, and every wave is done with tile t - 1
+        gt_wait<kFlight>();  // tile t is there (LINES: the next too), and every wave is done with tile t - 1
         issue(stage == 0 ? STAGES - 1 : stage - 1);
         const char *s = lds + stage * kStage;
+        const int next = stage + 1 == STAGES ? -stage * kStage : kStage;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
             u32x4 vm[FM], vn[NP][FN];
 #pragma unroll
             for (int j = 0; j < FM; ++j)
-                vm[j] = TM::read(s, (wm * FM + j) * 16, wk * KK + kk);
+                if constexpr (LINES)
+                    vm[j] = tm.read_lines(s, next, (wm * FM + j) * 16, wk * KK + kk);
+                else
+                    vm[j] = TM::read(s, (wm * FM + j) * 16, wk * KK + kk);
 #pragma unroll
             for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int i = 0; i < FN; ++i)
-                    vn[p][i] = TN::read(s + TM::kBytes + p * TN::kBytes, (wn * FN + i) * 16, wk * KK + kk);
+                for (int i = 0; i < FN; ++i) {
+                    const char *sn = s + TM::kBytes + p * TN::kBytes;
+                    if constexpr (LINES)
+                        vn[p][i] = tn.read_lines(sn, next, (wn * FN + i) * 16, wk * KK + kk);
+                    else
+                        vn[p][i] = TN::read(sn, (wn * FN + i) * 16, wk * KK + kk);
+                }
 #pragma unroll
             for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -534,11 +569,11 @@ __device__ __forceinline__ void gt_tile(const GtArgs &a, int block, char *lds)
     }
 }
 
-template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT>
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES, bool NT, bool LINES = false>
 __global__ __launch_bounds__(WM *WN *WK *cdk::kWave) void k_gt_product(const GtArgs a)
 {
     __shared__ __align__(1024) char lds[kGtLds<KIND, BM, BN, BK, WM, WN, WK, STAGES>];
-    gt_tile<KIND, BM, BN, BK, WM, WN, WK, STAGES, NT>(a, blockIdx.x, lds);
+    gt_tile<KIND, BM, BN, BK, WM, WN, WK, STAGES, NT, LINES>(a, blockIdx.x, lds);
 }
 
 constexpr int kGtBackK = 256;  // columns of k of its tiles of dx
@@ -598,11 +633,11 @@ __global__ __launch_bounds__(512) void k_gt_large(const GtArgs a)
 
     TM tm[MH];
     TN tn[2];
-    tm[0].init(ldm, M - m0);
+    tm[0].init(a.x, ldm, M - m0);
     if constexpr (MH == 2)
-        tm[1].init(ldm, M - m0 - 128);
-    tn[0].init(ldn, N - n0);
-    tn[1].init(ldn, N - n0 - (kTwo ? 0 : 128));
+        tm[1].init(a.x, ldm, M - m0 - 128);
+    tn[0].init(a.Wg, ldn, N - n0);
+    tn[1].init(a.Wg, ldn, N - n0 - (kTwo ? 0 : 128));
     const size_t mh = KIND == kGtDw ? 128 : 128 * ldm;  // to the second half of m
     GtWalk<KIND, BK> w;
     w.init(a, m0, n0, 128, second, first);
@@ -817,6 +852,19 @@ void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
         gt_sum<KIND>(a, s);
 }
 
+// whether rows begin inside a cache line
+bool gt_inside(const uint16_t *p, size_t ld) { return (reinterpret_cast<uintptr_t>(p) | ld * 2) % 128 != 0; }
+
+// Both projections by whole lines, four stages. Captured us a call against tiles of 64 columns as they lie: 333 tokens
+// of 3000 x 8008 47.0 / 55.9, 200 of 2040 x 5504 23.7 / 29.2, 180 of 4088 x 14336 63.8 / 84.1, 500 of 1000 x 3000 13.6 / 13.6.
+template <int KIND, int BM, int BN, int WM, int WN>
+void gt_lines(GtArgs a, hipStream_t s)
+{
+    gt_split<KIND>(a, 64, 1);
+    const int grid = gt_grid<KIND>(a, a.T, a.f, BM, BN);
+    k_gt_product<KIND, BM, BN, 64, WM, WN, 1, 4, false, true><<<grid, WM * WN * cdk::kWave, 0, s>>>(a);
+}
+
 template <int KIND, int MH>
 void gt_large(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
@@ -849,6 +897,7 @@ template <int KIND>
 void gt_projections(const GtArgs &a, hipStream_t s)
 {
     const auto fits = [&](int bm, int bn) { return (int64_t)ad_ceil(a.T, bm) * ad_ceil(a.f, bn) <= 256; };
+    const bool lines = gt_inside(a.x, a.ldx) || gt_inside(a.Wg, a.m);
     if (a.T <= 16)
         gt_product<KIND, 16, 16, 256, 1, 1, 4, 3>(a, a.T, a.f, s);
     else if (fits(32, 32))
@@ -857,6 +906,10 @@ void gt_projections(const GtArgs &a, hipStream_t s)
         gt_product<KIND, 64, 32, 128, 2, 2, 1, 4>(a, a.T, a.f, s);
     else if (a.T <= 64 || fits(64, 64))
         gt_product<KIND, 64, 64, 128, 2, 4, 1, 3>(a, a.T, a.f, s);
+    else if (lines && fits(128, 64))
+        gt_lines<KIND, 128, 64, 2, 4>(a, s);
+    else if (lines && fits(192, 64))
+        gt_lines<KIND, 192, 64, 4, 2>(a, s);
     else if (fits(128, 64))
         gt_product<KIND, 128, 64, 64, 2, 4, 1, 3>(a, a.T, a.f, s);
     else if (fits(192, 64))

@@ -337,6 +337,30 @@ def test_rows_past_32_bits(cd):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("m", [8, 56, 64, 72, 80, 96, 144, 200, 1000])
+@pytest.mark.parametrize("T,f,at", [(200, 5504, 0), (200, 5504, 24), (333, 8008, 0), (333, 8008, 40)])
+def test_rows_that_begin_inside_a_cache_line(cd, m, T, f, at):
+    c = Case(T, m, f)
+    wide = torch.full((T, m + 64), float("nan"), dtype=BF16, device="cuda")
+    x = wide[:, at:at + m]
+    x.copy_(c.x)
+    with cd.Gated(m, f, T, train=True) as p:
+        h = cd.countdown_gated_forward(p, x, c.Wg, c.Wu, h=torch.empty((T, f), device="cuda"))
+        check(h, *c.h(), "h")
+        for g, (name, (ref, bound)) in zip(cd.countdown_gated_backward(p, x, c.dh, c.Wg, c.Wu), c.grads(BF16).items()):
+            check(g, ref, bound, name)
+
+
+def test_weights_that_begin_inside_a_cache_line(cd):
+    c = Case(333, 192, 8008)
+    flat = torch.full((2 * 192 * 8008 + 64,), float("nan"), dtype=BF16, device="cuda")
+    n = 192 * 8008
+    Wg, Wu = flat[8:8 + n].view(8008, 192), flat[n + 32:2 * n + 32].view(8008, 192)  # by 16 and by 64 bytes
+    Wg.copy_(c.Wg), Wu.copy_(c.Wu)
+    with cd.Gated(192, 8008, 333) as p:
+        check(cd.countdown_gated_forward(p, c.x, Wg, Wu, h=torch.empty((333, 8008), device="cuda")), *c.h(), "h")
+
+
 def test_tokens_past_32_bits(cd):
     """h, dg and du of more than 2^32 bytes, against the last tokens alone."""
     T, m, f, n = 131080, 64, 8200, 300  # T 2 f > 2^31 elements
