@@ -855,14 +855,19 @@ void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 // whether rows begin inside a cache line
 bool gt_inside(const uint16_t *p, size_t ld) { return (reinterpret_cast<uintptr_t>(p) | ld * 2) % 128 != 0; }
 
-// Both projections by whole lines, four stages. Captured us a call against tiles of 64 columns as they lie: 333 tokens
-// of 3000 x 8008 47.0 / 55.9, 200 of 2040 x 5504 23.7 / 29.2, 180 of 4088 x 14336 63.8 / 84.1, 500 of 1000 x 3000 13.6 / 13.6.
-template <int KIND, int BM, int BN, int WM, int WN>
+// Both projections by whole lines. Captured us a call against the same tiles as they lie: 333 tokens of 3000 x 8008
+// 47.0 / 55.9, 200 of 2040 x 5504 23.7 / 29.2, 180 of 4088 x 14336 63.8 / 84.1, 32 of 4088 x 14336 44.0 / 52.8, 128 of
+// 3000 x 8008 30.3 / 35.1, 300 of 1000 x 3000 10.8 / 10.9. (64 x 32 tiles: 40 of 2040 x 5504 15.3 / 16.4, but 100 of
+// 1000 x 2200 8.9 / 8.2; 32 x 32: 60 of 1000 x 1000 8.5 / 6.7.)
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES = 4>
 void gt_lines(GtArgs a, hipStream_t s)
 {
     gt_split<KIND>(a, 64, 1);
     const int grid = gt_grid<KIND>(a, a.T, a.f, BM, BN);
-    k_gt_product<KIND, BM, BN, 64, WM, WN, 1, 4, false, true><<<grid, WM * WN * cdk::kWave, 0, s>>>(a);
+    if (BM <= 64 && a.mt == 1 && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
+        k_gt_product<KIND, BM, BN, 64, WM, WN, 1, STAGES, BM <= 64, true><<<grid, WM * WN * cdk::kWave, 0, s>>>(a);
+    else
+        k_gt_product<KIND, BM, BN, 64, WM, WN, 1, STAGES, false, true><<<grid, WM * WN * cdk::kWave, 0, s>>>(a);
 }
 
 template <int KIND, int MH>
@@ -904,6 +909,8 @@ void gt_projections(const GtArgs &a, hipStream_t s)
         gt_product<KIND, 32, 32, 128, 1, 2, 2, 4>(a, a.T, a.f, s);
     else if (fits(64, 32))
         gt_product<KIND, 64, 32, 128, 2, 2, 1, 4>(a, a.T, a.f, s);
+    else if (lines && (a.T <= 64 || fits(64, 64)))
+        gt_lines<KIND, 64, 64, 2, 4, 6>(a, s);
     else if (a.T <= 64 || fits(64, 64))
         gt_product<KIND, 64, 64, 128, 2, 4, 1, 3>(a, a.T, a.f, s);
     else if (lines && fits(128, 64))
