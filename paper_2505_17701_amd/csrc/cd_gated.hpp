@@ -93,9 +93,9 @@ __device__ __forceinline__ uint32_t gt_lds(const void *p)
 // by k & 3 and bit 3 of k, so that what the lanes of a transposing read take (rows 8 j + 0..3 of one
 // slot for 16 lanes, j = lane / 16) lies on different banks.
 //
-// LINES (KC, BK 64): rows that begin inside a cache line. A tile then holds a whole line of each row, of which the first
-// chunks may belong to the tile of k before, so that its loads take one line a row and not two; products read
-// two tiles in a row. Row r begins p8 + r ld8 chunks behind a line's start; its chunks' places in the line are
+// LINES (KC): rows that begin inside a cache line. A tile then holds whole lines of each row, of which the first
+// chunks may belong to the tile of k before, so that its loads take no line twice; products read two tiles in a
+// row. Row r begins p8 + r ld8 chunks behind a line's start; its chunks' places in the line are
 // permuted by the bits of r that this leaves alike.
 template <int R, int BK, bool KC, int THREADS, bool LINES = false>
 struct GtTile {
@@ -105,14 +105,15 @@ struct GtTile {
     static constexpr int kRowsALoad = THREADS / kRowChunks;
     static_assert(R * BK / 8 % THREADS == 0 && THREADS % kRowChunks == 0, "whole loads");
     static_assert(!KC || kRowsALoad % 8 == 0, "the row's swizzle is the same for every load");
-    static_assert(!LINES || (KC && BK == 64), "a line of a row");
+    static_assert(!LINES || KC, "lines of a row");
 
     int off[kLoads];  // byte offset from the tile's first element
     int k[kLoads];    // k of this thread's chunks
-    uint32_t p8, ld8;
+    uint32_t p8, ld8;  // LINES: the operand's address and row length, in chunks
 
     static __device__ __forceinline__ int slot_key(int k) { return ((k & 3) | (k >> 1 & 4)) & (R / 16 - 1); }
 
+    // LINES: eight rows begin at 8, 4, 2 or 1 places of a line by ld8's factors of 2; r's other bits tell the rest apart
     __device__ __forceinline__ int key(int r) const { return (r & 7) >> (3 - __builtin_ctz(ld8 | 8u)); }
 
     // p: the operand; valid: its rows (KC) or columns from this tile on
@@ -139,8 +140,7 @@ struct GtTile {
         }
     }
 
-    // the tile at base (uniform), of whose k `left` remain
-    // (start: it is the first, LINES)
+    // the tile at base (uniform), of whose k `left` remain (start: it is the first, LINES)
     template <bool NT = false>
     __device__ __forceinline__ void load(const uint16_t *base, int left, uint32_t lds, bool start = false) const
     {
@@ -156,8 +156,8 @@ struct GtTile {
     __device__ __forceinline__ u32x4 read_lines(const char *lds, int next, int r0, int kk) const
     {
         const int lane = threadIdx.x % cdk::kWave, i = lane % 16, c = kk * 4 + lane / 16 + (int)((p8 + i * ld8) & 7);
-        return *reinterpret_cast<const u32x4 *>(lds + (c < 8 ? 0 : next) + (r0 + i) * (BK * 2) +
-                                                (((c & 7) ^ key(i)) << 4));
+        return *reinterpret_cast<const u32x4 *>(lds + (c < kRowChunks ? 0 : next) + (r0 + i) * (BK * 2) +
+                                                ((c % kRowChunks ^ key(i)) << 4));
     }
 
     // operand of rows r0..r0 + 15 and k 32 kk..32 kk + 31 (lane: row lane % 16, k 8 (lane / 16)..)
@@ -857,17 +857,18 @@ bool gt_inside(const uint16_t *p, size_t ld) { return (reinterpret_cast<uintptr_
 
 // Both projections by whole lines. Captured us a call against the same tiles as they lie: 333 tokens of 3000 x 8008
 // 47.0 / 55.9, 200 of 2040 x 5504 23.7 / 29.2, 180 of 4088 x 14336 63.8 / 84.1, 32 of 4088 x 14336 44.0 / 52.8, 128 of
-// 3000 x 8008 30.3 / 35.1, 300 of 1000 x 3000 10.8 / 10.9. (64 x 32 tiles: 40 of 2040 x 5504 15.3 / 16.4, but 100 of
-// 1000 x 2200 8.9 / 8.2; 32 x 32: 60 of 1000 x 1000 8.5 / 6.7.)
-template <int KIND, int BM, int BN, int WM, int WN, int STAGES = 4>
+// 3000 x 8008 30.3 / 35.1, 40 of 2040 x 5504 14.8 / 16.5, 60 of 2000 x 3000 11.3 / 12.8, 17 of 1000 x 2056 6.6 / 6.5. Not for
+// 16 tokens: 8 of 4088 x 14336 40.0 / 43.2, 4 of 1000 x 3000 5.7 / 5.2. The large tiles have no room for the stage
+// more that this takes (8192 tokens of 4088 x 14336 1505 us, of 4096 x 14336 1294).
+template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
 void gt_lines(GtArgs a, hipStream_t s)
 {
-    gt_split<KIND>(a, 64, 1);
+    gt_split<KIND>(a, BK, 1);
     const int grid = gt_grid<KIND>(a, a.T, a.f, BM, BN);
     if (BM <= 64 && a.mt == 1 && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
-        k_gt_product<KIND, BM, BN, 64, WM, WN, 1, STAGES, BM <= 64, true><<<grid, WM * WN * cdk::kWave, 0, s>>>(a);
+        k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, BM <= 64, true><<<grid, WM * WN * WK * cdk::kWave, 0, s>>>(a);
     else
-        k_gt_product<KIND, BM, BN, 64, WM, WN, 1, STAGES, false, true><<<grid, WM * WN * cdk::kWave, 0, s>>>(a);
+        k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, false, true><<<grid, WM * WN * WK * cdk::kWave, 0, s>>>(a);
 }
 
 template <int KIND, int MH>
@@ -905,18 +906,22 @@ void gt_projections(const GtArgs &a, hipStream_t s)
     const bool lines = gt_inside(a.x, a.ldx) || gt_inside(a.Wg, a.m);
     if (a.T <= 16)
         gt_product<KIND, 16, 16, 256, 1, 1, 4, 3>(a, a.T, a.f, s);
+    else if (lines && fits(32, 32))
+        gt_lines<KIND, 32, 32, 128, 1, 2, 2, 5>(a, s);
     else if (fits(32, 32))
         gt_product<KIND, 32, 32, 128, 1, 2, 2, 4>(a, a.T, a.f, s);
+    else if (lines && fits(64, 32))
+        gt_lines<KIND, 64, 32, 128, 2, 2, 1, 5>(a, s);
     else if (fits(64, 32))
         gt_product<KIND, 64, 32, 128, 2, 2, 1, 4>(a, a.T, a.f, s);
     else if (lines && (a.T <= 64 || fits(64, 64)))
-        gt_lines<KIND, 64, 64, 2, 4, 6>(a, s);
+        gt_lines<KIND, 64, 64, 64, 2, 4, 1, 6>(a, s);
     else if (a.T <= 64 || fits(64, 64))
         gt_product<KIND, 64, 64, 128, 2, 4, 1, 3>(a, a.T, a.f, s);
     else if (lines && fits(128, 64))
-        gt_lines<KIND, 128, 64, 2, 4>(a, s);
+        gt_lines<KIND, 128, 64, 64, 2, 4, 1, 4>(a, s);
     else if (lines && fits(192, 64))
-        gt_lines<KIND, 192, 64, 4, 2>(a, s);
+        gt_lines<KIND, 192, 64, 64, 4, 2, 1, 4>(a, s);
     else if (fits(128, 64))
         gt_product<KIND, 128, 64, 64, 2, 4, 1, 3>(a, a.T, a.f, s);
     else if (fits(192, 64))

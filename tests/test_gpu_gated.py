@@ -338,7 +338,7 @@ def test_rows_past_32_bits(cd):
 
 
 @pytest.mark.parametrize("m", [8, 56, 64, 72, 80, 96, 144, 200, 1000])
-@pytest.mark.parametrize("T,f,at", [(200, 5504, 0), (200, 5504, 24), (333, 8008, 0), (333, 8008, 40)])
+@pytest.mark.parametrize("T,f,at", [(200, 5504, 0), (200, 5504, 24), (40, 2056, 0), (60, 4104, 8), (333, 8008, 0), (333, 8008, 40)])
 def test_rows_that_begin_inside_a_cache_line(cd, m, T, f, at):
     c = Case(T, m, f)
     wide = torch.full((T, m + 64), float("nan"), dtype=BF16, device="cuda")
