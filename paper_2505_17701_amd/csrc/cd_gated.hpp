@@ -58,19 +58,23 @@ __device__ __forceinline__ u32x4 gt_resource(const void *p)
 }
 
 // 16 bytes a lane from the resource to LDS at `lds` + 16 lane. The builtin would do, but the compiler
-// then waits for every load in flight before each LDS read. Nothing is written but LDS and m0 (which
-// compiled code sets where it uses it, and does not in these kernels); the waits and barriers are gt_wait's.
+// then waits for every load in flight before each LDS read. Nothing is written but LDS and m0, which is
+// named: code that the compiler sets it for sets it again behind this. (The warning ignored is that it would not be
+// kept for a program that relied on it across the statement.) The waits and barriers are gt_wait's.
 // NT: past the caches.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool NT = false>
 __device__ __forceinline__ void gt_load_lds(const u32x4 &r, int off, uint32_t lds)
 {
     if constexpr (NT)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
-                     ::"s"(lds), "v"(off), "s"(r) : "memory");
+                     ::"s"(lds), "v"(off), "s"(r) : "memory", "m0");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     ::"s"(lds), "v"(off), "s"(r) : "memory");
+                     ::"s"(lds), "v"(off), "s"(r) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // All but the last N loads of this wave have come, and its LDS reads; then every wave's have.
 template <int N>
