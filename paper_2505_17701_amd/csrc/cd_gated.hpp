@@ -846,9 +846,13 @@ void gt_product(GtArgs a, int M, int N, hipStream_t s, int splits = 1)
 {
     gt_split<KIND>(a, BK, splits);
     const int grid = gt_grid<KIND>(a, M, N, BM, BN), block = WM * WN * WK * cdk::kWave;
-    // Weights that are read once and would sweep most of the last-level cache go past it.
+    // Weights that this launch reads once and that would sweep most of the last-level cache go past it. (The
+    // backward call's projections too, though dx reads them again.) dx of several terms reads them once a term, from
+    // L2 but for the first, and keeps to the caches; fp32 gradients, captured us a call against going past them:
+    // 64 tokens of 8192 x 28672 953 / 1095, of 4096 x 14336 283 / 302, 4 tokens of 4096 x 11008 191 / 201, one of
+    // 4096 x 14336 244 / 237.
     constexpr bool weights = KIND != kGtDw && BM <= 64;
-    if (weights && a.mt == 1 && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
+    if (weights && a.mt == 1 && (KIND != kGtDx || a.terms == 1) && (size_t)a.f * a.m * 4 > ((size_t)64 << 20))
         k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, weights><<<grid, block, 0, s>>>(a);
     else
         k_gt_product<KIND, BM, BN, BK, WM, WN, WK, STAGES, false><<<grid, block, 0, s>>>(a);
