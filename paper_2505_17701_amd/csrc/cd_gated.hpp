@@ -379,7 +379,8 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
             const uint32_t p = (uint32_t)(w[i] >> (r / 2 * 32));
             const float dh = r % 2 ? cdk::bf16_hi(p) : cdk::bf16_lo(p);
             const float s = gt_sigmoid(g[i][r]);
-            d[0][i][r] = dh * u[i][r] * (s * (1.0f + g[i][r] * (1.0f - s)));
+            // (dh u first would overflow where the slope brings it back; the slope is at most 1.1)
+            d[0][i][r] = dh * (u[i][r] * (s * (1.0f + g[i][r] * (1.0f - s))));
             d[1][i][r] = dh * (g[i][r] * s);
         }
 #pragma unroll

@@ -36,3 +36,26 @@ def forward_and_backward(cd, shape, dtype):
                                          ((4, 4096, 4104), BF16)], ids=str)
 def test_weights_of_several_terms(cd, shape, dtype):
     forward_and_backward(cd, shape, dtype)
+
+
+def test_gradients_whose_factors_alone_overflow(cd):
+    """dg = dh u SiLU'(g) where dh u is past the largest number and the slope brings it back, or is 0.
+
+    u = 2^125, dh = 2^14, both exact. dg is off by 16 (1 + |g|) s u 2^-23 as in test_gpu_gated.py, of which the slope is
+    a part of (|g| - 1) / (|g| + 1) and more, 17 units; dx sums eight equal terms of three parts each, all of one
+    sign or below 2^-7 of it: 24 additions, each off by 2^-24. (W_up's factors meet du in another column.)"""
+    x = torch.zeros((4, 64), device="cuda")
+    x[:, 0] = torch.tensor([-200.0, -60.0, -40.0, 2.0 ** -60])
+    x[:, 1] = 2.0 ** 62
+    W, V = torch.zeros((8, 64), device="cuda"), torch.zeros((8, 64), device="cuda")
+    W[:, 0], V[:, 1] = 1.0, 2.0 ** 63
+    x, W, V = x.to(BF16), W.to(BF16), V.to(BF16)
+    dh = torch.full((4, 8), 2.0 ** 14, device="cuda", dtype=BF16)
+    dh[3] = 2.0 ** -14
+    with cd.Gated(64, 8, 4, train=True, fp32_grads=True) as p:
+        dx, _, _ = cd.countdown_gated_backward(p, x, dh, W, V, need=(True, False, False))
+    g = x[:, 0].double()
+    s = torch.sigmoid(g)
+    want = 8 * dh[:, 0].double() * 2.0 ** 125 * torch.where(g == -200.0, 0.0, s * (1 + g * (1 - s)))
+    assert bool(torch.isfinite(dx).all())
+    assert bool(((dx[:, 0].double() - want).abs() <= 32 * 2.0 ** -23 * want.abs()).all())
