@@ -433,8 +433,9 @@ void q4_launch(const Q4Args &a, hipStream_t s)
 template <int NM, int G, bool GATED>
 void q4_launch(const Q4Args &a, hipStream_t s)
 {
-    if (a.T <= 4)
-        q4_launch<NM, G, 4, GATED>(a, s);
+    constexpr bool few = GATED || NM == 1;  // (two row tiles of one matrix: from five tokens on)
+    if (few && a.T <= 4)
+        q4_launch<NM, G, few ? 4 : 8, GATED>(a, s);
     else if (a.T <= 8)
         q4_launch<NM, G, 8, GATED>(a, s);
     else

@@ -2,6 +2,8 @@
 cache lines, loads past the caches, row tiles and waves, at both sides of each rule (from the library's own host
 code on a machine without a GPU, see host_hip.py)."""
 import ctypes as C
+import re
+import subprocess
 from types import SimpleNamespace
 
 import pytest
@@ -50,3 +52,49 @@ def launches(host, T, m, f, type=1, **kw):
 def test_dx_reads_weights_past_the_caches_once(host, T, m, f, type, past):
     _, kernels = launches(host, T, m, f, type, dWg=None, dWu=None)
     assert kernels[1] == f"k_gt_product<2,64,128,64,2,2,1,3,{past},0>"
+
+
+def compiled(host, kernel):
+    """The instantiations of a kernel that the library holds."""
+    out = subprocess.run(["nm", "-C", host.lib._name], check=True, capture_output=True, text=True).stdout
+    found = re.findall(rf"\(anonymous namespace\)::__device_stub__({kernel}<[^>]*>)", out)
+    assert found
+    return {name(k) for k in found}
+
+
+# tokens, rows, cols of a project call; its row tiles, room for tokens, waves, and whether past the caches
+Q4_PROJECT = [
+    (1, 72, 264, 1, 4, 8, 0), (4, 6144, 264, 1, 4, 8, 0), (3, 4088, 33000, 1, 4, 8, 1),
+    (5, 6136, 264, 1, 8, 8, 0), (8, 4088, 520, 1, 8, 8, 0), (7, 4088, 33000, 1, 8, 8, 1),
+    (5, 6144, 264, 2, 8, 8, 0), (8, 8200, 264, 2, 8, 8, 0), (6, 8200, 17000, 2, 8, 8, 1),
+    (9, 4096, 264, 1, 16, 8, 0), (16, 4088, 33000, 1, 16, 8, 1),
+    (13, 4104, 1000, 1, 16, 4, 0), (16, 6136, 712, 1, 16, 4, 0), (13, 5000, 28680, 1, 16, 4, 1),
+    (9, 6144, 264, 2, 16, 8, 0), (16, 8192, 264, 2, 16, 8, 0), (9, 8184, 17000, 2, 16, 8, 1),
+    (9, 8200, 1000, 2, 16, 4, 0), (16, 8200, 17000, 2, 16, 4, 1),
+]
+# the same of a gated call, which has a tile of either matrix
+Q4_GATED = [
+    (1, 72, 264, 4, 8, 0), (4, 4104, 264, 4, 8, 0), (2, 4088, 16408, 4, 8, 1),
+    (5, 4104, 264, 8, 8, 0), (8, 72, 264, 8, 8, 0), (8, 4088, 16408, 8, 8, 1),
+    (9, 4096, 264, 16, 8, 0), (16, 4088, 16408, 16, 8, 1),
+    (13, 4104, 1000, 16, 4, 0), (11, 5000, 13096, 16, 4, 1),
+]
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_kernels_of_the_4_bit_calls(host, group):
+    seen = set()
+    for T, rows, cols, *want in Q4_PROJECT:
+        host.launches()
+        assert host.lib.countdown_q4_project(X, cols, T, WG, cols, rows, group, 0, None, 0, H, rows, None) == 0
+        (kernel, _), = host.launches()
+        tiles, room, waves, past = want
+        assert name(kernel) == f"k_q4<{tiles},{group},{room},{waves},0,{past}>", (T, rows, cols)
+        seen.add(name(kernel))
+    for T, rows, cols, room, waves, past in Q4_GATED:
+        host.launches()
+        assert host.lib.countdown_q4_gated(X, cols, T, WG, WU, cols, rows, group, 1, H, rows, None) == 0
+        (kernel, _), = host.launches()
+        assert name(kernel) == f"k_q4<2,{group},{room},{waves},1,{past}>", (T, rows, cols)
+        seen.add(name(kernel))
+    assert seen == {k for k in compiled(host, "k_q4") if k.split(",")[1] == str(group)}
