@@ -534,12 +534,16 @@ cd_status countdown_gated_backward(cd_gated *gated, const uint16_t *x, size_t ld
  * e = 2 p plus 8 at bits 4 p, that of e = 2 p + 1 at bits 16 + 4 p. Padding has code 0, scale 0.
  *
  * Products and sums are fp32: a code enters as 24 + code and 24 times the group's sum of x leaves
- * again, so |x| must stay below 2^100, and an infinity in x or a scale reaches its results as
- * infinity or NaN. x, base, y, h and W have row strides, base may be y itself, and outputs must
- * not share memory with inputs, as for the adapters' calls. Up to 16 tokens (CD_EUNSUPPORTED
- * beyond: unpack the weights and use a matrix product, e.g. countdown_gated_forward); T = 0 is a
- * valid empty call. No workspace: calls may overlap. The same call on the same inputs gives the
- * same bits.
+ * again, so |x| must stay below 2^100, and roundings are those of sums over (24 + code) scale x
+ * whatever the codes: smaller codes do not make them smaller. 4096 columns in groups of 128 are off
+ * by 1e-7 (2-norm, of the result) with codes spread over -8..7, by 5e-7 with codes of -1..1, and codes
+ * that are all 0 beside a scale that is not give up to some 2e-8 of the row's sum of |scale x| instead
+ * of 0 (a scale of 0 gives 0). An infinity in x or a scale reaches its results as infinity or NaN.
+ *
+ * x, base, y, h and W have row strides, base may be y itself, and outputs must not share memory with
+ * inputs, as for the adapters' calls. Up to 16 tokens (CD_EUNSUPPORTED beyond: unpack the weights and
+ * use a matrix product, e.g. countdown_gated_forward); T = 0 is a valid empty call. No workspace: calls
+ * may overlap. The same call on the same inputs gives the same bits.
  */
 /* Bytes of a packed matrix; 0 for sizes that the calls refuse. Host only. */
 size_t countdown_q4_bytes(int rows, int cols, int group);

@@ -9,6 +9,10 @@
 // is exactly 24 + c, two instructions for a pair of weights; the 24 goes again with one more product,
 // of -24 and the same tokens, that the sums of a group start from. Sums are fp32, the group's scale
 // multiplies a group's sum, not its weights.
+// Roundings are thus those of sums over 24 + code: 2-norm errors of 4096 columns 0.9e-7 to 1.2e-7 with codes over -8..7
+// (fp32 sums of the weights themselves 2.6e-7), but 1.5e-7 (G 32) to 5.2e-7 (G 128) with codes of -1..1 (1.3e-7),
+// and zero codes need not give 0. Sums of 24 and of 24 + code side by side, and their difference, give 0 there; other
+// errors are then up to twice as large, and G 32 up to 9 % slower (16 tokens of 8192 -> 28672 gated 77 us against 70).
 //
 // Packed layout: blocks of 16 rows x 128 columns, the blocks of 16 rows one after another in groups of eight
 // (the last group may have fewer): the codes of a group's blocks, 1024 bytes each, then their
