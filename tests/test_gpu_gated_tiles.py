@@ -6,6 +6,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from test_gpu_gated import BF16, F32, Case, check  # noqa: E402
+from test_host_gated_routes import PROJECTIONS  # noqa: E402
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -21,14 +22,24 @@ def cd():
     return binding
 
 
-def forward_and_backward(cd, shape, dtype):
+def forward_and_backward(cd, shape, dtype, at=0):
     c = Case(*shape)
+    if at:  # rows of x at `at` of longer ones
+        wide = torch.full((c.T, c.m + 64), float("nan"), dtype=BF16, device="cuda")
+        wide[:, at:at + c.m] = c.x
+        c.x = wide[:, at:at + c.m]
     with cd.Gated(c.m, c.f, c.T, train=True, fp32_grads=dtype is F32) as p:
         h = cd.countdown_gated_forward(p, c.x, c.Wg, c.Wu, h=torch.empty((c.T, c.f), dtype=dtype, device="cuda"))
         got = cd.countdown_gated_backward(p, c.x, c.dh, c.Wg, c.Wu)
     check(h, *c.h(), "h")
     for g, (name, (ref, bound)) in zip(got, c.grads(dtype).items()):
         check(g, ref, bound, name)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("call", [c[:4] for c in PROJECTIONS], ids=str)
+def test_every_tile_of_the_projections(cd, call, dtype):
+    forward_and_backward(cd, call[:3], dtype, call[3])
 
 
 # more than 64 MB of weights: dx of fp32 gradients (three terms), of two terms, of one

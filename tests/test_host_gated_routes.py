@@ -98,3 +98,56 @@ def test_kernels_of_the_4_bit_calls(host, group):
         assert name(kernel) == f"k_q4<2,{group},{room},{waves},1,{past}>", (T, rows, cols)
         seen.add(name(kernel))
     assert seen == {k for k in compiled(host, "k_q4") if k.split(",")[1] == str(group)}
+
+
+# tokens, d_model, d_ff, elements before x in its rows (which are 64 longer then); the tile of both projections: rows,
+# columns, k, waves of each, stages, past the caches, whole cache lines (large: halves of 128 rows)
+PROJECTIONS = [
+    (1, 256, 688, 0, "16,16,256,1,1,4,3,0,0"), (16, 264, 688, 8, "16,16,256,1,1,4,3,0,0"),
+    (16, 2120, 8192, 0, "16,16,256,1,1,4,3,1,0"),
+    (17, 256, 2048, 0, "32,32,128,1,2,2,4,0,0"), (17, 264, 2048, 0, "32,32,128,1,2,2,5,0,1"),
+    (17, 256, 2048, 8, "32,32,128,1,2,2,5,0,1"), (17, 256, 2048, 64, "32,32,128,1,2,2,4,0,0"),
+    (20, 2112, 8192, 0, "32,32,128,1,2,2,4,1,0"), (20, 2120, 8192, 0, "32,32,128,1,2,2,5,1,1"),
+    (128, 256, 4096, 0, "64,32,128,2,2,1,4,0,0"), (128, 264, 4096, 0, "64,32,128,2,2,1,5,0,1"),
+    (48, 2112, 8192, 0, "64,32,128,2,2,1,4,1,0"), (48, 2120, 8192, 0, "64,32,128,2,2,1,5,1,1"),
+    (200, 128, 3000, 0, "64,64,128,2,4,1,3,0,0"), (200, 128, 3000, 24, "64,64,64,2,4,1,6,0,1"),
+    (64, 2048, 8200, 0, "64,64,128,2,4,1,3,1,0"), (64, 2056, 8200, 0, "64,64,64,2,4,1,6,1,1"),
+    (500, 64, 3000, 0, "128,64,64,2,4,1,3,0,0"), (500, 72, 3000, 0, "128,64,64,2,4,1,4,0,1"),
+    (700, 64, 3520, 0, "192,64,64,4,2,1,3,0,0"), (700, 64, 3520, 40, "192,64,64,4,2,1,4,0,1"),
+    (900, 64, 4000, 0, "large1"), (900, 72, 4000, 0, "large1"), (2000, 264, 4104, 0, "large2"),
+]
+# tokens, d_model, d_ff, type (1 bf16, 0 fp32); the kernels behind the projections of a backward call
+BEHIND = [
+    (37, 256, 688, 1, "k_gt_back"), (300, 256, 1024, 0, "k_gt_product<2,64,128,64,2,2,1,3,0,0>",
+                                     "k_gt_product<3,64,64,64,2,2,1,3,0,0>"),
+    (4, 4096, 4104, 1, "k_gt_product<2,64,128,64,2,2,1,3,1,0>", "k_gt_product<3,128,128,64,2,2,1,2,0,0>"),
+    (1300, 1544, 2056, 1, "k_gt_large<2,2>", "k_gt_product<3,128,128,64,2,2,1,2,0,0>"),
+    (520, 2048, 2816, 0, "k_gt_large<2,2>", "k_gt_large<3,2>"),
+]
+
+
+def projection(kind, tile):
+    return f"k_gt_large<{kind},{tile[5:]}>" if tile.startswith("large") else f"k_gt_product<{kind},{tile}>"
+
+
+def test_kernels_of_the_gated_block(host):
+    seen = set()
+    for T, m, f, at, tile in PROJECTIONS:
+        forward, backward = launches(host, T, m, f, x=X + 2 * at, ldx=m + (64 if at else 0))
+        assert forward == [projection(0, tile)] and backward[0] == projection(1, tile), (T, m, f, at)
+        seen.update(forward + backward)
+    for T, m, f, type, *want in BEHIND:
+        _, kernels = launches(host, T, m, f, type)
+        assert [k for k in kernels[1:] if not k.startswith("k_gt_sum")] == want, (T, m, f, type)
+        seen.update(kernels)
+    for kernel in ("k_gt_product", "k_gt_large"):
+        assert {k for k in seen if k.startswith(kernel)} == compiled(host, kernel)
+
+
+def test_what_begins_inside_a_cache_line(host):
+    """x's first row, its row length, the weights' row length or W_gate's first row."""
+    for kw, lines in (({}, 0), ({"x": X + 16}, 1), ({"x": X + 128, "ldx": 320}, 0), ({"ldx": 264}, 1),
+                      ({"Wg": WG + 64}, 1), ({"Wg": WG + 256}, 0)):
+        forward, backward = launches(host, 200, 256, 3000, **kw)
+        tile = "64,64,64,2,4,1,6,0,1" if lines else "64,64,128,2,4,1,3,0,0"
+        assert forward == [projection(0, tile)] and backward[0] == projection(1, tile), kw
