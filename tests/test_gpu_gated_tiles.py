@@ -70,3 +70,32 @@ def test_gradients_whose_factors_alone_overflow(cd):
     want = 8 * dh[:, 0].double() * 2.0 ** 125 * torch.where(g == -200.0, 0.0, s * (1 + g * (1 - s)))
     assert bool(torch.isfinite(dx).all())
     assert bool(((dx[:, 0].double() - want).abs() <= 32 * 2.0 ** -23 * want.abs()).all())
+
+
+def test_forward_calls_of_one_handle_at_once(cd):
+    """The forward call uses no workspace."""
+    cases = [Case(300, 520, 2056, seed=s) for s in (1, 2)]
+    with cd.Gated(520, 2056, 300) as p:
+        want = [cd.countdown_gated_forward(p, c.x, c.Wg, c.Wu) for c in cases]
+        torch.cuda.synchronize()
+        streams, got = [torch.cuda.Stream() for _ in cases], []
+        for _ in range(8):
+            for c, s in zip(cases, streams):
+                with torch.cuda.stream(s):
+                    got.append(cd.countdown_gated_forward(p, c.x, c.Wg, c.Wu))
+        torch.cuda.synchronize()
+    for i, h in enumerate(got):
+        assert torch.equal(h, want[i % 2])
+
+
+@pytest.mark.parametrize("T", [5, 300])
+def test_one_matrix_for_both_projections(cd, T):
+    """Inputs may be one and the same."""
+    c = Case(T, 264, 712)
+    c.Wu = c.Wg
+    with cd.Gated(c.m, c.f, T, train=True, fp32_grads=True) as p:
+        h = cd.countdown_gated_forward(p, c.x, c.Wg, c.Wg, h=torch.empty((T, c.f), device="cuda"))
+        got = cd.countdown_gated_backward(p, c.x, c.dh, c.Wg, c.Wg)
+    check(h, *c.h(), "h")
+    for g, (name, (ref, bound)) in zip(got, c.grads(F32).items()):
+        check(g, ref, bound, name)
