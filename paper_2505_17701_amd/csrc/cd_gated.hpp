@@ -417,7 +417,9 @@ __device__ __forceinline__ void gt_backward(const GtArgs &a, size_t t, int n, bo
 //
 // Few tokens wait for the weights, which long tiles of k (512 bytes of a row at a time) and 64 to 100 KB in
 // flight a CU bring at 5.8 to 6.4 TB/s: 4 tokens of 4096 x 11008 31 us, of 8192 x 28672 146. Some hundreds
-// wait for their tiles: a CU takes 35 to 45 bytes a ns of them, whatever their shape and the stages. Rows that
+// wait for their tiles: a CU takes 35 to 45 bytes a ns of them, whatever their shape and the stages (the loads alone, without
+// reads and products, 38.8 us of 46.5 at 333 tokens of 3000 x 8008 and 61.5 of 62.1 at 128 of 4096 x 14336; reads and
+// products alone 34 and 32, the matrix cores 32 and 19 % busy). Rows that
 // do not begin on 128 bytes cost two lines for one (333 tokens of 3000 x 8008 56 us, of 3008 x 8008 43): LINES.
 template <int KIND, int BM, int BN, int BK, int WM, int WN, int WK, int STAGES>
 constexpr int kGtLds = std::max(STAGES * (BM + (KIND == kGtForward || KIND == kGtBackward ? 2 : 1) * BN) * BK * 2,
@@ -1153,10 +1155,12 @@ cd_status countdown_gated_backward(cd_gated *p, const uint16_t *x, size_t ldx, c
     a.d = p->d;
     a.fd = gt_fd(p->f);
     a.part = p->part;
-    // The errors of few rounded numbers do not average out in a gradient (that of one token over 64
-    // neurons may be 1.5 times as far off as its own rounding puts it, over many 1.41); a second term
-    // takes them out. Everywhere it would cost 3 us (of 16: 37 tokens, 256 x 688) to 35 (of 145: one
-    // token, 4096 x 11008).
+    // One bf16 term is the operand of a bf16 product: a gradient's 2-norm error is then 1.41 times that of its own
+    // rounding, over many independent roundings (2.3e-3 against 1.7e-3). Over few it may by chance be 1.5 times
+    // (one token, 64 neurons), and a second term takes the first rounding out. The border is one of cost, 3 us
+    // (of 16: 37 tokens, 256 x 688) to 35 (of 145: one token, 4096 x 11008) and twice the products of dx and of the weights'
+    // gradients, and of whole outputs, not of rows: on either side, what one token adds to a row of dW has one
+    // rounding, beyond the border by up to 2^-8. Who needs more takes fp32 gradients.
     a.terms = type == CD_TYPE_F32 ? kGtTerms : (int64_t)T * a.f <= kGtFew ? 2 : 1;
     gt_projections<kGtBackward>(a, s);
     GtArgs ax = a, aw = a;

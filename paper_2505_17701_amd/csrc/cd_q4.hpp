@@ -92,8 +92,9 @@ __host__ __device__ constexpr int q4_stages(int stage)
 
 // Bound by the stream of the codes and, with many tokens, by that of the tokens (each workgroup reads them
 // all from L2; two row tiles a part halve that): 8192 -> 28672 gated at one token, 242 MB, 46 us (5.2 TB/s; the
-// same loads without products 42, a plain stream 35); 4096 -> 11008 gated at 13 tokens, 51 MB, 19.5 (4 of
-// them the tokens' loads). Deeper rings, tokens whole in LDS and twice the waves measured the same or slower.
+// same loads without products 43, a plain stream 35); 4096 -> 11008 gated at 13 tokens, 51 MB, 19.6 (the loads alone
+// 16.4, products alone 12.3); 14336 -> 4096 at 1, 8 and 16 tokens 11.0, 12.6 and 14.3, the loads alone 8.4, 11.9 and 13.7
+// (products alone 8.7 to 9). Deeper rings, tokens whole in LDS and twice the waves measured the same or slower.
 //
 // A part is 16 rows of both matrices (gated), or NM x 16 rows of one; a workgroup takes part after part. A
 // step is 1024 columns, a block of each of NM row tiles for each wave; its codes, scales and tokens go to
